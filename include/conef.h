@@ -427,6 +427,88 @@ int conef_matrix_family(const conef_ctx *ctx, int mat, int *family);
 void conef_destroy(conef_ctx *ctx);
 const char *conef_strerror(int code);
 
+/* ---- A worker's own step in front of the compressor: dropout, layer norm and products in microscaled 4-bit floating point.
+ * These calls have no context.  What they share with the rest: caller-owned device memory, the caller's stream, no
+ * allocation and no synchronisation, draws from Philox4x32-10 by counter, so that no mask and no noise is ever stored.
+ * A matrix is rows x cols elements (CONEF_F32 or CONEF_BF16), one after the other in a row, with `pitch` >= cols elements
+ * from a row to the next; its address is a multiple of its element's size, no more.  An output may be an input's buffer
+ * (same address and pitch) unless stated otherwise.  0 rows: nothing is read or written (sums over rows are 0).
+ * rows < 2^31, 1 <= cols < 2^31, rows ceil(cols / 8) < 2^32.  Sums are fp32 or wider, in an order that depends on the sizes only,
+ * and results are rounded once, to the output's type.
+ * Draws: element (i, j) uses 16 bits, half (j & 1) of word (j & 7) >> 1 of the call with counter (i ceil(cols / 8) + j / 8,
+ * base + site, lo32(step), hi32(step)) and key (lo32(seed), hi32(seed)); base is 3 2^30 for dropout, 3 2^30 + 2^27 and
+ * 3 2^30 + 2^28 for the quantisation by rows and by columns; `site` < 2^27 tells a model's places apart.
+ * Errors: CONEF_EINVAL, CONEF_EHIP as for conef_step. */
+
+/* A dropout: p in [0, 1) is the share dropped, taken as T = floor(65536 p + 1/2) parts in 65536 (65535 at most).
+ * keep(v) of an element is v where its draw is at least T and 0 elsewhere; kept ones are scaled by s = fl32(65536 / (65536 - T)). */
+typedef struct { float p; uint32_t site; uint64_t seed, step; } conef_drop;
+
+/* y <- residual + s keep(x), each operation in fp32; residual may be null (nothing is added).
+ * The backward pass draws the same mask again: dx <- s keep(dy); the residual's gradient is dy. */
+int conef_dropout_forward(const conef_drop *drop, int64_t rows, int64_t cols, int dtype, const void *x, int64_t x_pitch,
+                          const void *residual, int64_t residual_pitch, void *y, int64_t y_pitch, void *hip_stream);
+int conef_dropout_backward(const conef_drop *drop, int64_t rows, int64_t cols, int dtype, const void *dy, int64_t dy_pitch,
+                           void *dx, int64_t dx_pitch, void *hip_stream);
+
+/* Layer norm over each row, with a dropout and a residual in front of it:
+ *   z = residual + s keep(x)     y = (z - mean) rstd gamma + beta,  rstd = 1 / sqrt(variance + eps)
+ * drop, residual   either may be null; with both null z is x, and z_out has to be null (CONEF_EINVAL otherwise)
+ * z_out            device, out, needed if drop or residual is there: z; mean and variance are those of the stored values
+ * gamma, beta      device, in, cols floats      mean_out, rstd_out   device, out, rows floats each (either may be null)
+ * y and z_out must not be the same buffer. */
+int conef_norm_forward(const conef_drop *drop, float eps, int64_t rows, int64_t cols, int dtype, const void *x, int64_t x_pitch,
+                       const void *residual, int64_t residual_pitch, const float *gamma, const float *beta, void *z_out,
+                       int64_t z_pitch, void *y, int64_t y_pitch, float *mean_out, float *rstd_out, void *hip_stream);
+
+/* Its backward pass.  With hat = (z - mean) rstd, a = dy gamma and means over a row:
+ *   dz = rstd (a - mean(a) - hat mean(a hat)) + dz_in       dx = s keep(dz), from dz before it is rounded
+ *   dgamma = sum over rows of dy hat                         dbeta = sum over rows of dy
+ * z, mean, rstd    what the forward pass was taken of (z_out, or x) and left
+ * dz_in            device, in, may be null: a gradient that reaches z past the norm (the residual stream's)
+ * dz               device, out: the gradient of the residual, and of x if there is no dropout
+ * dx               device, out, only with a dropout: the gradient of x.  Must not be dz.
+ * dgamma, dbeta    device, out, cols floats each.  Any of the four outputs may be null, not all of them.
+ * workspace        device, conef_norm_workspace() bytes, 16-byte aligned; may be null if dgamma and dbeta are */
+int conef_norm_workspace(int64_t rows, int64_t cols, size_t *bytes);
+int conef_norm_backward(const conef_drop *drop, int64_t rows, int64_t cols, int dtype, const void *dy, int64_t dy_pitch,
+                        const void *z, int64_t z_pitch, const float *gamma, const float *mean, const float *rstd,
+                        const void *dz_in, int64_t dz_in_pitch, void *dz, int64_t dz_pitch, void *dx, int64_t dx_pitch,
+                        float *dgamma, float *dbeta, void *workspace, void *hip_stream);
+
+/* Microscaled 4-bit floating point: 32 consecutive elements of a row share a scale 2^(b - 127), b a byte (255: all of them are
+ * NaN); an element is a sign bit over three bits for 0, 0.5, 1, 1.5, 2, 3, 4, 6.  With e = floor(log2) of a block's largest
+ * magnitude:
+ *   CONEF_MX_NEAREST      b = e - 2 + 127, to nearest, ties to the even code; what is above 6 steps becomes 6
+ *   CONEF_MX_STOCHASTIC   b one higher where the largest is above 6 2^(e - 2), so that nothing is cut off; with f the distance
+ *                         from the lower neighbour over that between the neighbours, up iff floor(65536 f) + draw >= 65536
+ * (b is at least 0.)  A block with an infinity or a NaN gets b = 255 and codes 0.
+ * A packed operand holds rows in 64s and columns in 128s, the rest filled with zeros; with P = ceil(cols / 128), element (i, j) is in
+ *   code byte   ((i / 16) P + j / 128) 1024 + (j / 32 % 4) 256 + (i % 16) 16 + (j % 32) / 2, the low four bits for even j
+ *   scale byte  ((i / 64) P + j / 128)  256 + (j / 32 % 4)  64 + (i % 16) 4 + (i % 64) / 16
+ * conef_mx_sizes       bytes of the two buffers (either pointer may be null), 16-byte aligned; 0 <= rows, cols here and below, and
+ *                      also cols ceil(rows / 8) < 2^32
+ * conef_mx_quantise    x by rows into codes / scales, and by columns (the rows of x's transpose) into codes_t / scales_t, sized for
+ *                      cols x rows; either pair may be null.  seed, site and step matter to stochastic rounding only.
+ * conef_mx_dequantise  the values of a packed operand, exactly */
+enum { CONEF_MX_NEAREST = 0, CONEF_MX_STOCHASTIC = 1 };
+int conef_mx_sizes(int64_t rows, int64_t cols, size_t *code_bytes, size_t *scale_bytes);
+int conef_mx_quantise(const void *x, int64_t x_pitch, int64_t rows, int64_t cols, int dtype, int rounding, uint64_t seed,
+                      uint32_t site, uint64_t step, uint8_t *codes, uint8_t *scales, uint8_t *codes_t, uint8_t *scales_t,
+                      void *hip_stream);
+int conef_mx_dequantise(const uint8_t *codes, const uint8_t *scales, int64_t rows, int64_t cols, void *out, int64_t out_pitch,
+                        int dtype, void *hip_stream);
+
+/* C <- alpha A B^T + beta C for packed A (m x k) and B (n x k), summed in fp32; C is m x n of dtype.  beta = 0: C is not
+ * read.  A linear layer's output is x by rows with its weight by rows, its input's gradient the output's gradient by rows with the
+ * weight by columns, and its weight's gradient the output's gradient and x by columns: with alpha the step size and C at
+ * grad_off of the flat gradient buffer, that is what conef_step takes.
+ *   workspace   device, conef_mx_product_workspace() bytes (may be 0), 256-byte aligned */
+int conef_mx_product_workspace(int64_t m, int64_t n, int64_t k, size_t *bytes);
+int conef_mx_product(const uint8_t *a_codes, const uint8_t *a_scales, const uint8_t *b_codes, const uint8_t *b_scales, int64_t m,
+                     int64_t n, int64_t k, float alpha, float beta, void *c, int64_t c_pitch, int dtype, void *workspace,
+                     void *hip_stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -28,11 +28,19 @@ EXPORTS = ["conef_init", "conef_sizes", "conef_offsets", "conef_step", "conef_st
            "conef_i2_configure", "conef_i2_sizes", "conef_i2_offsets", "conef_i2_start", "conef_i2_rb_step", "conef_i2_rk_step",
            "conef_rk_configure", "conef_rk_configure_uniform", "conef_rk_sizes", "conef_rk_offsets", "conef_rk_index", "conef_rk_step", "conef_cs_rk_step",
            "conef_cs_init", "conef_csc_init", "conef_cs_sizes", "conef_cs_offsets", "conef_cs_hash", "conef_cs_step",
-           "conef_cs_step_p", "conef_cs_step_q", "conef_cs_step_err", "conef_cs_decode_error"]
+           "conef_cs_step_p", "conef_cs_step_q", "conef_cs_step_err", "conef_cs_decode_error",
+           "conef_dropout_forward", "conef_dropout_backward", "conef_norm_forward", "conef_norm_workspace", "conef_norm_backward",
+           "conef_mx_sizes", "conef_mx_quantise", "conef_mx_dequantise", "conef_mx_product_workspace", "conef_mx_product"]
+MX_NEAREST, MX_STOCHASTIC = 0, 1
 
 
 class conef_mat(ctypes.Structure):
     _fields_ = [("rows", ctypes.c_int64), ("cols", ctypes.c_int64)]
+
+
+class conef_drop(ctypes.Structure):
+    """A dropout: p, and site, seed and step that key its draws."""
+    _fields_ = [("p", ctypes.c_float), ("site", ctypes.c_uint32), ("seed", ctypes.c_uint64), ("step", ctypes.c_uint64)]
 
 
 _lib = None
@@ -109,6 +117,17 @@ def lib() -> ctypes.CDLL:
     L.conef_cs_step_q.argtypes = [vp, vp, vp, vp, vp, vp, vp]
     L.conef_cs_step_err.argtypes = [vp, vp, vp, vp, vp, vp, vp]
     L.conef_cs_decode_error.argtypes = [vp, vp, vp, vp]
+    i64, f32, drop = ctypes.c_int64, ctypes.c_float, ctypes.POINTER(conef_drop)
+    L.conef_dropout_forward.argtypes = [drop, i64, i64, i32, vp, i64, vp, i64, vp, i64, vp]
+    L.conef_dropout_backward.argtypes = [drop, i64, i64, i32, vp, i64, vp, i64, vp]
+    L.conef_norm_forward.argtypes = [drop, f32, i64, i64, i32, vp, i64, vp, i64, vp, vp, vp, i64, vp, i64, vp, vp, vp]
+    L.conef_norm_workspace.argtypes = [i64, i64, szp]
+    L.conef_norm_backward.argtypes = [drop, i64, i64, i32, vp, i64, vp, i64, vp, vp, vp, vp, i64, vp, i64, vp, i64, vp, vp, vp, vp]
+    L.conef_mx_sizes.argtypes = [i64, i64, szp, szp]
+    L.conef_mx_quantise.argtypes = [vp, i64, i64, i64, i32, i32, u64, ctypes.c_uint32, u64, vp, vp, vp, vp, vp]
+    L.conef_mx_dequantise.argtypes = [vp, vp, i64, i64, vp, i64, i32, vp]
+    L.conef_mx_product_workspace.argtypes = [i64, i64, i64, szp]
+    L.conef_mx_product.argtypes = [vp, vp, vp, vp, i64, i64, i64, f32, f32, vp, i64, i32, vp, vp]
     L.conef_destroy.argtypes = [vp]
     L.conef_destroy.restype = None
     L.conef_strerror.argtypes = [i32]
@@ -459,6 +478,129 @@ def conef_cs_step_err(ctx, grads, table, P_hat, Q_new, workspace, stream=0):
 
 def conef_cs_decode_error(ctx, table, e_out, stream=0):
     _check(lib().conef_cs_decode_error(ctx, _ptr(table), _ptr(e_out), stream), "conef_cs_decode_error")
+
+
+# a worker's own step: dropout, layer norm, microscaled 4-bit floating point.  Matrices are torch tensors of two dimensions
+# (rows may be strided); their shape, type and pitch go with their address.
+def _matrix(t, shape=None, dtype=None) -> Tuple[int, int, int, int, int]:
+    """(address, pitch, rows, cols, type) of a two-dimensional tensor whose rows are contiguous; of None: all 0."""
+    import torch
+
+    if t is None:
+        return 0, 0, 0, 0, 0
+    kind = {torch.float32: F32, torch.bfloat16: BF16}.get(t.dtype, -1)
+    if t.dim() != 2 or kind < 0 or (t.shape[1] > 1 and t.stride(1) != 1):
+        raise ConefError(EINVAL, f"a matrix of fp32 or bf16 with contiguous rows is wanted, not {tuple(t.shape)} {t.dtype} {t.stride()}")
+    rows, cols = t.shape
+    if (shape is not None and (rows, cols) != shape) or (dtype is not None and kind != dtype):
+        raise ConefError(EINVAL, f"a matrix of {shape} and type {dtype} is wanted, not {(rows, cols)} of type {kind}")
+    return t.data_ptr(), t.stride(0) if rows > 1 else max(cols, 1), rows, cols, kind
+
+
+def _vector(t, n: int) -> int:
+    """Address of n contiguous floats; 0 for None."""
+    if t is None:
+        return 0
+    if t.dim() != 1 or t.shape[0] != n or str(t.dtype) != "torch.float32" or (n > 1 and t.stride(0) != 1):
+        raise ConefError(EINVAL, f"{n} contiguous floats are wanted, not {tuple(t.shape)} {t.dtype}")
+    return t.data_ptr()
+
+
+def _room(t, bytes_: int) -> int:
+    """Address of a buffer of at least `bytes_` bytes; 0 for None."""
+    if t is None:
+        return 0
+    if not t.is_contiguous() or t.numel() * t.element_size() < bytes_:
+        raise ConefError(EINVAL, f"a contiguous buffer of {bytes_} bytes is wanted, not {t.numel() * t.element_size()}")
+    return t.data_ptr()
+
+
+def _packed(pair, rows: int, cols: int) -> Tuple[int, int]:
+    """Addresses of the codes and scales of a packed rows x cols operand; 0 for None."""
+    if pair is None:
+        return 0, 0
+    s = conef_mx_sizes(rows, cols)
+    return _room(pair[0], s["code_bytes"]), _room(pair[1], s["scale_bytes"])
+
+
+def conef_dropout_forward(drop, x, residual, y, stream=0):
+    px, ix, rows, cols, kind = _matrix(x)
+    pr, ir = _matrix(residual, (rows, cols), kind)[:2]
+    py, iy = _matrix(y, (rows, cols), kind)[:2]
+    _check(lib().conef_dropout_forward(drop, rows, cols, kind, px, ix, pr, ir, py, iy, stream), "conef_dropout_forward")
+
+
+def conef_dropout_backward(drop, dy, dx, stream=0):
+    py, iy, rows, cols, kind = _matrix(dy)
+    px, ix = _matrix(dx, (rows, cols), kind)[:2]
+    _check(lib().conef_dropout_backward(drop, rows, cols, kind, py, iy, px, ix, stream), "conef_dropout_backward")
+
+
+def conef_norm_forward(drop, eps: float, x, residual, gamma, beta, z_out, y, mean_out, rstd_out, stream=0):
+    px, ix, rows, cols, kind = _matrix(x)
+    pr, ir = _matrix(residual, (rows, cols), kind)[:2]
+    pz, iz = _matrix(z_out, (rows, cols), kind)[:2]
+    py, iy = _matrix(y, (rows, cols), kind)[:2]
+    _check(lib().conef_norm_forward(drop, eps, rows, cols, kind, px, ix, pr, ir, _vector(gamma, cols), _vector(beta, cols), pz, iz, py,
+                                    iy, _vector(mean_out, rows), _vector(rstd_out, rows), stream), "conef_norm_forward")
+
+
+def conef_norm_workspace(rows: int, cols: int) -> int:
+    v = ctypes.c_size_t()
+    _check(lib().conef_norm_workspace(rows, cols, ctypes.byref(v)), "conef_norm_workspace")
+    return int(v.value)
+
+
+def conef_norm_backward(drop, dy, z, gamma, mean, rstd, dz_in, dz, dx, dgamma, dbeta, workspace, stream=0):
+    py, iy, rows, cols, kind = _matrix(dy)
+    pz, iz = _matrix(z, (rows, cols), kind)[:2]
+    pi, ii = _matrix(dz_in, (rows, cols), kind)[:2]
+    po, io = _matrix(dz, (rows, cols), kind)[:2]
+    px, ix = _matrix(dx, (rows, cols), kind)[:2]
+    ws = _room(workspace, conef_norm_workspace(rows, cols))
+    _check(lib().conef_norm_backward(drop, rows, cols, kind, py, iy, pz, iz, _vector(gamma, cols), _vector(mean, rows),
+                                     _vector(rstd, rows), pi, ii, po, io, px, ix, _vector(dgamma, cols), _vector(dbeta, cols), ws,
+                                     stream), "conef_norm_backward")
+
+
+def conef_mx_sizes(rows: int, cols: int) -> dict:
+    v = [ctypes.c_size_t() for _ in range(2)]
+    _check(lib().conef_mx_sizes(rows, cols, *[ctypes.byref(x) for x in v]), "conef_mx_sizes")
+    return {"code_bytes": int(v[0].value), "scale_bytes": int(v[1].value)}
+
+
+def mx_alloc(rows: int, cols: int, device="cuda:0"):
+    """(codes, scales): zeroed buffers of a packed rows x cols operand, as the conef_mx_* calls take it."""
+    import torch
+
+    s = conef_mx_sizes(rows, cols)
+    return tuple(torch.zeros(s[k], dtype=torch.uint8, device=device) for k in ("code_bytes", "scale_bytes"))
+
+
+def conef_mx_quantise(x, rounding: int, seed: int, site: int, step: int, packed, packed_t, stream=0):
+    """packed: (codes, scales) of x by rows, packed_t: of its transpose by rows; either may be None."""
+    px, ix, rows, cols, kind = _matrix(x)
+    _check(lib().conef_mx_quantise(px, ix, rows, cols, kind, rounding, seed, site, step, *_packed(packed, rows, cols),
+                                   *_packed(packed_t, cols, rows), stream), "conef_mx_quantise")
+
+
+def conef_mx_dequantise(packed, out, stream=0):
+    po, io, rows, cols, kind = _matrix(out)
+    _check(lib().conef_mx_dequantise(*_packed(packed, rows, cols), rows, cols, po, io, kind, stream), "conef_mx_dequantise")
+
+
+def conef_mx_product_workspace(m: int, n: int, k: int) -> int:
+    v = ctypes.c_size_t()
+    _check(lib().conef_mx_product_workspace(m, n, k, ctypes.byref(v)), "conef_mx_product_workspace")
+    return int(v.value)
+
+
+def conef_mx_product(a, b, k: int, alpha: float, beta: float, c, workspace, stream=0):
+    """c [m, n] <- alpha A B^T + beta c of the packed operands a (m x k) and b (n x k)."""
+    pc, ic, m, n, kind = _matrix(c)
+    ws = _room(workspace, conef_mx_product_workspace(m, n, k))
+    _check(lib().conef_mx_product(*_packed(a, m, k), *_packed(b, n, k), m, n, k, alpha, beta, pc, ic, kind, ws, stream),
+           "conef_mx_product")
 
 
 def conef_set_timing(ctx, on: bool):

@@ -1,0 +1,464 @@
+// Dropout whose mask is drawn again where it is needed, and layer norm's forward and backward pass with that dropout and the
+// residual in front of it.
+//
+// z = residual + keep(x) / (share kept), y = (z - mean) rstd gamma + beta; the statistics of a row are those of z as it is
+// stored, so that the backward pass, which reads the stored z, differentiates what was computed.
+// With a = dy gamma and hat = (z - mean) rstd:
+//   dz = rstd (a - mean(a) - hat mean(a hat)) + dz_in,   dx = keep(dz) / (share kept),
+//   dgamma = sum over rows of dy hat,   dbeta = sum over rows of dy.
+// All sums are fp32 in a fixed order (no atomics), those over rows fp64 at the last level; a row's variance is that of the values less
+// their mean, in a second sweep over registers.
+#include <algorithm>
+#include <type_traits>
+
+#include "layers_device.h"
+
+namespace conef {
+
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kMostCols = 16384;        // the widest row that a workgroup holds in registers, eight octets a lane
+constexpr int kPartials = 512;          // workgroups of the backward pass, each with its sums for dgamma and dbeta
+
+// ---------------------------------------------------------------- dropout
+template <bool BF16>
+__global__ __launch_bounds__(kThreads) void k_dropout(DropoutArgs a, uint32_t octets, uint32_t per_row)
+{
+    const uint32_t o = blockIdx.x * kThreads + threadIdx.x;
+    if (o >= octets) return;
+    const uint32_t row = o / per_row;
+    const int col = (int)(o - row * per_row) * 8, left = a.cols - col;
+    float v[8];
+    load_octet<BF16>(a.x.data, row * a.x.pitch + col, left, v);
+    drop_octet(a.d, o, v);
+    if (a.residual.data) {
+        float r[8];
+        load_octet<BF16>(a.residual.data, row * a.residual.pitch + col, left, r);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = r[i] + v[i];
+    }
+    store_octet<BF16>(a.y.data, row * a.y.pitch + col, left, v);
+}
+
+// ---------------------------------------------------------------- layer norm
+// Sums of N values over the G lanes that share a row, in every one of them.  G = 256: `red` holds 2 x 4 x N floats, used in
+// turn by consecutive calls (`turn`), so one barrier a call is enough.
+template <int G, int N>
+__device__ __forceinline__ void group_sum(float v[N], float *red, int &turn)
+{
+#pragma unroll
+    for (int i = 0; i < N; ++i) v[i] = lanes_sum(v[i]);
+    if constexpr (G == kThreads) {
+        float *slot = red + turn * 4 * N;
+        turn ^= 1;
+        if ((threadIdx.x & 63) == 0)
+#pragma unroll
+            for (int i = 0; i < N; ++i) slot[(threadIdx.x >> 6) * N + i] = v[i];
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < N; ++i) v[i] = (slot[i] + slot[N + i]) + (slot[2 * N + i] + slot[3 * N + i]);
+    }
+}
+
+// G lanes hold a row, V octets each: octet v of lane t starts at column 8 (t + G v).
+template <bool BF16, int G, int V, bool FUSED>
+__global__ __launch_bounds__(kThreads) void k_norm_forward(NormArgs a)
+{
+    __shared__ float red[8];
+    int turn = 0;
+    const int t = threadIdx.x % G;
+    const float inv = 1.0f / (float)a.cols;
+    const uint32_t per_row = (uint32_t)(a.cols + 7) >> 3;
+    float gamma[V][8], beta[V][8];
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+        const int col = 8 * (t + G * v);
+        load_octet<false>(a.gamma, col, a.cols - col, gamma[v]);
+        load_octet<false>(a.beta, col, a.cols - col, beta[v]);
+    }
+    for (int64_t row = (int64_t)blockIdx.x * (kThreads / G) + threadIdx.x / G; row < a.rows; row += (int64_t)gridDim.x * (kThreads / G)) {
+        float z[V][8];
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            const int col = 8 * (t + G * v);
+            load_octet<BF16>(a.x.data, row * a.x.pitch + col, a.cols - col, z[v]);
+        }
+        if constexpr (FUSED) {
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+                const int col = 8 * (t + G * v);
+                if (a.drop) drop_octet(a.d, (uint32_t)row * per_row + (uint32_t)(t + G * v), z[v]);
+                if (a.residual.data) {
+                    float r[8];
+                    load_octet<BF16>(a.residual.data, row * a.residual.pitch + col, a.cols - col, r);
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) z[v][i] = r[i] + z[v][i];
+                }
+                store_octet<BF16>(a.z.data, row * a.z.pitch + col, a.cols - col, z[v]);
+            }
+        }
+        float sum[1] = {0.0f};
+#pragma unroll
+        for (int v = 0; v < V; ++v)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) sum[0] += z[v][i];
+        group_sum<G, 1>(sum, red, turn);
+        const float mean = sum[0] * inv;
+        sum[0] = 0.0f;
+#pragma unroll
+        for (int v = 0; v < V; ++v)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const float c = 8 * (t + G * v) + i < a.cols ? z[v][i] - mean : 0.0f;
+                sum[0] = __builtin_fmaf(c, c, sum[0]);
+            }
+        group_sum<G, 1>(sum, red, turn);
+        const float rstd = 1.0f / sqrtf(sum[0] * inv + a.eps);
+        if (t == 0) {
+            if (a.mean_out) a.mean_out[row] = mean;
+            if (a.rstd_out) a.rstd_out[row] = rstd;
+        }
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            const int col = 8 * (t + G * v);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) z[v][i] = __builtin_fmaf((z[v][i] - mean) * rstd, gamma[v][i], beta[v][i]);
+            store_octet<BF16>(a.y.data, row * a.y.pitch + col, a.cols - col, z[v]);
+        }
+    }
+}
+
+// A row of any length, in three sweeps over it by a workgroup.
+template <bool BF16, bool FUSED>
+__global__ __launch_bounds__(kThreads) void k_norm_forward_long(NormArgs a)
+{
+    __shared__ float red[8];
+    int turn = 0;
+    const float inv = 1.0f / (float)a.cols;
+    const uint32_t per_row = (uint32_t)(a.cols + 7) >> 3;
+    for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
+        const void *src = FUSED ? a.z.data : a.x.data;
+        const int64_t at = row * (FUSED ? a.z.pitch : a.x.pitch);
+        float sum[1] = {0.0f};
+        for (int64_t col = 8 * threadIdx.x; col < a.cols; col += 8 * kThreads) {
+            const int left = (int)(a.cols - col < 8 ? a.cols - col : 8);
+            float z[8];
+            load_octet<BF16>(a.x.data, row * a.x.pitch + col, left, z);
+            if constexpr (FUSED) {
+                if (a.drop) drop_octet(a.d, (uint32_t)row * per_row + (uint32_t)(col >> 3), z);
+                if (a.residual.data) {
+                    float r[8];
+                    load_octet<BF16>(a.residual.data, row * a.residual.pitch + col, left, r);
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) z[i] = r[i] + z[i];
+                }
+                store_octet<BF16>(a.z.data, at + col, left, z);
+            }
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                if (i < left) sum[0] += z[i];
+        }
+        group_sum<kThreads, 1>(sum, red, turn);
+        const float mean = sum[0] * inv;
+        sum[0] = 0.0f;
+        for (int64_t col = 8 * threadIdx.x; col < a.cols; col += 8 * kThreads) {
+            const int left = (int)(a.cols - col < 8 ? a.cols - col : 8);
+            float z[8];
+            load_octet<BF16>(src, at + col, left, z);
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                if (i < left) sum[0] = __builtin_fmaf(z[i] - mean, z[i] - mean, sum[0]);
+        }
+        group_sum<kThreads, 1>(sum, red, turn);
+        const float rstd = 1.0f / sqrtf(sum[0] * inv + a.eps);
+        if (threadIdx.x == 0) {
+            if (a.mean_out) a.mean_out[row] = mean;
+            if (a.rstd_out) a.rstd_out[row] = rstd;
+        }
+        for (int64_t col = 8 * threadIdx.x; col < a.cols; col += 8 * kThreads) {
+            const int left = (int)(a.cols - col < 8 ? a.cols - col : 8);
+            float z[8], gamma[8], beta[8];
+            load_octet<BF16>(src, at + col, left, z);
+            load_octet<false>(a.gamma, col, left, gamma);
+            load_octet<false>(a.beta, col, left, beta);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) z[i] = __builtin_fmaf((z[i] - mean) * rstd, gamma[i], beta[i]);
+            store_octet<BF16>(a.y.data, row * a.y.pitch + col, left, z);
+        }
+    }
+}
+
+// hat and a = dy gamma of an octet
+__device__ __forceinline__ void hat_and_a(const float z[8], const float dy[8], const float gamma[8], float mean, float rstd,
+                                          float hat[8], float a[8])
+{
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        hat[i] = (z[i] - mean) * rstd;
+        a[i] = dy[i] * gamma[i];
+    }
+}
+
+// Adds dz_in, writes dz and, from the unrounded values, dx.
+template <bool BF16>
+__device__ __forceinline__ void finish_dz(const NormArgs &a, int64_t row, int64_t col, int left, uint32_t octet, float v[8])
+{
+    if (a.dz_in.data) {
+        float r[8];
+        load_octet<BF16>(a.dz_in.data, row * a.dz_in.pitch + col, left, r);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] += r[i];
+    }
+    if (a.dx.data) {
+        float x[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[i] = v[i];
+        if (a.drop) drop_octet(a.d, octet, x);
+        store_octet<BF16>(a.dx.data, row * a.dx.pitch + col, left, x);
+    }
+    if (a.dz.data) store_octet<BF16>(a.dz.data, row * a.dz.pitch + col, left, v);
+}
+
+// Each workgroup takes every gridDim-th row (or 256 / G of them) and keeps its share of dgamma and dbeta in registers, since a lane
+// sees the same columns in every row; k_norm_columns adds the shares.
+template <bool BF16, int G, int V>
+__global__ __launch_bounds__(kThreads) void k_norm_backward(NormArgs a)
+{
+    constexpr int kRows = kThreads / G;
+    __shared__ float red[16];
+    __shared__ float share[G == kThreads ? 1 : 2 * 8 * G * V];
+    int turn = 0;
+    const int t = threadIdx.x % G;
+    const float inv = 1.0f / (float)a.cols;
+    const uint32_t per_row = (uint32_t)(a.cols + 7) >> 3;
+    float gamma[V][8], dgamma[V][8] = {}, dbeta[V][8] = {};
+#pragma unroll
+    for (int v = 0; v < V; ++v) load_octet<false>(a.gamma, 8 * (t + G * v), a.cols - 8 * (t + G * v), gamma[v]);
+    for (int64_t row = (int64_t)blockIdx.x * kRows + threadIdx.x / G; row < a.rows; row += (int64_t)gridDim.x * kRows) {
+        float z[V][8], dy[V][8];
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            const int col = 8 * (t + G * v);
+            load_octet<BF16>(a.z_in.data, row * a.z_in.pitch + col, a.cols - col, z[v]);
+            load_octet<BF16>(a.dy.data, row * a.dy.pitch + col, a.cols - col, dy[v]);
+        }
+        const float mean = a.mean[row], rstd = a.rstd[row];
+        float sums[2] = {0.0f, 0.0f};
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            float hat[8], w[8];
+            hat_and_a(z[v], dy[v], gamma[v], mean, rstd, hat, w);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                // (columns beyond the row's end have dy = gamma = 0)
+                sums[0] += w[i];
+                sums[1] = __builtin_fmaf(w[i], hat[i], sums[1]);
+                dgamma[v][i] = __builtin_fmaf(dy[v][i], hat[i], dgamma[v][i]);
+                dbeta[v][i] += dy[v][i];
+            }
+        }
+        group_sum<G, 2>(sums, red, turn);
+        const float m0 = sums[0] * inv, m1 = sums[1] * inv;
+        if (a.dz.data || a.dx.data) {
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+                const int col = 8 * (t + G * v);
+                float hat[8], w[8];
+                hat_and_a(z[v], dy[v], gamma[v], mean, rstd, hat, w);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) w[i] = rstd * ((w[i] - m0) - hat[i] * m1);
+                finish_dz<BF16>(a, row, col, a.cols - col, (uint32_t)row * per_row + (uint32_t)(t + G * v), w);
+            }
+        }
+    }
+    if (!a.partials) return;
+    float *out = a.partials + (int64_t)blockIdx.x * 2 * a.cols;
+    if constexpr (G == kThreads) {
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            const int col = 8 * (t + G * v);
+            store_octet<false>(out, col, a.cols - col, dgamma[v]);
+            store_octet<false>(out + a.cols, col, a.cols - col, dbeta[v]);
+        }
+    } else {
+        // the workgroup's groups one after the other, then columns of the sum by all threads
+        for (int g = 0; g < kRows; ++g) {
+            if ((int)threadIdx.x / G == g)
+#pragma unroll
+                for (int v = 0; v < V; ++v)
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        float *p = share + 8 * (t + G * v) + i, *q = p + 8 * G * V;
+                        *p = g ? *p + dgamma[v][i] : dgamma[v][i];
+                        *q = g ? *q + dbeta[v][i] : dbeta[v][i];
+                    }
+            __syncthreads();
+        }
+        for (int c = threadIdx.x; c < a.cols; c += kThreads) {
+            out[c] = share[c];
+            out[a.cols + c] = share[8 * G * V + c];
+        }
+    }
+}
+
+// Rows of any length: two sweeps by a workgroup; the sums over rows are k_norm_column_parts's.
+template <bool BF16>
+__global__ __launch_bounds__(kThreads) void k_norm_backward_long(NormArgs a)
+{
+    __shared__ float red[16];
+    int turn = 0;
+    const float inv = 1.0f / (float)a.cols;
+    const uint32_t per_row = (uint32_t)(a.cols + 7) >> 3;
+    for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
+        const float mean = a.mean[row], rstd = a.rstd[row];
+        float sums[2] = {0.0f, 0.0f}, z[8], dy[8], gamma[8], hat[8], w[8];
+        for (int64_t col = 8 * threadIdx.x; col < a.cols; col += 8 * kThreads) {
+            const int left = (int)(a.cols - col < 8 ? a.cols - col : 8);
+            load_octet<BF16>(a.z_in.data, row * a.z_in.pitch + col, left, z);
+            load_octet<BF16>(a.dy.data, row * a.dy.pitch + col, left, dy);
+            load_octet<false>(a.gamma, col, left, gamma);
+            hat_and_a(z, dy, gamma, mean, rstd, hat, w);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                sums[0] += w[i];
+                sums[1] = __builtin_fmaf(w[i], hat[i], sums[1]);
+            }
+        }
+        group_sum<kThreads, 2>(sums, red, turn);
+        const float m0 = sums[0] * inv, m1 = sums[1] * inv;
+        for (int64_t col = 8 * threadIdx.x; col < a.cols; col += 8 * kThreads) {
+            const int left = (int)(a.cols - col < 8 ? a.cols - col : 8);
+            load_octet<BF16>(a.z_in.data, row * a.z_in.pitch + col, left, z);
+            load_octet<BF16>(a.dy.data, row * a.dy.pitch + col, left, dy);
+            load_octet<false>(a.gamma, col, left, gamma);
+            hat_and_a(z, dy, gamma, mean, rstd, hat, w);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) w[i] = rstd * ((w[i] - m0) - hat[i] * m1);
+            finish_dz<BF16>(a, row, col, left, (uint32_t)row * per_row + (uint32_t)(col >> 3), w);
+        }
+    }
+}
+
+// Shares of dgamma and dbeta for rows too long for registers: workgroup (x, y) takes 2048 columns of every gridDim.y-th row.
+template <bool BF16>
+__global__ __launch_bounds__(kThreads) void k_norm_column_parts(NormArgs a)
+{
+    const int64_t col = 8 * ((int64_t)blockIdx.x * kThreads + threadIdx.x);
+    if (col >= a.cols) return;
+    const int left = (int)(a.cols - col < 8 ? a.cols - col : 8);
+    float dgamma[8] = {}, dbeta[8] = {};
+    for (int64_t row = blockIdx.y; row < a.rows; row += gridDim.y) {
+        const float mean = a.mean[row], rstd = a.rstd[row];
+        float z[8], dy[8];
+        load_octet<BF16>(a.z_in.data, row * a.z_in.pitch + col, left, z);
+        load_octet<BF16>(a.dy.data, row * a.dy.pitch + col, left, dy);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            dgamma[i] = __builtin_fmaf(dy[i], (z[i] - mean) * rstd, dgamma[i]);
+            dbeta[i] += dy[i];
+        }
+    }
+    float *out = a.partials + (int64_t)blockIdx.y * 2 * a.cols;
+    store_octet<false>(out, col, left, dgamma);
+    store_octet<false>(out + a.cols, col, left, dbeta);
+}
+
+// Adds the shares: 64 of the 2 cols sums a workgroup, sixteen threads to a sum.
+__global__ __launch_bounds__(1024) void k_norm_columns(const float *partials, int parts, int cols, float *dgamma, float *dbeta)
+{
+    __shared__ double red[16][64];
+    const int lane = threadIdx.x & 63, part = threadIdx.x >> 6;
+    const int64_t c = (int64_t)blockIdx.x * 64 + lane, n = 2 * (int64_t)cols;
+    double s = 0.0;
+    if (c < n)
+        for (int p = part; p < parts; p += 16) s += (double)partials[p * n + c];
+    red[part][lane] = s;
+    __syncthreads();
+    if (part || c >= n) return;
+#pragma unroll
+    for (int p = 1; p < 16; ++p) s += red[p][lane];
+    float *out = c < cols ? dgamma : dbeta;
+    if (out) out[c < cols ? c : c - cols] = (float)s;
+}
+
+template <typename F>
+void by_width(int cols, F &&go)
+{
+    using std::integral_constant;
+    if (cols <= 512) go(integral_constant<int, 64>{}, integral_constant<int, 1>{});
+    else if (cols <= 1024) go(integral_constant<int, 64>{}, integral_constant<int, 2>{});
+    else if (cols <= 2048) go(integral_constant<int, 256>{}, integral_constant<int, 1>{});
+    else if (cols <= 4096) go(integral_constant<int, 256>{}, integral_constant<int, 2>{});
+    else if (cols <= 8192) go(integral_constant<int, 256>{}, integral_constant<int, 4>{});
+    else go(integral_constant<int, 256>{}, integral_constant<int, 8>{});
+}
+
+template <typename F>
+void by_bool(bool v, F &&go)
+{
+    if (v) go(std::true_type{});
+    else go(std::false_type{});
+}
+
+}  // namespace
+
+void launch_dropout(const DropoutArgs &a, bool bf16, hipStream_t st)
+{
+    const uint32_t per_row = (uint32_t)(a.cols + 7) / 8, octets = (uint32_t)a.rows * per_row;
+    const dim3 grid((unsigned)(((uint64_t)octets + kThreads - 1) / kThreads));
+    by_bool(bf16, [&](auto b) { hipLaunchKernelGGL((k_dropout<decltype(b)::value>), grid, dim3(kThreads), 0, st, a, octets, per_row); });
+}
+
+void launch_norm_forward(const NormArgs &a, bool bf16, hipStream_t st)
+{
+    by_bool(bf16, [&](auto b) {
+        by_bool(a.z.data != nullptr, [&](auto fused) {
+            if (a.cols > kMostCols) {
+                const dim3 grid((unsigned)std::min<int64_t>(a.rows, 1 << 20));
+                hipLaunchKernelGGL((k_norm_forward_long<decltype(b)::value, decltype(fused)::value>), grid, dim3(kThreads), 0, st, a);
+                return;
+            }
+            by_width(a.cols, [&](auto g, auto v) {
+                const int64_t per = kThreads / decltype(g)::value, groups = (a.rows + per - 1) / per;
+                hipLaunchKernelGGL((k_norm_forward<decltype(b)::value, decltype(g)::value, decltype(v)::value, decltype(fused)::value>),
+                                   dim3((unsigned)std::min<int64_t>(groups, 2048)), dim3(kThreads), 0, st, a);
+            });
+        });
+    });
+}
+
+int64_t norm_partials(int64_t rows, int64_t cols)
+{
+    (void)cols;
+    return std::min<int64_t>(rows, kPartials);
+}
+
+void launch_norm_backward(const NormArgs &a, bool bf16, hipStream_t st)
+{
+    const int64_t parts = norm_partials(a.rows, a.cols);
+    int used = (int)parts;
+    if (parts > 0) by_bool(bf16, [&](auto b) {
+        if (a.cols > kMostCols) {
+            // (first: dz may take the place of dy or z)
+            if (a.partials)
+                hipLaunchKernelGGL((k_norm_column_parts<decltype(b)::value>), dim3((unsigned)((a.cols + 2047) / 2048), (unsigned)parts),
+                                   dim3(kThreads), 0, st, a);
+            if (a.dz.data || a.dx.data)
+                hipLaunchKernelGGL((k_norm_backward_long<decltype(b)::value>), dim3((unsigned)std::min<int64_t>(a.rows, 1 << 20)),
+                                   dim3(kThreads), 0, st, a);
+            return;
+        }
+        by_width(a.cols, [&](auto g, auto v) {
+            const int64_t per = kThreads / decltype(g)::value;
+            used = (int)std::min<int64_t>((a.rows + per - 1) / per, parts);
+            hipLaunchKernelGGL((k_norm_backward<decltype(b)::value, decltype(g)::value, decltype(v)::value>), dim3((unsigned)used),
+                               dim3(kThreads), 0, st, a);
+        });
+    });
+    if (a.dgamma || a.dbeta)
+        hipLaunchKernelGGL(k_norm_columns, dim3((unsigned)((2 * (int64_t)a.cols + 63) / 64)), dim3(1024), 0, st, a.partials, used, a.cols,
+                           a.dgamma, a.dbeta);
+}
+
+}  // namespace conef

@@ -1,0 +1,131 @@
+// Device helpers of the operators of a training step: octets of rows of any alignment, draws of an octet, sums over a wave.
+#pragma once
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "device_common.h"
+#include "layers.h"
+
+namespace conef {
+
+// Sixteen bytes at any address that an element may have: the hardware takes them in one access.
+typedef uint32_t u32x4_any __attribute__((ext_vector_type(4), aligned(2)));
+
+__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi)
+{
+    typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+    const bf16x2 v = {(__bf16)lo, (__bf16)hi};          // to nearest even, NaN stays NaN
+    return __builtin_bit_cast(uint32_t, v);
+}
+
+// `left` elements (8 or more: all) of the octet that starts at element `at`; the others are 0
+template <bool BF16>
+__device__ __forceinline__ void load_octet(const void *data, int64_t at, int left, float v[8])
+{
+    if constexpr (BF16) {
+        const uint16_t *p = static_cast<const uint16_t *>(data) + at;
+        if (left >= 8) {
+            const u32x4_any u = *reinterpret_cast<const u32x4_any *>(p);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                v[2 * i] = __uint_as_float(u[i] << 16);
+                v[2 * i + 1] = __uint_as_float(u[i] & 0xFFFF0000u);
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] = i < left ? bf16_bits_to_f32(p[i]) : 0.0f;
+        }
+    } else {
+        const float *p = static_cast<const float *>(data) + at;
+        if (left >= 8) {
+            const u32x4_any a = *reinterpret_cast<const u32x4_any *>(p), b = *reinterpret_cast<const u32x4_any *>(p + 4);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                v[i] = __uint_as_float(a[i]);
+                v[4 + i] = __uint_as_float(b[i]);
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] = i < left ? p[i] : 0.0f;
+        }
+    }
+}
+
+// Writes the octet's first `left` elements; v becomes what has been written (rounded to bf16 where the elements are).
+template <bool BF16>
+__device__ __forceinline__ void store_octet(void *data, int64_t at, int left, float v[8])
+{
+    if constexpr (BF16) {
+        uint16_t *p = static_cast<uint16_t *>(data) + at;
+        u32x4_any u;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            u[i] = pack_bf16(v[2 * i], v[2 * i + 1]);
+            v[2 * i] = __uint_as_float(u[i] << 16);
+            v[2 * i + 1] = __uint_as_float(u[i] & 0xFFFF0000u);
+        }
+        if (left >= 8) {
+            *reinterpret_cast<u32x4_any *>(p) = u;
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                if (i < left) p[i] = (uint16_t)(u[i >> 1] >> (16 * (i & 1)));
+        }
+    } else {
+        float *p = static_cast<float *>(data) + at;
+        if (left >= 8) {
+            u32x4_any a, b;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                a[i] = __float_as_uint(v[i]);
+                b[i] = __float_as_uint(v[4 + i]);
+            }
+            *reinterpret_cast<u32x4_any *>(p) = a;
+            *reinterpret_cast<u32x4_any *>(p + 4) = b;
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                if (i < left) p[i] = v[i];
+        }
+    }
+}
+
+// the four words that hold the eight 16-bit draws of an octet
+__device__ __forceinline__ void octet_draws(const Draws &d, uint32_t octet, uint32_t out[4])
+{
+    philox4x32_10(octet, d.word, d.step_lo, d.step_hi, d.seed_lo, d.seed_hi, out);
+}
+
+// v <- v * scale where it is kept, else 0
+__device__ __forceinline__ void drop_octet(const DropArgs &d, uint32_t octet, float v[8])
+{
+    uint32_t u[4];
+    octet_draws(d.draws, octet, u);
+    const uint32_t high = d.threshold << 16;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        v[2 * i] = (u[i] << 16) >= high ? v[2 * i] * d.scale : 0.0f;
+        v[2 * i + 1] = u[i] >= high ? v[2 * i + 1] * d.scale : 0.0f;
+    }
+}
+
+template <int CTRL>
+__device__ __forceinline__ float dpp(float v)
+{
+    return __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(v), CTRL, 0xF, 0xF, true));
+}
+
+// sum over the 64 lanes of a wave, in every lane: quads, halves and wholes of a row of 16, then across the rows
+__device__ __forceinline__ float lanes_sum(float v)
+{
+    v += dpp<0xB1>(v);          // lane ^ 1
+    v += dpp<0x4E>(v);          // lane ^ 2
+    v += dpp<0x141>(v);         // the other quad of a half row
+    v += dpp<0x140>(v);         // the other half row
+    auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    v = __uint_as_float(r[0]) + __uint_as_float(r[1]);
+    r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+
+}  // namespace conef
