@@ -38,80 +38,288 @@ __device__ __forceinline__ void unroll(F &&f)
     unroll_impl(f, std::make_integer_sequence<int, N>{});
 }
 
-// alpha v (+ beta c), to four neighbours of a row of C
-template <bool BF16>
-__device__ __forceinline__ void store_four(const MxProductArgs &a, int64_t row, int64_t col, f32x4 v)
+// Sixteen bytes (or four) a lane from `src` to LDS, one lane's after the other's: `dst` is the wave's.
+template <int BYTES>
+__device__ __forceinline__ void to_lds(const uint8_t *src, uint8_t *dst)
+{
+    const auto *from = (const __attribute__((address_space(1))) void *)src;
+    auto *to = (__attribute__((address_space(3))) void *)dst;
+    if constexpr (BYTES == 16) __builtin_amdgcn_global_load_lds(from, to, 16, 0, 0);
+    else __builtin_amdgcn_global_load_lds(from, to, 4, 0, 0);
+}
+
+// all but the last N loads of this wave have arrived, and all its reads from LDS
+template <int N>
+__device__ __forceinline__ void wait_loads()
+{
+    // (the builtin, which the compiler counts with: bits 3:0 and 15:14 loads, 6:4 exports, 11:8 LDS)
+    __builtin_amdgcn_s_waitcnt((N & 15) | (N >> 4 << 14) | 7 << 4);
+    asm volatile("" ::: "memory");
+}
+
+// sixteen bytes to any address; PAST: past the caches
+template <bool PAST>
+__device__ __forceinline__ void store_16(void *p, u32x4_any v)
+{
+    if constexpr (PAST) __builtin_nontemporal_store(v, static_cast<u32x4_any *>(p));
+    else *static_cast<u32x4_any *>(p) = v;
+}
+
+// alpha v (+ beta c) to N neighbours of a row of C
+template <bool BF16, bool ADD, bool PAST, int N>
+__device__ __forceinline__ void store_row(const MxProductArgs &a, int64_t row, int64_t col, const float *v)
 {
     const int64_t at = row * a.c.pitch + col;
+    const int left = (int)(a.n - col < N ? a.n - col : N);
+    float x[N];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        if (col + i >= a.n) return;
-        float x = a.alpha * v[i];
-        if constexpr (BF16) {
-            uint16_t *p = static_cast<uint16_t *>(a.c.data) + at + i;
-            if (a.beta != 0.0f) x = __builtin_fmaf(a.beta, bf16_bits_to_f32(*p), x);
-            *p = (uint16_t)pack_bf16(x, x);
-        } else {
-            float *p = static_cast<float *>(a.c.data) + at + i;
-            if (a.beta != 0.0f) x = __builtin_fmaf(a.beta, *p, x);
-            *p = x;
+    for (int i = 0; i < N; ++i) {
+        x[i] = a.alpha * v[i];
+        if (ADD && i < left)
+            x[i] = __builtin_fmaf(a.beta, BF16 ? bf16_bits_to_f32(static_cast<const uint16_t *>(a.c.data)[at + i]) : static_cast<const float *>(a.c.data)[at + i], x[i]);
+    }
+    if constexpr (BF16) {
+        uint16_t *p = static_cast<uint16_t *>(a.c.data) + at;
+        uint32_t u[N / 2];
+#pragma unroll
+        for (int i = 0; i < N / 2; ++i) u[i] = pack_bf16(x[2 * i], x[2 * i + 1]);
+        if (left == N && N == 8) {
+            store_16<PAST>(p, u32x4_any{u[0], u[1], u[2], u[3]});
+            return;
         }
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+            if (i < left) p[i] = (uint16_t)(u[i / 2] >> (16 * (i & 1)));
+    } else {
+        float *p = static_cast<float *>(a.c.data) + at;
+        if (left == N && N == 4) {
+            store_16<PAST>(p, u32x4_any{__float_as_uint(x[0]), __float_as_uint(x[1]), __float_as_uint(x[2]), __float_as_uint(x[3])});
+            return;
+        }
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+            if (i < left) p[i] = x[i];
     }
 }
 
-// WM x WN waves of TM x TN tiles of 16 x 16; 128 elements of the long axis at a time.
-template <bool BF16, int WM, int WN, int TM, int TN>
-__global__ __launch_bounds__(64 * WM * WN) void k_mx_product(MxProductArgs a, int64_t pieces, int64_t a_groups, int64_t b_groups,
-                                                             int64_t tiles_m)
+// The four columns that a lane holds of each of two neighbouring tiles of 16, to C.  bf16: two rows of 16 lanes exchange halves first, so that a
+// lane has eight columns of one of the tiles and writes 16 bytes.
+template <bool BF16, bool ADD, bool PAST>
+__device__ __forceinline__ void store_pair(const MxProductArgs &a, int64_t row, int64_t col, int quad, f32x4 u, f32x4 v)
 {
-    constexpr int kM = WM * TM * 16, kN = WN * TN * 16, kWaves = WM * WN;
-    __shared__ __attribute__((aligned(16))) uint8_t lds[(kM + kN) * 64 + (kM + kN) * 4];
+    if constexpr (BF16) {
+        float x[8];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(u[i]), __float_as_uint(v[i]), false, false);
+            x[i] = __uint_as_float(r[0]);
+            x[4 + i] = __uint_as_float(r[1]);
+        }
+        col += 16 * (quad & 1) + 8 * (quad >> 1);
+        if (row < a.m && col < a.n) store_row<true, ADD, PAST, 8>(a, row, col, x);
+    } else if (row < a.m) {
+        const float x[4] = {u[0], u[1], u[2], u[3]}, y[4] = {v[0], v[1], v[2], v[3]};
+        if (col + 4 * quad < a.n) store_row<false, ADD, PAST, 4>(a, row, col + 4 * quad, x);
+        if (col + 16 + 4 * quad < a.n) store_row<false, ADD, PAST, 4>(a, row, col + 16 + 4 * quad, y);
+    }
+}
+
+// Fragments of one step along the long axis: a wave's TM + TN operands of 16 rows and their scales, four operands to a register.
+template <int TM, int TN>
+struct Step {
+    v4i a[TM], b[TN];
+    int ea[(TM + 3) / 4], eb[(TN + 3) / 4];
+};
+
+// A product's shape in tiles; items are tiles times parts of the long axis (`per_part` pieces, the last may have fewer), parts outermost.
+struct Shape {
+    int pieces, a_groups, b_groups, tiles_m, tiles_n, per_part, items;
+};
+
+// WM x WN waves of TM x TN tiles of 16 x 16; 128 elements of the long axis (one piece) a step, STAGES of them in LDS.  Step s + STAGES is
+// fetched into the place of step s as soon as every wave has that in registers, and the fragments of step s + 1 are read while
+// those of step s are multiplied, so there is one barrier a step and nothing is waited for that was not asked for a step before.
+// WAVES: waves a SIMD, of all the workgroups that a CU is to hold.
+template <bool BF16, bool ADD, bool PAST, int WM, int WN, int TM, int TN, int STAGES, int WAVES>
+__global__ __launch_bounds__(64 * WM * WN, WAVES) void k_mx_product(MxProductArgs a, Shape z)
+{
+    constexpr int kM = WM * TM * 16, kN = WN * TN * 16, kWaves = WM * WN, kStage = (kM + kN) * 68;
+    constexpr int kCodeLoads = (kM + kN) / 16 / kWaves, kScaleLoads = ((kM + kN) / 64 + kWaves - 1) / kWaves;
+    constexpr int kLoads = kCodeLoads + kScaleLoads;
+    static_assert((kM + kN) / 16 % kWaves == 0 && kM % 64 == 0 && kN % 64 == 0 && TM % 2 == 0 && TN % 2 == 0 && STAGES >= 2, "");
+    static_assert((STAGES - 1) * kLoads < 64, "the counter of loads");
+    __shared__ __attribute__((aligned(1024))) uint8_t lds[STAGES * kStage];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int wm = wave % WM, wn = wave / WM;
-    const int64_t m0 = (int64_t)(blockIdx.x % tiles_m) * kM, n0 = (int64_t)(blockIdx.x / tiles_m) * kN;
+    // Workgroups go to the eight dies in turn; each die gets a run of neighbouring items, rows of tiles in eights, so that what its
+    // workgroups read at one time stays in its cache.
+    const int die = blockIdx.x & 7, per_die = z.items >> 3, more = z.items & 7, tiles = z.tiles_m * z.tiles_n;
+    const int item = die * per_die + (die < more ? die : more) + (int)(blockIdx.x >> 3), tile = item % tiles, part = item / tiles;
+    const int band = tile / (8 * z.tiles_n), in_band = tile - band * 8 * z.tiles_n, high = min(z.tiles_m - 8 * band, 8);
+    const int m0 = (8 * band + in_band % high) * kM, n0 = in_band / high * kN;
+    const int first = part * z.per_part, pieces = min(z.per_part, z.pieces - first);
+
+    // what this wave fetches: 1024 bytes of codes at a time, 256 of scales; a row group beyond the operand's last takes the last
+    // one's place (what comes of it is not stored)
+    const uint8_t *src[kCodeLoads], *scale_src[kScaleLoads];
+    int scale_dst[kScaleLoads];
+#pragma unroll
+    for (int i = 0; i < kCodeLoads; ++i) {
+        const int g = wave + i * kWaves;
+        const bool is_a = g < kM / 16;
+        const int group = is_a ? min(m0 / 16 + g, z.a_groups - 1) : min(n0 / 16 + g - kM / 16, z.b_groups - 1);
+        src[i] = (is_a ? a.a.codes : a.b.codes) + ((int64_t)group * z.pieces + first) * 1024;
+    }
+#pragma unroll
+    for (int i = 0; i < kScaleLoads; ++i) {
+        const int g = (wave + i * kWaves) % ((kM + kN) / 64);       // (some twice, so that every wave has as many loads in flight)
+        const bool is_a = g < kM / 64;
+        const int group = is_a ? min(m0 / 64 + g, z.a_groups / 4 - 1) : min(n0 / 64 + g - kM / 64, z.b_groups / 4 - 1);
+        scale_src[i] = (is_a ? a.a.scales : a.b.scales) + ((int64_t)group * z.pieces + first) * 256;
+        scale_dst[i] = (kM + kN) * 64 + g * 256;
+    }
+    auto fetch = [&](int s, int slot) {
+        uint8_t *to = lds + slot * kStage;
+#pragma unroll
+        for (int i = 0; i < kCodeLoads; ++i) to_lds<16>(src[i] + (int64_t)s * 1024 + lane * 16, to + (wave + i * kWaves) * 1024);
+#pragma unroll
+        for (int i = 0; i < kScaleLoads; ++i) to_lds<4>(scale_src[i] + (int64_t)s * 256 + lane * 4, to + scale_dst[i]);
+    };
+    const int la = wm * TM * 1024 + lane * 16, lb = (kM / 16 + wn * TN) * 1024 + lane * 16;
+    const int sa = (kM + kN) * 64 + wm * TM / 4 * 256 + lane * 4, sb = (kM + kN) * 64 + kM * 4 + wn * TN / 4 * 256 + lane * 4;
+    typedef Step<TM, TN> S;
+    auto read = [&](int slot, S &f) {
+        const uint8_t *from = lds + slot * kStage;
+        // (two tiles of 16 rows a wave: every other wave has the upper two of a register's scales)
+#pragma unroll
+        for (int i = 0; i < (TM + 3) / 4; ++i) f.ea[i] = *reinterpret_cast<const int *>(from + sa + i * 256) >> (TM == 2 ? wm % 2 * 16 : 0);
+#pragma unroll
+        for (int i = 0; i < (TN + 3) / 4; ++i) f.eb[i] = *reinterpret_cast<const int *>(from + sb + i * 256) >> (TN == 2 ? wn % 2 * 16 : 0);
+#pragma unroll
+        for (int i = 0; i < TN; ++i) f.b[i] = *reinterpret_cast<const v4i *>(from + lb + i * 1024);
+#pragma unroll
+        for (int i = 0; i < TM; ++i) f.a[i] = *reinterpret_cast<const v4i *>(from + la + i * 1024);
+    };
     f32x4 acc[TN][TM] = {};
-    for (int64_t kc = 0; kc < pieces; ++kc) {
-        // a row group beyond the operand's last takes the last one's place: what comes of it is not stored
-        for (int g = wave; g < (kM + kN) / 16; g += kWaves) {
-            const bool is_a = g < kM / 16;
-            const int64_t group = is_a ? min(m0 / 16 + g, a_groups - 1) : min(n0 / 16 + g - kM / 16, b_groups - 1);
-            const uint8_t *src = (is_a ? a.a.codes : a.b.codes) + (group * pieces + kc) * 1024;
-            *reinterpret_cast<v4i *>(lds + g * 1024 + lane * 16) = *reinterpret_cast<const v4i *>(src + lane * 16);
-        }
-        for (int g = wave; g < (kM + kN) / 64; g += kWaves) {
-            const bool is_a = g < kM / 64;
-            const int64_t group = is_a ? min(m0 / 64 + g, a_groups / 4 - 1) : min(n0 / 64 + g - kM / 64, b_groups / 4 - 1);
-            const uint8_t *src = (is_a ? a.a.scales : a.b.scales) + (group * pieces + kc) * 256;
-            *reinterpret_cast<int *>(lds + (kM + kN) * 64 + g * 256 + lane * 4) = *reinterpret_cast<const int *>(src + lane * 4);
-        }
-        __syncthreads();
-        const uint8_t *la = lds + wm * TM * 1024 + lane * 16, *lb = lds + (kM / 16 + wn * TN) * 1024 + lane * 16;
-        const uint8_t *sa = lds + (kM + kN) * 64 + wm * TM * 64 + lane * 4, *sb = lds + (kM + kN) * 64 + kM * 4 + wn * TN * 64 + lane * 4;
-        v4i fa[TM], fb[TN];
-        int ea[TM / 4], eb[TN / 4];
-#pragma unroll
-        for (int i = 0; i < TM; ++i) fa[i] = *reinterpret_cast<const v4i *>(la + i * 1024);
-#pragma unroll
-        for (int i = 0; i < TN; ++i) fb[i] = *reinterpret_cast<const v4i *>(lb + i * 1024);
-#pragma unroll
-        for (int i = 0; i < TM / 4; ++i) ea[i] = *reinterpret_cast<const int *>(sa + i * 256);
-#pragma unroll
-        for (int i = 0; i < TN / 4; ++i) eb[i] = *reinterpret_cast<const int *>(sb + i * 256);
-        unroll<TN>([&](auto j) {
-            unroll<TM>([&](auto i) {
+    int slot = 0;
+    // Step s: its fragments are in `now`; those of the next one go to `next` (behind the last step: what is left there, for nothing), a read
+    // after every few products: reads wait for LDS in the order of their issue, and products behind them would wait with them.
+    auto step = [&](int s, auto steady, const S &now, S &next) {
+        const int after = slot + 1 == STAGES ? 0 : slot + 1;
+        wait_loads<decltype(steady)::value ? (STAGES - 2) * kLoads : 0>();
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+        if (decltype(steady)::value || s + STAGES < pieces) fetch(s + STAGES, slot);
+        __builtin_amdgcn_sched_barrier(0);
+        read(after, next);
+        unroll<TM>([&](auto i) {
+            unroll<TN>([&](auto j) {
                 constexpr int I = decltype(i)::value, J = decltype(j)::value;
-                acc[J][I] = mfma_mx<J % 4, I % 4>(fb[J], fa[I], acc[J][I], eb[J / 4], ea[I / 4]);
+                acc[J][I] = mfma_mx<J % 4, I % 4>(now.b[J], now.a[I], acc[J][I], now.eb[J / 4], now.ea[I / 4]);
             });
         });
-        __syncthreads();
+        unroll<TM + TN>([&](auto r) {
+            constexpr int R = decltype(r)::value, kReads = TM + TN, kProducts = TM * TN;
+            __builtin_amdgcn_sched_group_barrier(0x008, (R + 1) * kProducts / kReads - R * kProducts / kReads, 0);
+            __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+        });
+        __builtin_amdgcn_sched_barrier(0);
+        slot = after;
+    };
+
+    for (int s = 0; s < min(pieces, STAGES); ++s) fetch(s, s);
+    if (pieces >= STAGES) wait_loads<(STAGES - 1) * kLoads>();
+    else wait_loads<0>();
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+    S even, odd;
+    read(0, even);
+    int s = 0;
+    // (steps in twos, so that fragments need not be moved; the loop of steady steps is a block without branches: the compiler would move
+    // products over a branch, away from the reads that they are to hide)
+    for (; s + 1 + STAGES < pieces; s += 2) {
+        step(s, std::true_type{}, even, odd);
+        step(s + 1, std::true_type{}, odd, even);
+    }
+    for (; s < pieces; s += 2) {
+        step(s, std::false_type{}, even, odd);
+        if (s + 1 >= pieces) odd = S{};
+        step(s + 1, std::false_type{}, odd, even);
+    }
+    if (a.partials) {
+        a.c.data = a.partials + (int64_t)part * a.m * a.n;
+        a.c.pitch = a.n;
     }
 #pragma unroll
     for (int i = 0; i < TM; ++i) {
         const int64_t row = m0 + (wm * TM + i) * 16 + (lane & 15);
-        if (row >= a.m) continue;
 #pragma unroll
-        for (int j = 0; j < TN; ++j) store_four<BF16>(a, row, n0 + (wn * TN + j) * 16 + 4 * (lane >> 4), acc[j][i]);
+        for (int j = 0; j < TN; j += 2) store_pair<BF16, ADD, PAST>(a, row, n0 + (wn * TN + j) * 16, lane >> 4, acc[j][i], acc[j + 1][i]);
     }
+}
+
+// Few rows of A (16 MT at most): a workgroup takes 16 rows of B, read once, straight to registers; its WAVES waves take pieces of the long axis in
+// turn, and their sums are added in order.
+template <bool BF16, bool ADD, int MT, int WAVES>
+__global__ __launch_bounds__(64 * WAVES) void k_mx_rows(MxProductArgs a, int pieces)
+{
+    __shared__ f32x4 sums[WAVES][MT][64];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int64_t group = blockIdx.x;
+    const uint8_t *b = a.b.codes + group * pieces * 1024 + lane * 16, *eb = a.b.scales + (group >> 2) * pieces * 256 + lane * 4;
+    const uint8_t *ac = a.a.codes + lane * 16, *ea = a.a.scales + lane * 4;
+    const int shift = (int)(group & 3) * 8;
+    f32x4 acc[MT] = {};
+    constexpr int kDeep = 4;
+    for (int p0 = wave; p0 < pieces; p0 += kDeep * WAVES) {
+        v4i fb[kDeep], fa[kDeep][MT];
+        int sb[kDeep], sa[kDeep];
+#pragma unroll
+        for (int d = 0; d < kDeep; ++d) {
+            const int p = min(p0 + d * WAVES, pieces - 1);
+            fb[d] = *reinterpret_cast<const v4i *>(b + (int64_t)p * 1024);
+            sb[d] = *reinterpret_cast<const int *>(eb + (int64_t)p * 256) >> shift;
+            sa[d] = *reinterpret_cast<const int *>(ea + (int64_t)p * 256);
+#pragma unroll
+            for (int i = 0; i < MT; ++i) fa[d][i] = *reinterpret_cast<const v4i *>(ac + ((int64_t)i * pieces + p) * 1024);
+        }
+#pragma unroll
+        for (int d = 0; d < kDeep; ++d)
+            if (p0 + d * WAVES < pieces)
+                unroll<MT>([&](auto i) {
+                    constexpr int I = decltype(i)::value;
+                    acc[I] = mfma_mx<0, I>(fb[d], fa[d][I], acc[I], sb[d], sa[d]);
+                });
+    }
+#pragma unroll
+    for (int i = 0; i < MT; ++i) sums[wave][i][lane] = acc[i];
+    __syncthreads();
+    for (int i = wave; i < MT; i += WAVES) {
+        f32x4 v = sums[0][i][lane];
+#pragma unroll
+        for (int w = 1; w < WAVES; ++w) v += sums[w][i][lane];
+        const int64_t row = i * 16 + (lane & 15), col = group * 16 + 4 * (lane >> 4);
+        const float x[4] = {v[0], v[1], v[2], v[3]};
+        if (row < a.m && col < a.n) store_row<BF16, ADD, false, 4>(a, row, col, x);
+    }
+}
+
+// Adds the parts of the long axis in their order, four columns a thread.
+template <bool BF16, bool ADD>
+__global__ __launch_bounds__(256) void k_mx_join(MxProductArgs a, int parts, uint32_t fours_a_row)
+{
+    const uint64_t t = (uint64_t)blockIdx.x * 256 + threadIdx.x;
+    const int64_t row = (int64_t)(t / fours_a_row), col = (int64_t)(t % fours_a_row) * 4;
+    if (row >= a.m) return;
+    const int left = (int)min<int64_t>(a.n - col, 4);
+    float v[4] = {};
+    for (int p = 0; p < parts; ++p) {
+        const float *from = a.partials + ((int64_t)p * a.m + row) * a.n + col;
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (i < left) v[i] += from[i];
+    }
+    store_row<BF16, ADD, false, 4>(a, row, col, v);
 }
 
 template <typename F>
@@ -121,21 +329,106 @@ void by_bool(bool v, F &&go)
     else go(std::false_type{});
 }
 
+enum Tiles { kRows, kTiny, kSmall, kWide, kLarge };
+
+struct Choice {
+    Tiles tiles;
+    int parts, per_part;                // of the long axis
+};
+
+constexpr int kCus = 256;
+
+// Which kernel.  us of a call in a graph (bf16 C), kernel / the next best one:
+//   rows (m <= 64)   8 x 8192 x 2048 2.7 / 4.8 tiny, 1 x 50304 x 2048 11.3 / 11.8 small, 64 x 2048 x 8192 5.4 / 9.8 tiny in 4 parts
+//   large, 256 x 256, eight waves: the fewest reads from LDS, but a CU holds one workgroup, which begins and ends alone:
+//                    8192 x 8192 x 8192 242 / 257 wide, 8192 x 2048 x 8192 68 / 72 wide, but 4096 x 50304 x 2048 263 / 236 wide
+//   wide, 256 x 128, two workgroups a CU:  8192 x 8192 x 2048 81 / 83, 4096 x 50304 x 2048 236 / 247 small, but 1024 x 50304 x 768 41 / 39 small
+//   small, 128 x 128, three a CU:  2048 x 2048 x 16384 43 / 56 in 2 parts, 60 tiny, 65 wide; 512 x 8192 x 2048 9.4 / 11.8 tiny
+//   tiny, 64 x 64, where small ones do not reach every CU:  1024 x 1024 x 1024 4.0 / 5.6, 16384 x 16 x 4096 8.4 / 11.7, 128 x 4096 x 1024 3.8 / 5.5
+// The long axis in parts, added up by a launch of its own: 256 x 256 x 8192 9.4 in 4 parts / 12.6, but 200 x 1024 x 4096 8.7 in 2 / 7.6.
+Choice choose(int64_t m, int64_t n, int64_t k)
+{
+    const int64_t pieces = std::max<int64_t>((k + 127) / 128, 1);
+    auto tiles = [&](int64_t tm, int64_t tn) { return ((m + tm - 1) / tm) * ((n + tn - 1) / tn); };
+    if (m <= 64) return {kRows, 1, (int)pieces};
+    if (tiles(256, 256) >= 192 && pieces >= 12) return {pieces >= 48 ? kLarge : kWide, 1, (int)pieces};
+    if (tiles(128, 128) >= 200) return {kSmall, 1, (int)pieces};
+    const int64_t parts = pieces < 64 ? 1 : std::max<int64_t>(std::min<int64_t>(kCus / tiles(64, 64), pieces / 16), 1);
+    const int64_t per = (pieces + parts - 1) / parts;
+    return {kTiny, (int)((pieces + per - 1) / per), (int)per};
+}
+
+template <bool BF16, bool ADD, bool PAST, int WM, int WN, int TM, int TN, int STAGES, int WAVES>
+void launch_tiles(const MxProductArgs &a, const Choice &c, hipStream_t st)
+{
+    constexpr int kM = WM * TM * 16, kN = WN * TN * 16;
+    Shape z;
+    z.pieces = (int)((a.k + 127) / 128);
+    z.a_groups = (int)((a.m + 63) / 64 * 4);
+    z.b_groups = (int)((a.n + 63) / 64 * 4);
+    z.tiles_m = (int)((a.m + kM - 1) / kM);
+    z.tiles_n = (int)((a.n + kN - 1) / kN);
+    z.per_part = c.per_part;
+    z.items = z.tiles_m * z.tiles_n * c.parts;
+    hipLaunchKernelGGL((k_mx_product<BF16, ADD, PAST, WM, WN, TM, TN, STAGES, WAVES>), dim3((unsigned)z.items), dim3(64 * WM * WN), 0, st, a, z);
+}
+
+template <bool BF16, bool ADD>
+void launch_rows(const MxProductArgs &a, hipStream_t st)
+{
+    const int64_t groups = (a.n + 15) / 16;
+    const int pieces = (int)((a.k + 127) / 128);
+    auto go = [&](auto mt, auto waves) {
+        constexpr int W = decltype(waves)::value;
+        hipLaunchKernelGGL((k_mx_rows<BF16, ADD, decltype(mt)::value, W>), dim3((unsigned)groups), dim3(64 * W), 0, st, a, pieces);
+    };
+    auto by_waves = [&](auto mt) {
+        if (pieces > 4 && (groups < 2 * kCus || pieces >= 64)) go(mt, std::integral_constant<int, 8>{});
+        else go(mt, std::integral_constant<int, 4>{});
+    };
+    if (a.m <= 16) by_waves(std::integral_constant<int, 1>{});
+    else if (a.m <= 32) by_waves(std::integral_constant<int, 2>{});
+    else by_waves(std::integral_constant<int, 4>{});
+}
+
 }  // namespace
 
 size_t mx_product_workspace(int64_t m, int64_t n, int64_t k)
 {
-    (void)m; (void)n; (void)k;
-    return 0;
+    const Choice c = choose(m, n, k);
+    return c.parts > 1 ? (size_t)c.parts * (size_t)m * (size_t)n * sizeof(float) : 0;
 }
 
 void launch_mx_product(const MxProductArgs &a, bool bf16, hipStream_t st)
 {
-    const int64_t pieces = (a.k + 127) / 128, a_groups = (a.m + 63) / 64 * 4, b_groups = (a.n + 63) / 64 * 4;
-    const int64_t tiles_m = (a.m + 127) / 128, tiles_n = (a.n + 127) / 128;
+    const Choice c = choose(a.m, a.n, a.k);
+    if (c.parts > 1) {
+        MxProductArgs p = a;
+        p.alpha = 1.0f;                     // (beta is for the launch that adds the parts)
+        launch_tiles<false, false, false, 2, 2, 2, 2, 4, 4>(p, c, st);
+    }
+    // a C larger than the card's last cache goes past the caches: 4096 x 50304 in bf16 236 / 290 us, but 8192 x 8192 85 / 80
+    const bool past = a.m * a.n * (bf16 ? 2 : 4) > (int64_t)256 << 20;
     by_bool(bf16, [&](auto b) {
-        hipLaunchKernelGGL((k_mx_product<decltype(b)::value, 2, 2, 4, 4>), dim3((unsigned)(tiles_m * tiles_n)), dim3(256), 0, st, a, pieces,
-                           a_groups, b_groups, tiles_m);
+        by_bool(a.beta != 0.0f, [&](auto add) {
+            constexpr bool B = decltype(b)::value, ADD = decltype(add)::value;
+            if (c.tiles == kRows) {
+                launch_rows<B, ADD>(a, st);
+            } else if (c.parts > 1) {
+                const uint32_t fours = (uint32_t)((a.n + 3) / 4);
+                hipLaunchKernelGGL((k_mx_join<B, ADD>), dim3((unsigned)(((uint64_t)a.m * fours + 255) / 256)), dim3(256), 0, st, a, c.parts,
+                                   fours);
+            } else if (c.tiles == kTiny) {
+                launch_tiles<B, ADD, false, 2, 2, 2, 2, 4, 4>(a, c, st);
+            } else if (c.tiles == kSmall) {
+                launch_tiles<B, ADD, false, 2, 2, 4, 4, 3, 3>(a, c, st);
+            } else {
+                by_bool(past, [&](auto p) {
+                    if (c.tiles == kWide) launch_tiles<B, ADD, decltype(p)::value, 2, 2, 8, 4, 3, 2>(a, c, st);
+                    else launch_tiles<B, ADD, decltype(p)::value, 2, 4, 8, 4, 4, 2>(a, c, st);
+                });
+            }
+        });
     });
 }
 
