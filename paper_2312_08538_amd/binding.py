@@ -482,26 +482,31 @@ def conef_cs_decode_error(ctx, table, e_out, stream=0):
 
 # a worker's own step: dropout, layer norm, microscaled 4-bit floating point.  Matrices are torch tensors of two dimensions
 # (rows may be strided); their shape, type and pitch go with their address.
+_kinds: dict = {}             # element types of matrices, once torch is there
+
+
 def _matrix(t, shape=None, dtype=None) -> Tuple[int, int, int, int, int]:
     """(address, pitch, rows, cols, type) of a two-dimensional tensor whose rows are contiguous; of None: all 0."""
-    import torch
-
     if t is None:
         return 0, 0, 0, 0, 0
-    kind = {torch.float32: F32, torch.bfloat16: BF16}.get(t.dtype, -1)
-    if t.dim() != 2 or kind < 0 or (t.shape[1] > 1 and t.stride(1) != 1):
-        raise ConefError(EINVAL, f"a matrix of fp32 or bf16 with contiguous rows is wanted, not {tuple(t.shape)} {t.dtype} {t.stride()}")
-    rows, cols = t.shape
-    if (shape is not None and (rows, cols) != shape) or (dtype is not None and kind != dtype):
+    if not _kinds:
+        import torch
+
+        _kinds.update({torch.float32: F32, torch.bfloat16: BF16})
+    kind, size, stride = _kinds.get(t.dtype, -1), t.shape, t.stride()
+    if len(size) != 2 or kind < 0 or (stride[1] != 1 and size[1] > 1):
+        raise ConefError(EINVAL, f"a matrix of fp32 or bf16 with contiguous rows is wanted, not {tuple(size)} {t.dtype} {stride}")
+    rows, cols = size
+    if shape is not None and (rows, cols, kind) != (*shape, dtype):
         raise ConefError(EINVAL, f"a matrix of {shape} and type {dtype} is wanted, not {(rows, cols)} of type {kind}")
-    return t.data_ptr(), t.stride(0) if rows > 1 else max(cols, 1), rows, cols, kind
+    return t.data_ptr(), stride[0] if rows > 1 else max(cols, 1), rows, cols, kind
 
 
 def _vector(t, n: int) -> int:
     """Address of n contiguous floats; 0 for None."""
     if t is None:
         return 0
-    if t.dim() != 1 or t.shape[0] != n or str(t.dtype) != "torch.float32" or (n > 1 and t.stride(0) != 1):
+    if t.shape != (n,) or str(t.dtype) != "torch.float32" or not t.is_contiguous():
         raise ConefError(EINVAL, f"{n} contiguous floats are wanted, not {tuple(t.shape)} {t.dtype}")
     return t.data_ptr()
 
@@ -510,17 +515,17 @@ def _room(t, bytes_: int) -> int:
     """Address of a buffer of at least `bytes_` bytes; 0 for None."""
     if t is None:
         return 0
-    if not t.is_contiguous() or t.numel() * t.element_size() < bytes_:
-        raise ConefError(EINVAL, f"a contiguous buffer of {bytes_} bytes is wanted, not {t.numel() * t.element_size()}")
+    if t.nbytes < bytes_ or not t.is_contiguous():
+        raise ConefError(EINVAL, f"a contiguous buffer of {bytes_} bytes is wanted, not {t.nbytes}")
     return t.data_ptr()
 
 
 def _packed(pair, rows: int, cols: int) -> Tuple[int, int]:
-    """Addresses of the codes and scales of a packed rows x cols operand; 0 for None."""
+    """Addresses of the codes and scales of a packed rows x cols operand, of conef_mx_sizes() bytes; 0 for None."""
     if pair is None:
         return 0, 0
-    s = conef_mx_sizes(rows, cols)
-    return _room(pair[0], s["code_bytes"]), _room(pair[1], s["scale_bytes"])
+    elements = -(-rows // 64) * -(-cols // 128) * 8192
+    return _room(pair[0], elements // 2), _room(pair[1], elements // 32)
 
 
 def conef_dropout_forward(drop, x, residual, y, stream=0):
@@ -557,7 +562,7 @@ def conef_norm_backward(drop, dy, z, gamma, mean, rstd, dz_in, dz, dx, dgamma, d
     pi, ii = _matrix(dz_in, (rows, cols), kind)[:2]
     po, io = _matrix(dz, (rows, cols), kind)[:2]
     px, ix = _matrix(dx, (rows, cols), kind)[:2]
-    ws = _room(workspace, conef_norm_workspace(rows, cols))
+    ws = _room(workspace, conef_norm_workspace(rows, cols)) if workspace is not None else 0
     _check(lib().conef_norm_backward(drop, rows, cols, kind, py, iy, pz, iz, _vector(gamma, cols), _vector(mean, rows),
                                      _vector(rstd, rows), pi, ii, po, io, px, ix, _vector(dgamma, cols), _vector(dbeta, cols), ws,
                                      stream), "conef_norm_backward")
@@ -598,7 +603,7 @@ def conef_mx_product_workspace(m: int, n: int, k: int) -> int:
 def conef_mx_product(a, b, k: int, alpha: float, beta: float, c, workspace, stream=0):
     """c [m, n] <- alpha A B^T + beta c of the packed operands a (m x k) and b (n x k)."""
     pc, ic, m, n, kind = _matrix(c)
-    ws = _room(workspace, conef_mx_product_workspace(m, n, k))
+    ws = _room(workspace, conef_mx_product_workspace(m, n, k)) if workspace is not None else 0
     _check(lib().conef_mx_product(*_packed(a, m, k), *_packed(b, n, k), m, n, k, alpha, beta, pc, ic, kind, ws, stream),
            "conef_mx_product")
 

@@ -15,101 +15,195 @@ namespace conef {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kTile = 128;              // rows and columns of a workgroup
-constexpr int kPitch = 130;             // of the tile in LDS: four rows 8 apart lie 8 banks apart
 
-// The scale byte of a block and the factor that takes its elements over the scale (exact: 2^(127 - byte) is normal)
-__device__ __forceinline__ uint32_t scale_byte(uint32_t most_bits, bool stochastic)
+// The scale byte of a block whose largest magnitude has these bits: its exponent less 2, at least 0; stochastic: one more for a mantissa
+// above 1.5, by a carry (below 2^-125 the scale is the smallest there is, and what it divides stays below 4).
+__device__ __forceinline__ uint32_t scale_byte(uint32_t most, bool stochastic)
 {
-    const uint32_t e = most_bits >> 23;
-    if (e == 255) return 255;
-    uint32_t s = e > 2 ? e - 2 : 0;
-    // (below 2^-125 the scale is the smallest there is, and what it divides stays below 4)
-    if (stochastic && e >= 2 && (most_bits & 0x7FFFFFu) > 0x400000u) s = e - 1;
-    return s;
+    const uint32_t s = ((max(most, 2u << 23) + (stochastic ? 0x3FFFFFu : 0u)) >> 23) - 2;
+    return most >= 255u << 23 ? 255u : s;
 }
 
-// Code of a value over its scale, to nearest even
-__device__ __forceinline__ uint32_t code_nearest(float v)
-{
-    const float a = fabsf(v);
-    const uint32_t c = (uint32_t)(a > 0.25f) + (uint32_t)(a >= 0.75f) + (uint32_t)(a > 1.25f) + (uint32_t)(a >= 1.75f) +
-                       (uint32_t)(a > 2.5f) + (uint32_t)(a >= 3.5f) + (uint32_t)(a > 5.0f);
-    return c | (__float_as_uint(v) >> 31 << 3);
-}
+typedef float f32x2 __attribute__((ext_vector_type(2)));
 
-// The same with a 16-bit draw u: in units of 2^-17 the step below 2 is 65536, from 2 on twice, from 4 on four times that.
-__device__ __forceinline__ uint32_t code_stochastic(float v, uint32_t u)
-{
-    const uint32_t f = (uint32_t)(fabsf(v) * 131072.0f);
-    const uint32_t wide = (uint32_t)(f >= (1u << 18)) + (uint32_t)(f >= (1u << 19));
-    const uint32_t c = (((f >> wide) + u) >> 16) + 2 * wide;
-    return c | (__float_as_uint(v) >> 31 << 3);
-}
+// The values of an octet, each in the lower of two neighbouring registers, as the conversion that rounds stochastically takes
+// them.  What the upper one holds is not used: the empty asm is its definition, without an instruction.
+struct Values {
+    f32x2 v[8];
 
-// Quantises a block of which each of four neighbouring lanes holds an octet: returns the lane's eight codes and the block's
-// scale byte.
-template <bool STOCHASTIC>
-__device__ __forceinline__ uint32_t quantise_quad(const float v[8], const Draws &d, uint32_t octet, uint32_t &byte)
-{
-    uint32_t most = 0;
+    __device__ __forceinline__ Values()
+    {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) most = max(most, __float_as_uint(v[i]) & 0x7FFFFFFFu);       // (a NaN's bits are above infinity's)
-    most = max(most, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)most, 0xB1, 0xF, 0xF, true));
-    most = max(most, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)most, 0x4E, 0xF, 0xF, true));
-    byte = scale_byte(most, STOCHASTIC);
-    if (byte == 255) return 0;
-    const float over = __uint_as_float((254u - byte) << 23);
-    uint32_t codes = 0;
-    if constexpr (STOCHASTIC) {
-        uint32_t u[4];
-        octet_draws(d, octet, u);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) codes |= code_stochastic(v[i] * over, (i & 1) ? u[i >> 1] >> 16 : u[i >> 1] & 0xFFFFu) << (4 * i);
-    } else {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) codes |= code_nearest(v[i] * over) << (4 * i);
+        for (int i = 0; i < 8; ++i) asm volatile("" : "=v"(v[i]));
     }
-    return codes;
+};
+
+template <bool BF16>
+__device__ __forceinline__ void widen(const Octet<BF16> &o, Values &x)
+{
+    float v[8];
+    widen<BF16>(o, v);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x.v[i].x = v[i];
 }
 
-// A workgroup takes 128 x 128 elements.  By rows: a wave takes 16 rows, of which its lanes read 32 columns at a time, four
-// lanes a block, and writes the 256 bytes of that piece together.  By columns: the same on the tile in LDS, turned.
-template <bool BF16, bool STOCHASTIC, bool BY_ROWS, bool BY_COLS>
-__global__ __launch_bounds__(kThreads) void k_mx_quantise(MxQuantArgs a, int64_t row_pieces, int64_t col_pieces, int64_t padded_rows,
-                                                          int64_t padded_cols)
+// Eight values over the scale of byte `byte` as codes, by the conversion instructions.  They take the scale from a float's exponent
+// (0: 2^-127), denormal values as they are, and keep 6 for what is above it.  The one that rounds stochastically adds its
+// random word to the bits it drops, aligned at the top, for the lower of its two values: with a draw in the upper half of that word, zeros
+// below, it rounds up iff floor(65536 f) + draw >= 65536.  The upper value gets other bits of the word, so each value takes an
+// instruction of its own, of which the lower four bits count: four codes are put together from there in five more.
+template <bool STOCHASTIC>
+__device__ __forceinline__ uint32_t codes_over(const Values &x, uint32_t byte, const uint32_t u[4])
 {
+    const float scale = __uint_as_float(byte << 23);
+    if constexpr (STOCHASTIC) {
+        uint32_t two[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const uint32_t low = u[i] << 16, high = u[i] & 0xFFFF0000u;
+            const uint32_t even = __builtin_amdgcn_cvt_scalef32_sr_pk_fp4_f32(low, x.v[2 * i], low, scale, 0);
+            const uint32_t odd = __builtin_amdgcn_cvt_scalef32_sr_pk_fp4_f32(high, x.v[2 * i + 1], high, scale, 0);
+            two[i] = (even & 0xFu) | (odd << 4 & ~0xFu);
+        }
+        const uint32_t low = __builtin_amdgcn_perm(two[1], two[0], 0x00000400u), high = __builtin_amdgcn_perm(two[3], two[2], 0x00000400u);
+        return __builtin_amdgcn_perm(high, low, 0x05040100u);
+    } else {
+        uint32_t c = 0;
+        c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, x.v[0].x, x.v[1].x, scale, 0);
+        c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, x.v[2].x, x.v[3].x, scale, 1);
+        c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, x.v[4].x, x.v[5].x, scale, 2);
+        return __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, x.v[6].x, x.v[7].x, scale, 3);
+    }
+}
+
+// bits of the largest magnitude; a NaN's if there is one (its bits are above infinity's)
+__device__ __forceinline__ uint32_t largest(const Values &x)
+{
+    float m = fabsf(x.v[0].x);
+#pragma unroll
+    for (int i = 1; i < 8; ++i) m = __builtin_elementwise_maximum(m, fabsf(x.v[i].x));
+    return __float_as_uint(m) & 0x7FFFFFFFu;
+}
+
+// Quantises a block of which each of four lanes holds an octet, `most` the largest magnitude of all four: returns the lane's eight codes and
+// the block's scale byte.
+template <bool STOCHASTIC>
+__device__ __forceinline__ uint32_t quantise_octet(const Values &x, uint32_t most, const Draws &d, uint32_t octet, uint32_t &byte)
+{
+    byte = scale_byte(most, STOCHASTIC);
+    uint32_t u[4] = {};
+    if constexpr (STOCHASTIC) octet_draws(d, octet, u);
+    const uint32_t c = codes_over<STOCHASTIC>(x, byte, u);
+    return byte == 255 ? 0 : c;
+}
+
+// the largest over the lanes l ^ 1, l ^ 2 / over l ^ 16, l ^ 32
+__device__ __forceinline__ uint32_t quad_largest(uint32_t m)
+{
+    m = max(m, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)m, 0xB1, 0xF, 0xF, true));
+    return max(m, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)m, 0x4E, 0xF, 0xF, true));
+}
+__device__ __forceinline__ uint32_t rows_largest(uint32_t m)
+{
+    auto r = __builtin_amdgcn_permlane16_swap(m, m, false, false);
+    m = max((uint32_t)r[0], (uint32_t)r[1]);
+    r = __builtin_amdgcn_permlane32_swap(m, m, false, false);
+    return max((uint32_t)r[0], (uint32_t)r[1]);
+}
+
+// 128 rows of 64 columns in LDS, for reading eight rows of a column.  bf16: by transposing reads, sixteen lanes 4 rows x 16 columns at a
+// time; a row has half the banks, and where in it a piece of 16 columns lies goes by the row, so that the eight rows that half a
+// wave reads from lie in banks of their own.  fp32: element by element.
+template <bool BF16>
+struct Turned {
+    static constexpr int kPitch = BF16 ? 64 : 66;
     typedef std::conditional_t<BF16, uint16_t, float> Elem;
-    __shared__ Elem tile[BY_COLS ? kTile * kPitch : 1];
-    __shared__ __attribute__((aligned(4))) uint8_t scales[2][512];
+    Elem e[128 * kPitch];
+
+    static __device__ __forceinline__ int piece(int row, int col) { return ((col >> 4) ^ (row >> 1 & 1) ^ (row >> 2 & 2)) << 4; }
+
+    __device__ __forceinline__ void put(int row, int col, const Octet<BF16> &o)
+    {
+        if constexpr (BF16) {
+            *reinterpret_cast<uint4 *>(e + row * kPitch + piece(row, col) + (col & 8)) = make_uint4(o.w[0][0], o.w[0][1], o.w[0][2], o.w[0][3]);
+        } else {
+            uint2 *p = reinterpret_cast<uint2 *>(e + row * kPitch + col);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) p[i] = make_uint2(o.w[i >> 1][2 * (i & 1)], o.w[i >> 1][2 * (i & 1) + 1]);
+        }
+    }
+
+    // rows row .. row + 7 (row: a multiple of 8, the same for 16 lanes) of column col + lane % 16
+    __device__ __forceinline__ void get(int row, int col, int lane, Values &v) const
+    {
+        if constexpr (BF16) {
+            typedef short s16x4 __attribute__((ext_vector_type(4)));
+            typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+            const int from = row + (lane >> 2 & 3);
+            const Elem *p = e + from * kPitch + piece(from, col) + 4 * (lane & 3);          // (the row four on has the same place)
+            union { s16x4 v; uint2 u; } lo, hi;
+            lo.v = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(p));
+            hi.v = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(p + 4 * kPitch));
+            Octet<BF16> o;
+            o.w[0] = u32x4_any{lo.u.x, lo.u.y, hi.u.x, hi.u.y};
+            widen<BF16>(o, v);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v.v[i].x = e[(row + i) * kPitch + col + (lane & 15)];
+        }
+    }
+};
+
+// A workgroup takes 64 rows of 128 columns, or 128 rows of 64 columns if it quantises by columns too.  By rows: a wave takes 16 rows, of which
+// its lanes read 32 columns at a time, four lanes a block, and writes the 256 bytes of that piece together.  By columns: the same on
+// the tile in LDS, turned, the four octets of a block 16 lanes apart.
+template <bool BF16, bool STOCHASTIC, bool BY_ROWS, bool BY_COLS>
+__global__ __launch_bounds__(kThreads) void k_mx_quantise(MxQuantArgs a, int64_t row_pieces, int64_t col_pieces, int64_t col_tiles,
+                                                          int64_t padded_rows, int64_t padded_cols)
+{
+    constexpr int kRows = BY_COLS ? 128 : 64, kCols = BY_COLS ? 64 : 128, kBlocks = kCols / 32;
+    __shared__ __attribute__((aligned(16))) std::conditional_t<BY_COLS, Turned<BF16>, char> tile;
+    __shared__ __attribute__((aligned(4))) uint8_t scales[2][256];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r = lane >> 2, q = lane & 3;
-    const int64_t tc = blockIdx.x % col_pieces, tr = blockIdx.x / col_pieces, row0 = tr * kTile, col0 = tc * kTile;
+    const int64_t row0 = blockIdx.x / col_tiles * kRows, col0 = blockIdx.x % col_tiles * kCols;
     const uint32_t per_row = (uint32_t)((a.cols + 7) >> 3), per_col = (uint32_t)((a.rows + 7) >> 3);
+    Octet<BF16> o[kRows / 64][kBlocks];
+    auto fetch = [&](bool whole) {
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-        const int group = wave + 4 * h;
-        const int64_t row = row0 + 16 * group + r;
+        for (int h = 0; h < kRows / 64; ++h) {
+            const int64_t row = row0 + 16 * (wave + 4 * h) + r;
 #pragma unroll
-        for (int b = 0; b < 4; ++b) {
-            const int64_t col = col0 + 32 * b + 8 * q;
-            float v[8];
-            load_octet<BF16>(a.x.data, row * a.x.pitch + col, row < a.rows ? (int)max<int64_t>(min<int64_t>(a.cols - col, 8), 0) : 0, v);
-            if constexpr (BY_COLS) {
-                Elem *t = tile + (16 * group + r) * kPitch + 32 * b + 8 * q;
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    if constexpr (BF16) t[i] = (uint16_t)(__float_as_uint(v[i]) >> 16);
-                    else t[i] = v[i];
-                }
+            for (int b = 0; b < kBlocks; ++b) {
+                const int64_t col = col0 + 32 * b + 8 * q;
+                o[h][b] = fetch_octet<BF16>(a.x.data, row * a.x.pitch + col, whole ? 8 : row < a.rows ? octet_left(a.cols - col) : 0);
             }
-            if constexpr (BY_ROWS) {
-                if (row0 + 16 * group < padded_rows) {
-                    uint32_t byte;
-                    const uint32_t c = quantise_quad<STOCHASTIC>(v, a.draws, (uint32_t)row * per_row + (uint32_t)(col >> 3), byte);
-                    const int64_t piece = (row0 / 16 + group) * col_pieces + tc;
-                    *reinterpret_cast<uint32_t *>(a.by_rows.codes + piece * 1024 + b * 256 + lane * 4) = c;
-                    if (q == 0) scales[0][(group >> 2) * 256 + b * 64 + r * 4 + (group & 3)] = (uint8_t)byte;
-                }
+        }
+    };
+    if (row0 + kRows <= a.rows && col0 + kCols <= a.cols) fetch(true);
+    else fetch(false);
+    if constexpr (BY_COLS) {
+#pragma unroll
+        for (int h = 0; h < kRows / 64; ++h)
+#pragma unroll
+            for (int b = 0; b < kBlocks; ++b) tile.put(16 * (wave + 4 * h) + r, 32 * b + 8 * q, o[h][b]);
+    }
+    if constexpr (BY_ROWS) {
+        const int64_t piece0 = row0 / 16 * col_pieces + col0 / 128;
+        const int block0 = BY_COLS ? (int)(col0 >> 5 & 3) : 0;               // of the piece
+#pragma unroll
+        for (int h = 0; h < kRows / 64; ++h) {
+            const int group = wave + 4 * h;
+            const int64_t row = row0 + 16 * group + r;
+            if (row0 + 16 * group >= padded_rows) continue;
+#pragma unroll
+            for (int b = 0; b < kBlocks; ++b) {
+                Values v;
+                widen<BF16>(o[h][b], v);
+                uint32_t byte;
+                const uint32_t octet = (uint32_t)row * per_row + (uint32_t)((col0 + 32 * b + 8 * q) >> 3);
+                const uint32_t c = quantise_octet<STOCHASTIC>(v, quad_largest(largest(v)), a.draws, octet, byte);
+                *reinterpret_cast<uint32_t *>(a.by_rows.codes + (piece0 + group * col_pieces) * 1024 + (block0 + b) * 256 + lane * 4) = c;
+                if (q == 0) scales[0][h * 64 * kBlocks + b * 64 + r * 4 + wave] = (uint8_t)byte;
             }
         }
     }
@@ -117,37 +211,45 @@ __global__ __launch_bounds__(kThreads) void k_mx_quantise(MxQuantArgs a, int64_t
     if constexpr (BY_COLS) {
         Draws d = a.draws;
         d.word += kMxColWord - kMxRowWord;
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            const int group = wave + 4 * h;
-            const int64_t col = col0 + 16 * group + r;                       // a row of the turned matrix
-            if (col0 + 16 * group >= padded_cols) continue;
+        const int c16 = lane & 15, q16 = lane >> 4;
+        const int64_t col = col0 + 16 * wave + c16;                          // a row of the turned matrix
+        if (col0 < padded_cols) {
+            uint8_t *codes = a.by_cols.codes + ((col0 / 16 + wave) * row_pieces + row0 / 128) * 1024 + c16 * 16 + q16 * 4;
 #pragma unroll
             for (int b = 0; b < 4; ++b) {
-                const int64_t row = row0 + 32 * b + 8 * q;
-                float v[8];
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    const Elem e = tile[(32 * b + 8 * q + i) * kPitch + 16 * group + r];
-                    if constexpr (BF16) v[i] = __uint_as_float((uint32_t)e << 16);
-                    else v[i] = e;
-                }
+                Values v;
+                tile.get(32 * b + 8 * q16, 16 * wave, lane, v);
                 uint32_t byte;
-                const uint32_t c = quantise_quad<STOCHASTIC>(v, d, (uint32_t)col * per_col + (uint32_t)(row >> 3), byte);
-                const int64_t piece = (col0 / 16 + group) * row_pieces + tr;
-                *reinterpret_cast<uint32_t *>(a.by_cols.codes + piece * 1024 + b * 256 + lane * 4) = c;
-                if (q == 0) scales[1][(group >> 2) * 256 + b * 64 + r * 4 + (group & 3)] = (uint8_t)byte;
+                const uint32_t octet = (uint32_t)col * per_col + (uint32_t)((row0 + 32 * b + 8 * q16) >> 3);
+                const uint32_t c = quantise_octet<STOCHASTIC>(v, rows_largest(largest(v)), d, octet, byte);
+                *reinterpret_cast<uint32_t *>(codes + b * 256) = c;
+                if (q16 == 0) scales[1][b * 64 + c16 * 4 + wave] = (uint8_t)byte;
             }
         }
         __syncthreads();
     }
-    // scales: two pieces of 256 bytes each way
-    const int half = (threadIdx.x >> 6) & 1, form = threadIdx.x >> 7;
-    const uint32_t word = reinterpret_cast<const uint32_t *>(scales[form])[half * 64 + lane];
-    if (BY_ROWS && form == 0 && row0 + 64 * half < padded_rows)
-        *reinterpret_cast<uint32_t *>(a.by_rows.scales + ((row0 / 64 + half) * col_pieces + tc) * 256 + lane * 4) = word;
-    if (BY_COLS && form == 1 && col0 + 64 * half < padded_cols)
-        *reinterpret_cast<uint32_t *>(a.by_cols.scales + ((col0 / 64 + half) * row_pieces + tr) * 256 + lane * 4) = word;
+    // the tile's scales, 256 bytes each way: by rows 64 bytes a block, two blocks of each 64 rows where there are 128
+    if (BY_ROWS && wave == 0) {
+        const int half = BY_COLS ? lane >> 5 : 0;
+        if (row0 + 64 * half < padded_rows)
+            *reinterpret_cast<uint32_t *>(a.by_rows.scales + ((row0 / 64 + half) * col_pieces + col0 / 128) * 256 + (BY_COLS ? (col0 >> 5 & 3) * 64 : 0) +
+                                          (lane - half * 32) * 4) = reinterpret_cast<const uint32_t *>(scales[0])[lane];
+    }
+    if (BY_COLS && wave == 1 && col0 < padded_cols)
+        *reinterpret_cast<uint32_t *>(a.by_cols.scales + (col0 / 64 * row_pieces + row0 / 128) * 256 + lane * 4) =
+            reinterpret_cast<const uint32_t *>(scales[1])[lane];
+}
+
+// What eight codes stand for
+__device__ __forceinline__ void values(uint32_t c, uint32_t byte, float v[8])
+{
+    const float scale = __uint_as_float(byte << 23);
+    const auto a = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c, scale, 0), b = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c, scale, 1);
+    const auto d = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c, scale, 2), e = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c, scale, 3);
+    v[0] = a[0]; v[1] = a[1]; v[2] = b[0]; v[3] = b[1]; v[4] = d[0]; v[5] = d[1]; v[6] = e[0]; v[7] = e[1];
+    if (byte == 255)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = __uint_as_float(0x7FC00000u);
 }
 
 // What a packed operand stands for: 16 rows a wave, 128 columns, four lanes a block.
@@ -164,18 +266,11 @@ __global__ __launch_bounds__(kThreads) void k_mx_dequantise(MxDequantArgs a, int
     for (int b = 0; b < 4; ++b) {
         const uint32_t c = *reinterpret_cast<const uint32_t *>(a.in.codes + p * 1024 + b * 256 + lane * 4);
         const uint32_t byte = scales[b * 64];
-        const float step = byte == 255 ? __uint_as_float(0x7FC00000u) : __uint_as_float(byte ? byte << 23 : 0x400000u);
         const int64_t col = tc * 128 + 32 * b + 8 * q;
         float v[8];
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const uint32_t m = (c >> (4 * i)) & 7;
-            // 0, 0.5, then (2 + (m & 1)) 2^(m / 2 - 2)
-            const float x = m < 2 ? 0.5f * (float)m : __uint_as_float(((126 + (m >> 1)) << 23) | ((m & 1) << 22));
-            v[i] = __uint_as_float(__float_as_uint(x) | ((c >> (4 * i + 3)) & 1) << 31) * step;
-        }
+        values(c, byte, v);
         if (row < a.rows && col < a.cols)
-            store_octet<BF16>(a.out.data, row * a.out.pitch + col, (int)min<int64_t>(a.cols - col, 8), v);
+            store_octet<BF16>(a.out.data, row * a.out.pitch + col, octet_left(a.cols - col), v);
     }
 }
 
@@ -192,12 +287,13 @@ void launch_mx_quantise(const MxQuantArgs &a, bool bf16, hipStream_t st)
 {
     const int64_t row_pieces = (a.rows + 127) / 128, col_pieces = (a.cols + 127) / 128;
     const int64_t padded_rows = (a.rows + 63) / 64 * 64, padded_cols = (a.cols + 63) / 64 * 64;
-    const dim3 grid((unsigned)(row_pieces * col_pieces));
+    const int64_t col_tiles = a.by_cols.codes ? 2 * col_pieces : col_pieces;
+    const dim3 grid((unsigned)((a.by_cols.codes ? row_pieces : padded_rows / 64) * col_tiles));
     by_bool(bf16, [&](auto b) {
         by_bool(a.stochastic != 0, [&](auto s) {
             auto go = [&](auto rows, auto cols) {
                 hipLaunchKernelGGL((k_mx_quantise<decltype(b)::value, decltype(s)::value, decltype(rows)::value, decltype(cols)::value>),
-                                   grid, dim3(kThreads), 0, st, a, row_pieces, col_pieces, padded_rows, padded_cols);
+                                   grid, dim3(kThreads), 0, st, a, row_pieces, col_pieces, col_tiles, padded_rows, padded_cols);
             };
             if (!a.by_cols.codes) go(std::true_type{}, std::false_type{});
             else if (!a.by_rows.codes) go(std::false_type{}, std::true_type{});

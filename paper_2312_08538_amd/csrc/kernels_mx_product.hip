@@ -311,7 +311,7 @@ __global__ __launch_bounds__(256) void k_mx_join(MxProductArgs a, int parts, uin
     const uint64_t t = (uint64_t)blockIdx.x * 256 + threadIdx.x;
     const int64_t row = (int64_t)(t / fours_a_row), col = (int64_t)(t % fours_a_row) * 4;
     if (row >= a.m) return;
-    const int left = (int)min<int64_t>(a.n - col, 4);
+    const int left = (int)(a.n - col < 4 ? a.n - col : 4);
     float v[4] = {};
     for (int p = 0; p < parts; ++p) {
         const float *from = a.partials + ((int64_t)p * a.m + row) * a.n + col;

@@ -18,37 +18,57 @@ __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi)
     return __builtin_bit_cast(uint32_t, v);
 }
 
+// elements of an octet with `left` of its row from it on, 0 to 8
+__device__ __forceinline__ int octet_left(int64_t left) { return left >= 8 ? 8 : left > 0 ? (int)left : 0; }
+
+// An octet as it lies in memory.
+template <bool BF16>
+struct Octet {
+    u32x4_any w[BF16 ? 1 : 2];
+};
+
 // `left` elements (8 or more: all) of the octet that starts at element `at`; the others are 0
 template <bool BF16>
-__device__ __forceinline__ void load_octet(const void *data, int64_t at, int left, float v[8])
+__device__ __forceinline__ Octet<BF16> fetch_octet(const void *data, int64_t at, int left)
 {
+    Octet<BF16> o = {};
     if constexpr (BF16) {
         const uint16_t *p = static_cast<const uint16_t *>(data) + at;
         if (left >= 8) {
-            const u32x4_any u = *reinterpret_cast<const u32x4_any *>(p);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                v[2 * i] = __uint_as_float(u[i] << 16);
-                v[2 * i + 1] = __uint_as_float(u[i] & 0xFFFF0000u);
-            }
+            o.w[0] = *reinterpret_cast<const u32x4_any *>(p);
         } else {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] = i < left ? bf16_bits_to_f32(p[i]) : 0.0f;
+            for (int i = 0; i < 8; ++i)
+                if (i < left) o.w[0][i >> 1] |= (uint32_t)p[i] << (16 * (i & 1));
         }
     } else {
         const float *p = static_cast<const float *>(data) + at;
         if (left >= 8) {
-            const u32x4_any a = *reinterpret_cast<const u32x4_any *>(p), b = *reinterpret_cast<const u32x4_any *>(p + 4);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                v[i] = __uint_as_float(a[i]);
-                v[4 + i] = __uint_as_float(b[i]);
-            }
+            o.w[0] = *reinterpret_cast<const u32x4_any *>(p);
+            o.w[1] = *reinterpret_cast<const u32x4_any *>(p + 4);
         } else {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] = i < left ? p[i] : 0.0f;
+            for (int i = 0; i < 8; ++i)
+                if (i < left) o.w[i >> 2][i & 3] = __float_as_uint(p[i]);
         }
     }
+    return o;
+}
+
+template <bool BF16>
+__device__ __forceinline__ void widen(const Octet<BF16> &o, float v[8])
+{
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        if constexpr (BF16) v[i] = __uint_as_float((i & 1) ? o.w[0][i >> 1] & 0xFFFF0000u : o.w[0][i >> 1] << 16);
+        else v[i] = __uint_as_float(o.w[i >> 2][i & 3]);
+    }
+}
+
+template <bool BF16>
+__device__ __forceinline__ void load_octet(const void *data, int64_t at, int left, float v[8])
+{
+    widen<BF16>(fetch_octet<BF16>(data, at, left), v);
 }
 
 // Writes the octet's first `left` elements; v becomes what has been written (rounded to bf16 where the elements are).
