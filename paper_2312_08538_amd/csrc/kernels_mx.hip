@@ -253,7 +253,7 @@ __device__ __forceinline__ void values(uint32_t c, uint32_t byte, float v[8])
 }
 
 // What a packed operand stands for: 16 rows a wave, 128 columns, four lanes a block.
-template <bool BF16>
+template <bool BF16, bool PAST>
 __global__ __launch_bounds__(kThreads) void k_mx_dequantise(MxDequantArgs a, int64_t pieces, int64_t groups)
 {
     const int64_t p = (int64_t)blockIdx.x * (kThreads / 64) + (threadIdx.x >> 6);
@@ -270,7 +270,7 @@ __global__ __launch_bounds__(kThreads) void k_mx_dequantise(MxDequantArgs a, int
         float v[8];
         values(c, byte, v);
         if (row < a.rows && col < a.cols)
-            store_octet<BF16>(a.out.data, row * a.out.pitch + col, octet_left(a.cols - col), v);
+            store_octet<BF16, PAST>(a.out.data, row * a.out.pitch + col, octet_left(a.cols - col), v);
     }
 }
 
@@ -306,8 +306,12 @@ void launch_mx_dequantise(const MxDequantArgs &a, bool bf16, hipStream_t st)
 {
     const int64_t pieces = (a.cols + 127) / 128, groups = (a.rows + 15) / 16;
     const dim3 grid((unsigned)((pieces * groups + 3) / 4));
+    // values that the dies' caches do not hold go past them: 8192 x 8192 in bf16, another buffer each time, 29 / 54 us
+    const bool past = a.rows * a.cols * (bf16 ? 2 : 4) > (int64_t)32 << 20;
     by_bool(bf16, [&](auto b) {
-        hipLaunchKernelGGL((k_mx_dequantise<decltype(b)::value>), grid, dim3(kThreads), 0, st, a, pieces, groups);
+        by_bool(past, [&](auto p) {
+            hipLaunchKernelGGL((k_mx_dequantise<decltype(b)::value, decltype(p)::value>), grid, dim3(kThreads), 0, st, a, pieces, groups);
+        });
     });
 }
 

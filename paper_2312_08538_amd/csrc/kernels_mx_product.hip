@@ -57,14 +57,6 @@ __device__ __forceinline__ void wait_loads()
     asm volatile("" ::: "memory");
 }
 
-// sixteen bytes to any address; PAST: past the caches
-template <bool PAST>
-__device__ __forceinline__ void store_16(void *p, u32x4_any v)
-{
-    if constexpr (PAST) __builtin_nontemporal_store(v, static_cast<u32x4_any *>(p));
-    else *static_cast<u32x4_any *>(p) = v;
-}
-
 // alpha v (+ beta c) to N neighbours of a row of C
 template <bool BF16, bool ADD, bool PAST, int N>
 __device__ __forceinline__ void store_row(const MxProductArgs &a, int64_t row, int64_t col, const float *v)

@@ -18,8 +18,13 @@ namespace conef {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kMostCols = 16384;        // the widest row that a workgroup holds in registers, eight octets a lane
-constexpr int kPartials = 512;          // workgroups of the backward pass, each with its sums for dgamma and dbeta
+constexpr int kForwardCols = 16384, kBackwardCols = 8192;       // the widest rows that a workgroup holds in registers
+constexpr int kForwardGroups = 2048;
+
+inline bool in_registers(int64_t cols, int most) { return cols >= 8 && cols <= most; }
+
+// threads of a workgroup in which G share a row
+constexpr int threads_of(int g) { return g > kThreads ? g : kThreads; }
 
 // ---------------------------------------------------------------- dropout
 template <bool BF16>
@@ -42,62 +47,90 @@ __global__ __launch_bounds__(kThreads) void k_dropout(DropoutArgs a, uint32_t oc
 }
 
 // ---------------------------------------------------------------- layer norm
-// Sums of N values over the G lanes that share a row, in every one of them.  G = 256: `red` holds 2 x 4 x N floats, used in
-// turn by consecutive calls (`turn`), so one barrier a call is enough.
+// Sums of N values over the G lanes that share a row, in every one of them.  G > 64 (a workgroup's threads): `red` holds 2 x G / 64 x N
+// floats, used in turn by consecutive calls (`turn`), so one barrier a call is enough.
 template <int G, int N>
 __device__ __forceinline__ void group_sum(float v[N], float *red, int &turn)
 {
 #pragma unroll
     for (int i = 0; i < N; ++i) v[i] = lanes_sum(v[i]);
-    if constexpr (G == kThreads) {
-        float *slot = red + turn * 4 * N;
+    if constexpr (G > 64) {
+        constexpr int W = G / 64;
+        float *slot = red + turn * W * N;
         turn ^= 1;
         if ((threadIdx.x & 63) == 0)
 #pragma unroll
             for (int i = 0; i < N; ++i) slot[(threadIdx.x >> 6) * N + i] = v[i];
         __syncthreads();
 #pragma unroll
-        for (int i = 0; i < N; ++i) v[i] = (slot[i] + slot[N + i]) + (slot[2 * N + i] + slot[3 * N + i]);
+        for (int i = 0; i < N; ++i) {
+            float s[W];
+#pragma unroll
+            for (int w = 0; w < W; ++w) s[w] = slot[w * N + i];
+#pragma unroll
+            for (int step = 1; step < W; step *= 2)
+#pragma unroll
+                for (int w = 0; w < W; w += 2 * step) s[w] += s[w + step];
+            v[i] = s[0];
+        }
     }
 }
 
-// G lanes hold a row, V octets each: octet v of lane t starts at column 8 (t + G v).
-template <bool BF16, int G, int V, bool FUSED>
-__global__ __launch_bounds__(kThreads) void k_norm_forward(NormArgs a)
+// a row's gamma or beta, laid out like the row
+template <int G, int V>
+__device__ __forceinline__ void load_columns(const float *p, int cols, int t, float out[V][8])
 {
-    __shared__ float red[8];
+    Octet<false> o[V] = {};
+#pragma unroll
+    for (int v = 0; v < V; ++v) begin_octet<false>(o[v], p, 8 * (t + G * v), cols - 8 * (t + G * v));
+#pragma unroll
+    for (int v = 0; v < V; ++v) finish_octet<false>(o[v], cols - 8 * (t + G * v), out[v]);
+}
+
+// G lanes hold a row, V octets each: octet v of lane t starts at column 8 (t + G v).  The next row's octets are on their way while a row is
+// worked on.
+template <bool BF16, int G, int V, bool FUSED>
+__global__ __launch_bounds__(threads_of(G)) void k_norm_forward(NormArgs a)
+{
+    constexpr int kRows = threads_of(G) / G;
+    __shared__ float red[G > 64 ? 2 * G / 64 : 1];
     int turn = 0;
     const int t = threadIdx.x % G;
     const float inv = 1.0f / (float)a.cols;
     const uint32_t per_row = (uint32_t)(a.cols + 7) >> 3;
-    float gamma[V][8], beta[V][8];
+    const int64_t stride = (int64_t)gridDim.x * kRows;
+    int64_t row = (int64_t)blockIdx.x * kRows + threadIdx.x / G;
+    Octet<BF16> x[V] = {}, r[FUSED ? V : 1] = {};
+    auto fetch = [&](int64_t from) {
 #pragma unroll
-    for (int v = 0; v < V; ++v) {
-        const int col = 8 * (t + G * v);
-        load_octet<false>(a.gamma, col, a.cols - col, gamma[v]);
-        load_octet<false>(a.beta, col, a.cols - col, beta[v]);
-    }
-    for (int64_t row = (int64_t)blockIdx.x * (kThreads / G) + threadIdx.x / G; row < a.rows; row += (int64_t)gridDim.x * (kThreads / G)) {
+        for (int v = 0; v < V; ++v) {
+            const int col = 8 * (t + G * v), left = from < a.rows ? a.cols - col : 0;
+            begin_octet<BF16>(x[v], a.x.data, from * a.x.pitch + col, left);
+            if (FUSED && a.residual.data) begin_octet<BF16>(r[v], a.residual.data, from * a.residual.pitch + col, left);
+        }
+    };
+    fetch(row);
+    float gamma[V][8], beta[V][8];
+    load_columns<G, V>(a.gamma, a.cols, t, gamma);
+    load_columns<G, V>(a.beta, a.cols, t, beta);
+    for (; row < a.rows; row += stride) {
         float z[V][8];
 #pragma unroll
         for (int v = 0; v < V; ++v) {
             const int col = 8 * (t + G * v);
-            load_octet<BF16>(a.x.data, row * a.x.pitch + col, a.cols - col, z[v]);
-        }
-        if constexpr (FUSED) {
-#pragma unroll
-            for (int v = 0; v < V; ++v) {
-                const int col = 8 * (t + G * v);
+            finish_octet<BF16>(x[v], a.cols - col, z[v]);
+            if constexpr (FUSED) {
                 if (a.drop) drop_octet(a.d, (uint32_t)row * per_row + (uint32_t)(t + G * v), z[v]);
                 if (a.residual.data) {
-                    float r[8];
-                    load_octet<BF16>(a.residual.data, row * a.residual.pitch + col, a.cols - col, r);
+                    float add[8];
+                    finish_octet<BF16>(r[v], a.cols - col, add);
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) z[v][i] = r[i] + z[v][i];
+                    for (int i = 0; i < 8; ++i) z[v][i] = add[i] + z[v][i];
                 }
                 store_octet<BF16>(a.z.data, row * a.z.pitch + col, a.cols - col, z[v]);
             }
         }
+        fetch(row + stride);
         float sum[1] = {0.0f};
 #pragma unroll
         for (int v = 0; v < V; ++v)
@@ -202,13 +235,12 @@ __device__ __forceinline__ void hat_and_a(const float z[8], const float dy[8], c
 
 // Adds dz_in, writes dz and, from the unrounded values, dx.
 template <bool BF16>
-__device__ __forceinline__ void finish_dz(const NormArgs &a, int64_t row, int64_t col, int left, uint32_t octet, float v[8])
+__device__ __forceinline__ void finish_dz(const NormArgs &a, int64_t row, int64_t col, int left, uint32_t octet, const float dz_in[8],
+                                          float v[8])
 {
     if (a.dz_in.data) {
-        float r[8];
-        load_octet<BF16>(a.dz_in.data, row * a.dz_in.pitch + col, left, r);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] += r[i];
+        for (int i = 0; i < 8; ++i) v[i] += dz_in[i];
     }
     if (a.dx.data) {
         float x[8];
@@ -221,60 +253,84 @@ __device__ __forceinline__ void finish_dz(const NormArgs &a, int64_t row, int64_
 }
 
 // Each workgroup takes every gridDim-th row (or 256 / G of them) and keeps its share of dgamma and dbeta in registers, since a lane
-// sees the same columns in every row; k_norm_columns adds the shares.
+// sees the same columns in every row; k_norm_columns adds the shares.  The next row's octets are on their way while a row is worked on.
 template <bool BF16, int G, int V>
-__global__ __launch_bounds__(kThreads) void k_norm_backward(NormArgs a)
+__global__ __launch_bounds__(threads_of(G)) void k_norm_backward(NormArgs a)
 {
-    constexpr int kRows = kThreads / G;
-    __shared__ float red[16];
-    __shared__ float share[G == kThreads ? 1 : 2 * 8 * G * V];
+    constexpr int kRows = threads_of(G) / G;
+    __shared__ float red[G > 64 ? 4 * G / 64 : 1];
+    __shared__ float share[G > 64 ? 1 : 2 * 8 * G * V];
     int turn = 0;
     const int t = threadIdx.x % G;
     const float inv = 1.0f / (float)a.cols;
     const uint32_t per_row = (uint32_t)(a.cols + 7) >> 3;
-    float gamma[V][8], dgamma[V][8] = {}, dbeta[V][8] = {};
-#pragma unroll
-    for (int v = 0; v < V; ++v) load_octet<false>(a.gamma, 8 * (t + G * v), a.cols - 8 * (t + G * v), gamma[v]);
-    for (int64_t row = (int64_t)blockIdx.x * kRows + threadIdx.x / G; row < a.rows; row += (int64_t)gridDim.x * kRows) {
-        float z[V][8], dy[V][8];
+    const int64_t stride = (int64_t)gridDim.x * kRows;
+    int64_t row = (int64_t)blockIdx.x * kRows + threadIdx.x / G;
+    Octet<BF16> z_next[V] = {}, dy_next[V] = {}, in_next[V] = {};
+    float mean_next = 0.0f, rstd_next = 0.0f;
+    auto fetch = [&](int64_t from) {
+        if (from < a.rows) {
+            mean_next = a.mean[from];
+            rstd_next = a.rstd[from];
+        }
 #pragma unroll
         for (int v = 0; v < V; ++v) {
-            const int col = 8 * (t + G * v);
-            load_octet<BF16>(a.z_in.data, row * a.z_in.pitch + col, a.cols - col, z[v]);
-            load_octet<BF16>(a.dy.data, row * a.dy.pitch + col, a.cols - col, dy[v]);
+            const int col = 8 * (t + G * v), left = from < a.rows ? a.cols - col : 0;
+            begin_octet<BF16>(z_next[v], a.z_in.data, from * a.z_in.pitch + col, left);
+            begin_octet<BF16>(dy_next[v], a.dy.data, from * a.dy.pitch + col, left);
+            if (a.dz_in.data) begin_octet<BF16>(in_next[v], a.dz_in.data, from * a.dz_in.pitch + col, left);
         }
-        const float mean = a.mean[row], rstd = a.rstd[row];
+    };
+    fetch(row);
+    float gamma[V][8], dgamma[V][8] = {}, dbeta[V][8] = {};
+    load_columns<G, V>(a.gamma, a.cols, t, gamma);
+    for (; row < a.rows; row += stride) {
+        Octet<BF16> z[V], dy[V], in[V];
+        const float mean = mean_next, rstd = rstd_next;
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            z[v] = z_next[v];
+            dy[v] = dy_next[v];
+            in[v] = in_next[v];
+        }
+        fetch(row + stride);
         float sums[2] = {0.0f, 0.0f};
 #pragma unroll
         for (int v = 0; v < V; ++v) {
-            float hat[8], w[8];
-            hat_and_a(z[v], dy[v], gamma[v], mean, rstd, hat, w);
+            float zv[8], dv[8], hat[8], w[8];
+            const int left = a.cols - 8 * (t + G * v);
+            finish_octet<BF16>(z[v], left, zv);
+            finish_octet<BF16>(dy[v], left, dv);
+            hat_and_a(zv, dv, gamma[v], mean, rstd, hat, w);
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 // (columns beyond the row's end have dy = gamma = 0)
                 sums[0] += w[i];
                 sums[1] = __builtin_fmaf(w[i], hat[i], sums[1]);
-                dgamma[v][i] = __builtin_fmaf(dy[v][i], hat[i], dgamma[v][i]);
-                dbeta[v][i] += dy[v][i];
+                dgamma[v][i] = __builtin_fmaf(dv[i], hat[i], dgamma[v][i]);
+                dbeta[v][i] += dv[i];
             }
         }
-        group_sum<G, 2>(sums, red, turn);
-        const float m0 = sums[0] * inv, m1 = sums[1] * inv;
         if (a.dz.data || a.dx.data) {
+            group_sum<G, 2>(sums, red, turn);
+            const float m0 = sums[0] * inv, m1 = sums[1] * inv;
 #pragma unroll
             for (int v = 0; v < V; ++v) {
-                const int col = 8 * (t + G * v);
-                float hat[8], w[8];
-                hat_and_a(z[v], dy[v], gamma[v], mean, rstd, hat, w);
+                float zv[8], dv[8], hat[8], w[8], add[8];
+                const int col = 8 * (t + G * v), left = a.cols - col;
+                finish_octet<BF16>(z[v], left, zv);
+                finish_octet<BF16>(dy[v], left, dv);
+                hat_and_a(zv, dv, gamma[v], mean, rstd, hat, w);
 #pragma unroll
                 for (int i = 0; i < 8; ++i) w[i] = rstd * ((w[i] - m0) - hat[i] * m1);
-                finish_dz<BF16>(a, row, col, a.cols - col, (uint32_t)row * per_row + (uint32_t)(t + G * v), w);
+                if (a.dz_in.data) finish_octet<BF16>(in[v], left, add);
+                finish_dz<BF16>(a, row, col, left, (uint32_t)row * per_row + (uint32_t)(t + G * v), add, w);
             }
         }
     }
     if (!a.partials) return;
     float *out = a.partials + (int64_t)blockIdx.x * 2 * a.cols;
-    if constexpr (G == kThreads) {
+    if constexpr (G > 64) {
 #pragma unroll
         for (int v = 0; v < V; ++v) {
             const int col = 8 * (t + G * v);
@@ -289,15 +345,17 @@ __global__ __launch_bounds__(kThreads) void k_norm_backward(NormArgs a)
                 for (int v = 0; v < V; ++v)
 #pragma unroll
                     for (int i = 0; i < 8; ++i) {
-                        float *p = share + 8 * (t + G * v) + i, *q = p + 8 * G * V;
+                        // (a row's octets: element i of lane t in place i G + t, so that neighbours lie in neighbouring banks)
+                        float *p = share + (v * 8 + i) * G + t, *q = p + 8 * G * V;
                         *p = g ? *p + dgamma[v][i] : dgamma[v][i];
                         *q = g ? *q + dbeta[v][i] : dbeta[v][i];
                     }
             __syncthreads();
         }
         for (int c = threadIdx.x; c < a.cols; c += kThreads) {
-            out[c] = share[c];
-            out[a.cols + c] = share[8 * G * V + c];
+            const int octet = c >> 3, at = ((octet / G) * 8 + (c & 7)) * G + octet % G;
+            out[c] = share[at];
+            out[a.cols + c] = share[8 * G * V + at];
         }
     }
 }
@@ -335,7 +393,9 @@ __global__ __launch_bounds__(kThreads) void k_norm_backward_long(NormArgs a)
             hat_and_a(z, dy, gamma, mean, rstd, hat, w);
 #pragma unroll
             for (int i = 0; i < 8; ++i) w[i] = rstd * ((w[i] - m0) - hat[i] * m1);
-            finish_dz<BF16>(a, row, col, left, (uint32_t)row * per_row + (uint32_t)(col >> 3), w);
+            float in[8];
+            if (a.dz_in.data) load_octet<BF16>(a.dz_in.data, row * a.dz_in.pitch + col, left, in);
+            finish_dz<BF16>(a, row, col, left, (uint32_t)row * per_row + (uint32_t)(col >> 3), in, w);
         }
     }
 }
@@ -371,8 +431,21 @@ __global__ __launch_bounds__(1024) void k_norm_columns(const float *partials, in
     const int lane = threadIdx.x & 63, part = threadIdx.x >> 6;
     const int64_t c = (int64_t)blockIdx.x * 64 + lane, n = 2 * (int64_t)cols;
     double s = 0.0;
-    if (c < n)
-        for (int p = part; p < parts; p += 16) s += (double)partials[p * n + c];
+    if (c < n) {
+        int p = part;
+        for (; p + 112 < parts; p += 128) {                 // eight loads on their way at a time
+            float v[8];
+#pragma unroll
+            for (int u = 0; u < 8; ++u) v[u] = partials[(p + 16 * u) * n + c];
+#pragma unroll
+            for (int u = 0; u < 8; ++u) s += (double)v[u];
+        }
+        float v[8];
+#pragma unroll
+        for (int u = 0; u < 8; ++u) v[u] = p + 16 * u < parts ? partials[(p + 16 * u) * n + c] : 0.0f;
+#pragma unroll
+        for (int u = 0; u < 8; ++u) s += (double)v[u];
+    }
     red[part][lane] = s;
     __syncthreads();
     if (part || c >= n) return;
@@ -382,16 +455,32 @@ __global__ __launch_bounds__(1024) void k_norm_columns(const float *partials, in
     if (out) out[c < cols ? c : c - cols] = (float)s;
 }
 
+// Lanes to a row and octets a lane: at most two, which registers hold together with the next row on its way.  A wave to a row needs no barrier, but
+// four octets a lane (2048 columns) take 256 registers: the backward pass of 16384 x 2048 in bf16 then takes 86 us, with a workgroup to
+// a row 75.
 template <typename F>
-void by_width(int cols, F &&go)
+void by_width(int64_t cols, F &&go)
 {
     using std::integral_constant;
-    if (cols <= 512) go(integral_constant<int, 64>{}, integral_constant<int, 1>{});
-    else if (cols <= 1024) go(integral_constant<int, 64>{}, integral_constant<int, 2>{});
-    else if (cols <= 2048) go(integral_constant<int, 256>{}, integral_constant<int, 1>{});
-    else if (cols <= 4096) go(integral_constant<int, 256>{}, integral_constant<int, 2>{});
-    else if (cols <= 8192) go(integral_constant<int, 256>{}, integral_constant<int, 4>{});
-    else go(integral_constant<int, 256>{}, integral_constant<int, 8>{});
+    typedef integral_constant<int, 1> One;
+    typedef integral_constant<int, 2> Two;
+    typedef integral_constant<int, 64> Wave;
+    typedef integral_constant<int, 256> Group;
+    if (cols <= 512) go(Wave{}, One{});
+    else if (cols <= 1024) go(Wave{}, Two{});
+    else if (cols <= 2048) go(Group{}, One{});
+    else if (cols <= 4096) go(Group{}, Two{});
+    else if (cols <= 8192) go(integral_constant<int, 512>{}, Two{});
+    else go(integral_constant<int, 1024>{}, Two{});
+}
+
+// Workgroups of the backward pass: as many as the card holds at a time (four, two or one a CU, by their registers).
+int64_t most_parts(int64_t cols)
+{
+    int64_t n = 0;
+    if (!in_registers(cols, kBackwardCols)) return 512;
+    by_width(cols, [&](auto g, auto v) { n = decltype(g)::value > kThreads ? 256 : decltype(v)::value == 1 ? 1024 : 512; });
+    return n;
 }
 
 template <typename F>
@@ -414,15 +503,16 @@ void launch_norm_forward(const NormArgs &a, bool bf16, hipStream_t st)
 {
     by_bool(bf16, [&](auto b) {
         by_bool(a.z.data != nullptr, [&](auto fused) {
-            if (a.cols > kMostCols) {
+            if (!in_registers(a.cols, kForwardCols)) {
                 const dim3 grid((unsigned)std::min<int64_t>(a.rows, 1 << 20));
                 hipLaunchKernelGGL((k_norm_forward_long<decltype(b)::value, decltype(fused)::value>), grid, dim3(kThreads), 0, st, a);
                 return;
             }
             by_width(a.cols, [&](auto g, auto v) {
-                const int64_t per = kThreads / decltype(g)::value, groups = (a.rows + per - 1) / per;
-                hipLaunchKernelGGL((k_norm_forward<decltype(b)::value, decltype(g)::value, decltype(v)::value, decltype(fused)::value>),
-                                   dim3((unsigned)std::min<int64_t>(groups, 2048)), dim3(kThreads), 0, st, a);
+                constexpr int G = decltype(g)::value;
+                const int64_t per = threads_of(G) / G, groups = (a.rows + per - 1) / per;
+                hipLaunchKernelGGL((k_norm_forward<decltype(b)::value, G, decltype(v)::value, decltype(fused)::value>),
+                                   dim3((unsigned)std::min<int64_t>(groups, kForwardGroups)), dim3(threads_of(G)), 0, st, a);
             });
         });
     });
@@ -430,8 +520,7 @@ void launch_norm_forward(const NormArgs &a, bool bf16, hipStream_t st)
 
 int64_t norm_partials(int64_t rows, int64_t cols)
 {
-    (void)cols;
-    return std::min<int64_t>(rows, kPartials);
+    return std::min(rows, most_parts(cols));
 }
 
 void launch_norm_backward(const NormArgs &a, bool bf16, hipStream_t st)
@@ -439,7 +528,7 @@ void launch_norm_backward(const NormArgs &a, bool bf16, hipStream_t st)
     const int64_t parts = norm_partials(a.rows, a.cols);
     int used = (int)parts;
     if (parts > 0) by_bool(bf16, [&](auto b) {
-        if (a.cols > kMostCols) {
+        if (!in_registers(a.cols, kBackwardCols)) {
             // (first: dz may take the place of dy or z)
             if (a.partials)
                 hipLaunchKernelGGL((k_norm_column_parts<decltype(b)::value>), dim3((unsigned)((a.cols + 2047) / 2048), (unsigned)parts),
@@ -450,10 +539,10 @@ void launch_norm_backward(const NormArgs &a, bool bf16, hipStream_t st)
             return;
         }
         by_width(a.cols, [&](auto g, auto v) {
-            const int64_t per = kThreads / decltype(g)::value;
+            constexpr int G = decltype(g)::value <= 512 ? decltype(g)::value : 512;         // (wider rows went the other way)
+            const int64_t per = threads_of(G) / G;
             used = (int)std::min<int64_t>((a.rows + per - 1) / per, parts);
-            hipLaunchKernelGGL((k_norm_backward<decltype(b)::value, decltype(g)::value, decltype(v)::value>), dim3((unsigned)used),
-                               dim3(kThreads), 0, st, a);
+            hipLaunchKernelGGL((k_norm_backward<decltype(b)::value, G, decltype(v)::value>), dim3((unsigned)used), dim3(threads_of(G)), 0, st, a);
         });
     });
     if (a.dgamma || a.dbeta)

@@ -27,7 +27,8 @@ struct Octet {
     u32x4_any w[BF16 ? 1 : 2];
 };
 
-// `left` elements (8 or more: all) of the octet that starts at element `at`; the others are 0
+// `left` elements (8 or more: all) of the octet that starts at element `at`; the others are 0.  Of an octet that its row does not fill
+// every element is loaded on its own, all of them at once: those beyond the end are the last one again, and not taken.
 template <bool BF16>
 __device__ __forceinline__ Octet<BF16> fetch_octet(const void *data, int64_t at, int left)
 {
@@ -36,23 +37,69 @@ __device__ __forceinline__ Octet<BF16> fetch_octet(const void *data, int64_t at,
         const uint16_t *p = static_cast<const uint16_t *>(data) + at;
         if (left >= 8) {
             o.w[0] = *reinterpret_cast<const u32x4_any *>(p);
-        } else {
+        } else if (left > 0) {
+            uint32_t e[8];
 #pragma unroll
-            for (int i = 0; i < 8; ++i)
-                if (i < left) o.w[0][i >> 1] |= (uint32_t)p[i] << (16 * (i & 1));
+            for (int i = 0; i < 8; ++i) e[i] = p[i < left ? i : left - 1];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) o.w[0][i >> 1] |= i < left ? e[i] << (16 * (i & 1)) : 0u;
         }
     } else {
         const float *p = static_cast<const float *>(data) + at;
         if (left >= 8) {
             o.w[0] = *reinterpret_cast<const u32x4_any *>(p);
             o.w[1] = *reinterpret_cast<const u32x4_any *>(p + 4);
-        } else {
+        } else if (left > 0) {
+            float e[8];
 #pragma unroll
-            for (int i = 0; i < 8; ++i)
-                if (i < left) o.w[i >> 2][i & 3] = __float_as_uint(p[i]);
+            for (int i = 0; i < 8; ++i) e[i] = p[i < left ? i : left - 1];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) o.w[i >> 2][i & 3] = i < left ? __float_as_uint(e[i]) : 0u;
         }
     }
     return o;
+}
+
+// The same for rows of 8 columns at least, in two steps, so that loads can be under way while other work is done: an octet that its row does not
+// fill is fetched as what lies in the row's last sixteen (thirty-two) bytes, and moved down when it is used.
+template <bool BF16>
+__device__ __forceinline__ void begin_octet(Octet<BF16> &o, const void *data, int64_t at, int left)
+{
+    if (left <= 0) return;
+    at -= left < 8 ? 8 - left : 0;
+    if constexpr (BF16) {
+        o.w[0] = *reinterpret_cast<const u32x4_any *>(static_cast<const uint16_t *>(data) + at);
+    } else {
+        const float *p = static_cast<const float *>(data) + at;
+        o.w[0] = *reinterpret_cast<const u32x4_any *>(p);
+        o.w[1] = *reinterpret_cast<const u32x4_any *>(p + 4);
+    }
+}
+
+// its elements; those beyond the row's end are 0
+template <bool BF16>
+__device__ __forceinline__ void finish_octet(const Octet<BF16> &o, int left, float v[8])
+{
+    constexpr int N = BF16 ? 4 : 8;
+    uint32_t w[N];
+#pragma unroll
+    for (int i = 0; i < N; ++i) w[i] = o.w[i >> 2][i & 3];
+    if (left < 8) {
+        const int s = left > 0 ? 8 - left : 8, words = BF16 ? s >> 1 : s;
+#pragma unroll
+        for (int step = N; step; step /= 2)
+#pragma unroll
+            for (int i = 0; i < N; ++i) w[i] = words & step ? (i + step < N ? w[i + step] : 0u) : w[i];
+        if constexpr (BF16) {
+#pragma unroll
+            for (int i = 0; i < N; ++i) w[i] = s & 1 ? (w[i] >> 16 | (i + 1 < N ? w[i + 1] << 16 : 0u)) : w[i];
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        if constexpr (BF16) v[i] = __uint_as_float((i & 1) ? w[i >> 1] & 0xFFFF0000u : w[i >> 1] << 16);
+        else v[i] = __uint_as_float(w[i]);
+    }
 }
 
 template <bool BF16>
@@ -71,8 +118,16 @@ __device__ __forceinline__ void load_octet(const void *data, int64_t at, int lef
     widen<BF16>(fetch_octet<BF16>(data, at, left), v);
 }
 
+// sixteen bytes to any address; PAST: past the caches
+template <bool PAST>
+__device__ __forceinline__ void store_16(void *p, u32x4_any v)
+{
+    if constexpr (PAST) __builtin_nontemporal_store(v, static_cast<u32x4_any *>(p));
+    else *static_cast<u32x4_any *>(p) = v;
+}
+
 // Writes the octet's first `left` elements; v becomes what has been written (rounded to bf16 where the elements are).
-template <bool BF16>
+template <bool BF16, bool PAST = false>
 __device__ __forceinline__ void store_octet(void *data, int64_t at, int left, float v[8])
 {
     if constexpr (BF16) {
@@ -85,27 +140,36 @@ __device__ __forceinline__ void store_octet(void *data, int64_t at, int left, fl
             v[2 * i + 1] = __uint_as_float(u[i] & 0xFFFF0000u);
         }
         if (left >= 8) {
-            *reinterpret_cast<u32x4_any *>(p) = u;
-        } else {
-#pragma unroll
-            for (int i = 0; i < 8; ++i)
-                if (i < left) p[i] = (uint16_t)(u[i >> 1] >> (16 * (i & 1)));
+            store_16<PAST>(p, u);
+        } else if (left > 0) {
+            // four, two, one
+            typedef uint32_t u32x2_any __attribute__((ext_vector_type(2), aligned(2)));
+            typedef uint32_t u32_any __attribute__((aligned(2)));
+            if (left & 4) *reinterpret_cast<u32x2_any *>(p) = u32x2_any{u[0], u[1]};
+            const uint32_t a = left & 4 ? u[2] : u[0], b = left & 4 ? u[3] : u[1];
+            p += left & 4;
+            if (left & 2) *reinterpret_cast<u32_any *>(p) = a;
+            if (left & 1) p[left & 2] = (uint16_t)(left & 2 ? b : a);
         }
     } else {
         float *p = static_cast<float *>(data) + at;
+        u32x4_any a, b;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            a[i] = __float_as_uint(v[i]);
+            b[i] = __float_as_uint(v[4 + i]);
+        }
         if (left >= 8) {
-            u32x4_any a, b;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                a[i] = __float_as_uint(v[i]);
-                b[i] = __float_as_uint(v[4 + i]);
-            }
-            *reinterpret_cast<u32x4_any *>(p) = a;
-            *reinterpret_cast<u32x4_any *>(p + 4) = b;
-        } else {
-#pragma unroll
-            for (int i = 0; i < 8; ++i)
-                if (i < left) p[i] = v[i];
+            store_16<PAST>(p, a);
+            store_16<PAST>(p + 4, b);
+        } else if (left > 0) {
+            typedef uint32_t u32x2_any __attribute__((ext_vector_type(2), aligned(4)));
+            if (left & 4) store_16<false>(p, a);
+            // (of the vectors, not of v: a choice between places of v would put v into memory)
+            const uint32_t c = left & 4 ? b[0] : a[0], d = left & 4 ? b[1] : a[1], e = left & 4 ? b[2] : a[2];
+            p += left & 4;
+            if (left & 2) *reinterpret_cast<u32x2_any *>(p) = u32x2_any{c, d};
+            if (left & 1) p[left & 2] = __uint_as_float(left & 2 ? e : c);
         }
     }
 }
