@@ -486,8 +486,8 @@ int conef_norm_backward(const conef_drop *drop, int64_t rows, int64_t cols, int 
  * A packed operand holds rows in 64s and columns in 128s, the rest filled with zeros; with P = ceil(cols / 128), element (i, j) is in
  *   code byte   ((i / 16) P + j / 128) 1024 + (j / 32 % 4) 256 + (i % 16) 16 + (j % 32) / 2, the low four bits for even j
  *   scale byte  ((i / 64) P + j / 128)  256 + (j / 32 % 4)  64 + (i % 16) 4 + (i % 64) / 16
- * conef_mx_sizes       bytes of the two buffers (either pointer may be null), 16-byte aligned; 0 <= rows, cols here and below, and
- *                      also cols ceil(rows / 8) < 2^32
+ * conef_mx_sizes       bytes of the two buffers (either pointer may be null), 16-byte aligned; 0 <= rows, cols < 2^30 here and
+ *                      below, and also cols ceil(rows / 8) < 2^32
  * conef_mx_quantise    x by rows into codes / scales, and by columns (the rows of x's transpose) into codes_t / scales_t, sized for
  *                      cols x rows; either pair may be null.  seed, site and step matter to stochastic rounding only.
  * conef_mx_dequantise  the values of a packed operand, exactly */

@@ -70,10 +70,10 @@ inline int64_t round_up(int64_t v, int64_t to) { return (v + to - 1) / to * to; 
 
 bool bad_packed(const void *codes, const void *scales) { return !codes || !scales || misaligned(codes, 16) || misaligned(scales, 16); }
 
-// sides of a packed operand: both turns of it have to be countable
+// sides of a packed operand: below 2^30, and both turns of it have to be countable
 bool bad_sides(int64_t rows, int64_t cols)
 {
-    return rows < 0 || cols < 0 || rows >= kMostSide || cols >= kMostSide || rows * ((cols + 7) / 8) >= (int64_t)1 << 32 ||
+    return rows < 0 || cols < 0 || rows >= kMostSide / 2 || cols >= kMostSide / 2 || rows * ((cols + 7) / 8) >= (int64_t)1 << 32 ||
            cols * ((rows + 7) / 8) >= (int64_t)1 << 32;
 }
 
