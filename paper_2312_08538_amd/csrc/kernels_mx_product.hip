@@ -242,11 +242,68 @@ __global__ __launch_bounds__(64 * WM * WN, WAVES) void k_mx_product(MxProductArg
         a.c.data = a.partials + (int64_t)part * a.m * a.n;
         a.c.pitch = a.n;
     }
+    if constexpr (ADD) {
 #pragma unroll
-    for (int i = 0; i < TM; ++i) {
-        const int64_t row = m0 + (wm * TM + i) * 16 + (lane & 15);
+        for (int i = 0; i < TM; ++i) {
+            const int64_t row = m0 + (wm * TM + i) * 16 + (lane & 15);
 #pragma unroll
-        for (int j = 0; j < TN; j += 2) store_pair<BF16, ADD, PAST>(a, row, n0 + (wn * TN + j) * 16, lane >> 4, acc[j][i], acc[j + 1][i]);
+            for (int j = 0; j < TN; j += 2) store_pair<BF16, ADD, PAST>(a, row, n0 + (wn * TN + j) * 16, lane >> 4, acc[j][i], acc[j + 1][i]);
+        }
+    } else {
+        // By way of LDS, as many rows at a time as fit, so that a store writes whole rows of the tile.
+        constexpr int kSize = BF16 ? 2 : 4, kPitch = kN * kSize + 16, kFit = STAGES * kStage / kPitch;
+        constexpr int kTurns = kM <= kFit ? 1 : kM / 2 <= kFit ? 2 : 4, kTiles = TM / kTurns, kRows = kM / kTurns, kPieces = kN * kSize / 16;
+        static_assert(kRows <= kFit && TM % kTurns == 0 && kRows * kPieces % (64 * kWaves) == 0, "");
+#pragma unroll
+        for (int turn = 0; turn < kTurns; ++turn) {
+            __syncthreads();
+#pragma unroll
+            for (int i = 0; i < kTiles; ++i) {
+                uint8_t *to = lds + ((wm * kTiles + i) * 16 + (lane & 15)) * kPitch + wn * TN * 16 * kSize;
+#pragma unroll
+                for (int j = 0; j < TN; j += 2) {
+                    const f32x4 u = acc[j][turn * kTiles + i], v = acc[j + 1][turn * kTiles + i];
+                    if constexpr (BF16) {
+                        uint32_t w[4];
+#pragma unroll
+                        for (int e = 0; e < 2; ++e) {
+                            auto x = __builtin_amdgcn_permlane16_swap(pack_bf16(a.alpha * u[2 * e], a.alpha * u[2 * e + 1]),
+                                                                      pack_bf16(a.alpha * v[2 * e], a.alpha * v[2 * e + 1]), false, false);
+                            w[e] = x[0];
+                            w[2 + e] = x[1];
+                        }
+                        const int col = j * 16 + 16 * ((lane >> 4) & 1) + 8 * (lane >> 5);
+                        *reinterpret_cast<uint4 *>(to + col * 2) = make_uint4(w[0], w[1], w[2], w[3]);
+                    } else {
+                        const int col = j * 16 + 4 * (lane >> 4);
+                        *reinterpret_cast<float4 *>(to + col * 4) = make_float4(a.alpha * u[0], a.alpha * u[1], a.alpha * u[2], a.alpha * u[3]);
+                        *reinterpret_cast<float4 *>(to + col * 4 + 64) = make_float4(a.alpha * v[0], a.alpha * v[1], a.alpha * v[2], a.alpha * v[3]);
+                    }
+                }
+            }
+            __syncthreads();
+#pragma unroll 4
+            for (int s = 0; s < kRows * kPieces / (64 * kWaves); ++s) {
+                const int at = s * 64 * kWaves + threadIdx.x, r = at / kPieces, c = at % kPieces;
+                const int64_t row = m0 + r / (kTiles * 16) * (TM * 16) + turn * kTiles * 16 + r % (kTiles * 16), col = n0 + c * (16 / kSize);
+                if (row >= a.m || col >= a.n) continue;
+                const uint4 w = *reinterpret_cast<const uint4 *>(lds + r * kPitch + c * 16);
+                uint8_t *to = static_cast<uint8_t *>(a.c.data) + (row * a.c.pitch + col) * kSize;
+                if (col + 16 / kSize <= a.n) {
+                    store_16<PAST>(to, u32x4_any{w.x, w.y, w.z, w.w});
+                } else if constexpr (BF16) {
+                    const uint32_t e[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+                    for (int i = 0; i < 8; ++i)
+                        if (col + i < a.n) reinterpret_cast<uint16_t *>(to)[i] = (uint16_t)(e[i >> 1] >> (16 * (i & 1)));
+                } else {
+                    const uint32_t e[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        if (col + i < a.n) reinterpret_cast<uint32_t *>(to)[i] = e[i];
+                }
+            }
+        }
     }
 }
 
@@ -330,20 +387,22 @@ struct Choice {
 
 constexpr int kCus = 256;
 
-// Which kernel.  us of a call in a graph (bf16 C), kernel / the next best one:
+// Which kernel, and whether C goes past the caches.  us of a call (bf16 C unless said otherwise), the one taken / the next best:
 //   rows (m <= 64)   8 x 8192 x 2048 2.7 / 4.8 tiny, 1 x 50304 x 2048 11.3 / 11.8 small, 64 x 2048 x 8192 5.4 / 9.8 tiny in 4 parts
-//   large, 256 x 256, eight waves: the fewest reads from LDS, but a CU holds one workgroup, which begins and ends alone:
-//                    8192 x 8192 x 8192 242 / 257 wide, 8192 x 2048 x 8192 68 / 72 wide, but 4096 x 50304 x 2048 263 / 236 wide
-//   wide, 256 x 128, two workgroups a CU:  8192 x 8192 x 2048 81 / 83, 4096 x 50304 x 2048 236 / 247 small, but 1024 x 50304 x 768 41 / 39 small
-//   small, 128 x 128, three a CU:  2048 x 2048 x 16384 43 / 56 in 2 parts, 60 tiny, 65 wide; 512 x 8192 x 2048 9.4 / 11.8 tiny
+//   large, 256 x 256, eight waves: the fewest reads from LDS, but a CU holds one workgroup, which begins and ends alone; for long sums:
+//                    8192 x 8192 x 8192 242 / 257 wide, 8192 x 2048 x 8192 66 / 71 wide; 4096 x 50304 x 2048 249 wide / 250
+//   wide, 256 x 128, two workgroups a CU:  4096 x 50304 x 2048 249 / 280 small; 8192 x 32768 x 1024 184 small / 190
+//   small, 128 x 128, three a CU:  2048 x 50304 x 768 65 / 69 wide, 2048 x 2048 x 16384 43 / 56 in 2 parts, 60 tiny; 512 x 8192 x 2048 9.4 / 11.8 tiny
 //   tiny, 64 x 64, where small ones do not reach every CU:  1024 x 1024 x 1024 4.0 / 5.6, 16384 x 16 x 4096 8.4 / 11.7, 128 x 4096 x 1024 3.8 / 5.5
 // The long axis in parts, added up by a launch of its own: 256 x 256 x 8192 9.4 in 4 parts / 12.6, but 200 x 1024 x 4096 8.7 in 2 / 7.6.
+// Past the caches what those of the dies do not hold: 8192 x 32768 x 1024 184 / 270, 8192 x 8192 x 2048 in fp32 88 / 97, 4096 x 8192 x 2048 42 / 43;
+// large tiles only what the card's last cache does not hold either: 4096 x 50304 x 2048 250 / 292, but 8192 x 8192 x 2048 94 / 88.
 Choice choose(int64_t m, int64_t n, int64_t k)
 {
     const int64_t pieces = std::max<int64_t>((k + 127) / 128, 1);
     auto tiles = [&](int64_t tm, int64_t tn) { return ((m + tm - 1) / tm) * ((n + tn - 1) / tn); };
     if (m <= 64) return {kRows, 1, (int)pieces};
-    if (tiles(256, 256) >= 192 && pieces >= 12) return {pieces >= 48 ? kLarge : kWide, 1, (int)pieces};
+    if (tiles(256, 256) >= 192 && pieces >= 12) return {pieces >= 32 ? kLarge : kWide, 1, (int)pieces};
     if (tiles(128, 128) >= 200) return {kSmall, 1, (int)pieces};
     const int64_t parts = pieces < 64 ? 1 : std::max<int64_t>(std::min<int64_t>(kCus / tiles(64, 64), pieces / 16), 1);
     const int64_t per = (pieces + parts - 1) / parts;
@@ -399,8 +458,7 @@ void launch_mx_product(const MxProductArgs &a, bool bf16, hipStream_t st)
         p.alpha = 1.0f;                     // (beta is for the launch that adds the parts)
         launch_tiles<false, false, false, 2, 2, 2, 2, 4, 4>(p, c, st);
     }
-    // a C larger than the card's last cache goes past the caches: 4096 x 50304 in bf16 236 / 290 us, but 8192 x 8192 85 / 80
-    const bool past = a.m * a.n * (bf16 ? 2 : 4) > (int64_t)256 << 20;
+    const bool past = a.m * a.n * (bf16 ? 2 : 4) > (int64_t)(c.tiles == kLarge ? 256 : 32) << 20;
     by_bool(bf16, [&](auto b) {
         by_bool(a.beta != 0.0f, [&](auto add) {
             constexpr bool B = decltype(b)::value, ADD = decltype(add)::value;
@@ -412,12 +470,12 @@ void launch_mx_product(const MxProductArgs &a, bool bf16, hipStream_t st)
                                    fours);
             } else if (c.tiles == kTiny) {
                 launch_tiles<B, ADD, false, 2, 2, 2, 2, 4, 4>(a, c, st);
-            } else if (c.tiles == kSmall) {
-                launch_tiles<B, ADD, false, 2, 2, 4, 4, 3, 3>(a, c, st);
             } else {
                 by_bool(past, [&](auto p) {
-                    if (c.tiles == kWide) launch_tiles<B, ADD, decltype(p)::value, 2, 2, 8, 4, 3, 2>(a, c, st);
-                    else launch_tiles<B, ADD, decltype(p)::value, 2, 4, 8, 4, 4, 2>(a, c, st);
+                    constexpr bool PAST = decltype(p)::value;
+                    if (c.tiles == kSmall) launch_tiles<B, ADD, PAST, 2, 2, 4, 4, 3, 3>(a, c, st);
+                    else if (c.tiles == kWide) launch_tiles<B, ADD, PAST, 2, 2, 8, 4, 3, 2>(a, c, st);
+                    else launch_tiles<B, ADD, PAST, 2, 4, 8, 4, 4, 2>(a, c, st);
                 });
             }
         });
