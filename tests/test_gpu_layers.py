@@ -516,3 +516,96 @@ def test_a_captured_step_replays_to_the_eager_results(env, rows, cols):
         torch.cuda.synchronize()
         for k in want:
             assert torch.equal(out[k], want[k]), k
+
+
+# ---------------------------------------------------------------------------------------------- more than 2^31 elements
+def test_elements_beyond_31_bits(env):
+    """The last rows of matrices of 2.2e9 elements (everything before them zero): dropout, norm, quantisation, product."""
+    torch, B = env
+    rows, cols, tail = 66001, 33336, 3
+    assert rows * cols > 2 ** 31 and (rows - tail) * cols > 2 ** 31
+    st = B.Model.stream_handle()
+    x = torch.zeros(rows, cols, dtype=torch.bfloat16, device="cuda:0")
+    last = R.bf16(rng_of(31).standard_normal((tail, cols)).astype(np.float32))
+    x[-tail:] = torch.from_numpy(last).cuda()
+    y = torch.ones_like(x)
+    B.conef_dropout_forward(B.conef_drop(p=0.25, site=0, seed=SEED, step=STEP), x, None, y, st)
+    per = cols // 8
+    # draws of the last rows alone: octets from (rows - tail) per on
+    t = int(np.floor(0.25 * 65536 + 0.5))
+    u = np.array([[R.philox(((rows - tail + i) * per + o, R.DROP, STEP & 0xFFFFFFFF, STEP >> 32), (SEED & 0xFFFFFFFF, SEED >> 32)) for o in range(0, per, 97)]
+                  for i in range(tail)], dtype=np.uint64)
+    halves = np.stack([u & np.uint64(0xFFFF), u >> np.uint64(16)], -1).reshape(tail, -1, 8).astype(np.int64)
+    octets = last.reshape(tail, per, 8)[:, ::97]
+    want = R.bf16(np.where(halves >= t, octets * np.float32(65536.0 / (65536 - t)), np.float32(0)))
+    same_bits(y[-tail:].float().cpu().numpy().reshape(tail, per, 8)[:, ::97], want)
+    assert not bool(y[:-tail].any())
+
+    gamma, beta = torch.ones(cols, device="cuda:0"), torch.full((cols,), 0.5, device="cuda:0")
+    B.conef_norm_forward(None, 1e-5, x, None, gamma, beta, None, y, None, None, st)
+    ty, _, _ = y_tolerance(last.astype(np.float64), np.ones(cols), np.full(cols, 0.5), 1e-5, True)
+    assert (np.abs(y[-tail:].float().cpu().numpy() - R.norm(last, 1.0, 0.5, 1e-5)[0]) <= ty).all()
+    assert bool((y[:-tail] == 0.5).all())
+    del y
+
+    p = B.mx_alloc(rows, cols)
+    B.conef_mx_quantise(x, B.MX_NEAREST, 0, 0, 0, p, None, st)
+    del x
+    code = R.mx_encode(last)
+    n, k = 48, cols
+    b = R.mx_encode(rng_of(32).standard_normal((n, k)).astype(np.float32))
+    c = torch.full((rows, n), 7.0, device="cuda:0")
+    B.conef_mx_product(p, on_gpu(torch, b), k, 1.0, 0.0, c, torch.empty(B.conef_mx_product_workspace(rows, n, k), dtype=torch.uint8, device="cuda:0"), st)
+    A, W = R.mx_decode(*code), R.mx_decode(*b)
+    assert (np.abs(c[-tail:].cpu().numpy() - A @ W.T) <= product_tolerance(A, W, k)).all()
+    assert not bool(c[:-tail].any())
+    del p, c
+
+    m, n, k = 66001, 33336, 96
+    a, b = R.mx_encode(rng_of(33).standard_normal((tail, k)).astype(np.float32)), R.mx_encode(rng_of(34).standard_normal((n, k)).astype(np.float32))
+    codes, scales = np.zeros((m, k), np.uint8), np.zeros((m, k // 32), np.uint8)
+    codes[-tail:], scales[-tail:] = a
+    c = torch.full((m, n), 7.0, dtype=torch.bfloat16, device="cuda:0")
+    B.conef_mx_product(on_gpu(torch, (codes, scales)), on_gpu(torch, b), k, 1.0, 0.0, c, None, st)
+    A, W = R.mx_decode(*a), R.mx_decode(*b)
+    want = A @ W.T
+    assert (np.abs(c[-tail:].float().cpu().numpy() - want) <= product_tolerance(A, W, k) + np.abs(want) * R.U16 * 1.01).all()
+    assert not bool(c[:-tail].any())
+
+
+def test_every_operator_on_a_stream_of_its_own(env):
+    """Inputs made on one stream, the calls on another that waits for it: the same bits as on one stream."""
+    torch, B = env
+    rows, cols = 300, 1000
+    g, x, gamma, beta = norm_inputs(rows, cols, True, 8)
+    d = B.conef_drop(p=0.3, site=3, seed=SEED, step=STEP)
+
+    def calls():
+        st = B.Model.stream_handle()
+        bf = dict(dtype=torch.bfloat16, device="cuda:0")
+        X, Rr = torch.from_numpy(x).cuda().bfloat16(), torch.from_numpy(x * 0.25).cuda().bfloat16()
+        z, y, dz, dx, o = (torch.zeros(rows, cols, **bf) for _ in range(5))
+        mean, rstd = torch.zeros(rows, device="cuda:0"), torch.zeros(rows, device="cuda:0")
+        G, Bt = column_vector(torch, gamma), column_vector(torch, beta)
+        dg, db = torch.zeros_like(G), torch.zeros_like(G)
+        ws = torch.empty(max(B.conef_norm_workspace(rows, cols), B.conef_mx_product_workspace(rows, rows, cols)), dtype=torch.uint8, device="cuda:0")
+        B.conef_norm_forward(d, 1e-5, X, Rr, G, Bt, z, y, mean, rstd, st)
+        p, pt = B.mx_alloc(rows, cols), B.mx_alloc(cols, rows)
+        B.conef_mx_quantise(y, B.MX_STOCHASTIC, SEED, 1, STEP, p, pt, st)
+        B.conef_mx_dequantise(p, o, st)
+        c, ct = torch.zeros(rows, rows, device="cuda:0"), torch.zeros(cols, cols, device="cuda:0")
+        B.conef_mx_product(p, p, cols, 1.0, 0.0, c, ws, st)
+        B.conef_mx_product(pt, pt, rows, 1.0, 0.0, ct, None, st)
+        B.conef_norm_backward(d, y, z, G, mean, rstd, Rr, dz, dx, dg, db, ws, st)
+        B.conef_dropout_backward(d, dz, dz, st)
+        return [z, y, mean, rstd, o, c, ct, dz, dx, dg, db, *p, *pt]
+
+    want = calls()
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        got = calls()
+    side.synchronize()
+    for a, b in zip(got, want):
+        assert torch.equal(a, b)
