@@ -485,10 +485,8 @@ def conef_cs_decode_error(ctx, table, e_out, stream=0):
 _kinds: dict = {}             # element types of matrices, once torch is there
 
 
-def _matrix(t, shape=None, dtype=None) -> Tuple[int, int, int, int, int]:
-    """(address, pitch, rows, cols, type) of a two-dimensional tensor whose rows are contiguous; of None: all 0."""
-    if t is None:
-        return 0, 0, 0, 0, 0
+def _matrix(t) -> Tuple[int, int, int, int, int]:
+    """(address, pitch, rows, cols, type) of a two-dimensional tensor whose rows are contiguous."""
     if not _kinds:
         import torch
 
@@ -497,16 +495,24 @@ def _matrix(t, shape=None, dtype=None) -> Tuple[int, int, int, int, int]:
     if len(size) != 2 or kind < 0 or (stride[1] != 1 and size[1] > 1):
         raise ConefError(EINVAL, f"a matrix of fp32 or bf16 with contiguous rows is wanted, not {tuple(size)} {t.dtype} {stride}")
     rows, cols = size
-    if shape is not None and (rows, cols, kind) != (*shape, dtype):
-        raise ConefError(EINVAL, f"a matrix of {shape} and type {dtype} is wanted, not {(rows, cols)} of type {kind}")
-    return t.data_ptr(), stride[0] if rows > 1 else max(cols, 1), rows, cols, kind
+    return t.data_ptr(), stride[0] if rows > 1 else cols or 1, rows, cols, kind
+
+
+def _like(t, of) -> Tuple[int, int]:
+    """(address, pitch) of a matrix of the shape and type of `of`; 0 for None."""
+    if t is None:
+        return 0, 0
+    size, stride = t.shape, t.stride()
+    if size != of.shape or t.dtype is not of.dtype or (stride[1] != 1 and size[1] > 1):
+        raise ConefError(EINVAL, f"a matrix like {tuple(of.shape)} {of.dtype} with contiguous rows is wanted, not {tuple(size)} {t.dtype} {stride}")
+    return t.data_ptr(), stride[0] if size[0] > 1 else size[1] or 1
 
 
 def _vector(t, n: int) -> int:
     """Address of n contiguous floats; 0 for None."""
     if t is None:
         return 0
-    if t.shape != (n,) or str(t.dtype) != "torch.float32" or not t.is_contiguous():
+    if t.shape != (n,) or _kinds.get(t.dtype) != F32 or not t.is_contiguous():
         raise ConefError(EINVAL, f"{n} contiguous floats are wanted, not {tuple(t.shape)} {t.dtype}")
     return t.data_ptr()
 
@@ -530,22 +536,22 @@ def _packed(pair, rows: int, cols: int) -> Tuple[int, int]:
 
 def conef_dropout_forward(drop, x, residual, y, stream=0):
     px, ix, rows, cols, kind = _matrix(x)
-    pr, ir = _matrix(residual, (rows, cols), kind)[:2]
-    py, iy = _matrix(y, (rows, cols), kind)[:2]
+    pr, ir = _like(residual, x)
+    py, iy = _like(y, x)
     _check(lib().conef_dropout_forward(drop, rows, cols, kind, px, ix, pr, ir, py, iy, stream), "conef_dropout_forward")
 
 
 def conef_dropout_backward(drop, dy, dx, stream=0):
     py, iy, rows, cols, kind = _matrix(dy)
-    px, ix = _matrix(dx, (rows, cols), kind)[:2]
+    px, ix = _like(dx, dy)
     _check(lib().conef_dropout_backward(drop, rows, cols, kind, py, iy, px, ix, stream), "conef_dropout_backward")
 
 
 def conef_norm_forward(drop, eps: float, x, residual, gamma, beta, z_out, y, mean_out, rstd_out, stream=0):
     px, ix, rows, cols, kind = _matrix(x)
-    pr, ir = _matrix(residual, (rows, cols), kind)[:2]
-    pz, iz = _matrix(z_out, (rows, cols), kind)[:2]
-    py, iy = _matrix(y, (rows, cols), kind)[:2]
+    pr, ir = _like(residual, x)
+    pz, iz = _like(z_out, x)
+    py, iy = _like(y, x)
     _check(lib().conef_norm_forward(drop, eps, rows, cols, kind, px, ix, pr, ir, _vector(gamma, cols), _vector(beta, cols), pz, iz, py,
                                     iy, _vector(mean_out, rows), _vector(rstd_out, rows), stream), "conef_norm_forward")
 
@@ -558,10 +564,10 @@ def conef_norm_workspace(rows: int, cols: int) -> int:
 
 def conef_norm_backward(drop, dy, z, gamma, mean, rstd, dz_in, dz, dx, dgamma, dbeta, workspace, stream=0):
     py, iy, rows, cols, kind = _matrix(dy)
-    pz, iz = _matrix(z, (rows, cols), kind)[:2]
-    pi, ii = _matrix(dz_in, (rows, cols), kind)[:2]
-    po, io = _matrix(dz, (rows, cols), kind)[:2]
-    px, ix = _matrix(dx, (rows, cols), kind)[:2]
+    pz, iz = _like(z, dy)
+    pi, ii = _like(dz_in, dy)
+    po, io = _like(dz, dy)
+    px, ix = _like(dx, dy)
     ws = _room(workspace, conef_norm_workspace(rows, cols)) if workspace is not None else 0
     _check(lib().conef_norm_backward(drop, rows, cols, kind, py, iy, pz, iz, _vector(gamma, cols), _vector(mean, rows),
                                      _vector(rstd, rows), pi, ii, po, io, px, ix, _vector(dgamma, cols), _vector(dbeta, cols), ws,
@@ -622,6 +628,9 @@ def conef_destroy(ctx):
     lib().conef_destroy(ctx)
 
 
+_raw_stream = None
+
+
 # ------------------------------------------------------------------ holder
 class Model:
     """One context plus its sizes and per-matrix offsets.  `alloc(device)` returns zeroed torch
@@ -661,10 +670,17 @@ class Model:
 
     @staticmethod
     def stream_handle() -> int:
-        import torch
+        """The current torch stream of the current device, as the calls take it."""
+        global _raw_stream
+        if _raw_stream is None:
+            import torch
 
-        return torch.cuda.current_stream().cuda_stream
-
+            torch.cuda.init()
+            # torch.cuda.current_stream() makes an object of it, which takes 2 us, as long as a launch; torch has it as a number too
+            raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+            current = torch.cuda.current_device
+            _raw_stream = (lambda: raw(current())) if raw else (lambda: torch.cuda.current_stream().cuda_stream)
+        return _raw_stream()
     def step(self, buf, step: int, Q_out=None):
         conef_step(self.ctx, buf["grads"], buf["codes"], buf["scales"], buf["Q"], buf["P"],
                    buf["Q"] if Q_out is None else Q_out, buf["ws"], step, self.stream_handle())
