@@ -157,6 +157,9 @@ struct Turned {
 // A workgroup takes 64 rows of 128 columns, or 128 rows of 64 columns if it quantises by columns too.  By rows: a wave takes 16 rows, of which
 // its lanes read 32 columns at a time, four lanes a block, and writes the 256 bytes of that piece together.  By columns: the same on
 // the tile in LDS, turned, the four octets of a block 16 lanes apart.
+// 8192 x 8192 in bf16 both ways: to nearest 45 us, 205 MB at 4.5 TB/s (by rows alone 32 us at 5.2), bound by memory; stochastically 65 us, bound by
+// its vector instructions, 113 an octet and way: 40 for the Philox call, eight conversions, which take 16 cycles each, 19 around
+// them.  (The same with the codes computed from integers: 100 us.)  64 columns and not 128 in the tile: 1203 x 1000 in fp32 4.7 / 6.0 us.
 template <bool BF16, bool STOCHASTIC, bool BY_ROWS, bool BY_COLS>
 __global__ __launch_bounds__(kThreads) void k_mx_quantise(MxQuantArgs a, int64_t row_pieces, int64_t col_pieces, int64_t col_tiles,
                                                           int64_t padded_rows, int64_t padded_cols)
@@ -252,7 +255,7 @@ __device__ __forceinline__ void values(uint32_t c, uint32_t byte, float v[8])
         for (int i = 0; i < 8; ++i) v[i] = __uint_as_float(0x7FC00000u);
 }
 
-// What a packed operand stands for: 16 rows a wave, 128 columns, four lanes a block.
+// What a packed operand stands for: 16 rows a wave, 128 columns, four lanes a block.  Bound by memory: 8192 x 8192 in bf16 28 us, 170 MB at 6.0 TB/s.
 template <bool BF16, bool PAST>
 __global__ __launch_bounds__(kThreads) void k_mx_dequantise(MxDequantArgs a, int64_t pieces, int64_t groups)
 {

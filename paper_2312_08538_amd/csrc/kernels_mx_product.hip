@@ -5,6 +5,11 @@
 // one byte of a register the block's scale.  A packed operand holds its codes in that order, 1024 bytes an instruction, and its
 // scales four row groups to a register, so a tile goes from memory to LDS and from there to registers as it lies, without a
 // bank conflict.  The instruction's first operand is B's rows: then a lane holds four consecutive columns of one row of C.
+//
+// What bounds it: the instructions alone, from registers, reach 6.8 PFLOP/s on zeros and 5.8 on random operands, where the card's power sets the
+// clock (the form of 32 x 32 x 64 9.8 and 6.6, but it adds to twice as many accumulators a product, and the same kernel on it took 255 us
+// for 8192 x 8192 x 8192 where this one took 238).  8192 x 8192 x 8192 reaches 4.6 PFLOP/s, 8192 x 2048 x 8192 4.3; with a shorter axis C's bytes and each
+// tile's beginning weigh more: 4096 x 50304 x 2048 3.7.
 #include <algorithm>
 #include <type_traits>
 #include <utility>
@@ -308,7 +313,7 @@ __global__ __launch_bounds__(64 * WM * WN, WAVES) void k_mx_product(MxProductArg
 }
 
 // Few rows of A (16 MT at most): a workgroup takes 16 rows of B, read once, straight to registers; its WAVES waves take pieces of the long axis in
-// turn, and their sums are added in order.
+// turn, and their sums are added in order.  8 x 8192 x 2048: 3.3 us with its launch, 9 MB.
 template <bool BF16, bool ADD, int MT, int WAVES>
 __global__ __launch_bounds__(64 * WAVES) void k_mx_rows(MxProductArgs a, int pieces)
 {

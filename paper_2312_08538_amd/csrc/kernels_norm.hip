@@ -26,6 +26,8 @@ inline bool in_registers(int64_t cols, int most) { return cols >= 8 && cols <= m
 constexpr int threads_of(int g) { return g > kThreads ? g : kThreads; }
 
 // ---------------------------------------------------------------- dropout
+// An octet a thread, which takes one Philox call.  Bound by memory: 16384 x 4096 in bf16 with a residual 67 us, 403 MB at 6.0 TB/s (a copy of
+// a gigabyte reaches 5.1; some of this comes from the card's last cache); the 150 vector instructions of an octet hide behind the loads.
 template <bool BF16>
 __global__ __launch_bounds__(kThreads) void k_dropout(DropoutArgs a, uint32_t octets, uint32_t per_row)
 {
@@ -87,7 +89,8 @@ __device__ __forceinline__ void load_columns(const float *p, int cols, int t, fl
 }
 
 // G lanes hold a row, V octets each: octet v of lane t starts at column 8 (t + G v).  The next row's octets are on their way while a row is
-// worked on.
+// worked on.  Bound by memory where there are rows enough for that: 16384 x 2048 in bf16 with dropout and residual 54 us, 268 MB at 5.0 TB/s,
+// without them 26 us; 777 x 5003 in fp32, two rows a workgroup at most, 21 us, 62 MB at 2.9 TB/s.
 template <bool BF16, int G, int V, bool FUSED>
 __global__ __launch_bounds__(threads_of(G)) void k_norm_forward(NormArgs a)
 {
@@ -253,6 +256,8 @@ __device__ __forceinline__ void finish_dz(const NormArgs &a, int64_t row, int64_
 
 // Each workgroup takes every gridDim-th row (or 256 / G of them) and keeps its share of dgamma and dbeta in registers, since a lane
 // sees the same columns in every row; k_norm_columns adds the shares.  The next row's octets are on their way while a row is worked on.
+// Bound by memory: 16384 x 2048 in bf16 with dropout and residual's gradient 60 us, 336 MB and 17 MB of shares at 5.9 TB/s, and 6 us for the
+// shares' sum; 777 x 5003 in fp32 20 us, 88 MB at 4.4 TB/s, and 4 us.
 template <bool BF16, int G, int V>
 __global__ __launch_bounds__(threads_of(G)) void k_norm_backward(NormArgs a)
 {
@@ -359,7 +364,8 @@ __global__ __launch_bounds__(threads_of(G)) void k_norm_backward(NormArgs a)
     }
 }
 
-// Rows of any length: two sweeps by a workgroup; the sums over rows are k_norm_column_parts's.
+// Rows of any length: two sweeps by a workgroup; the sums over rows are k_norm_column_parts's, which reads dy and z once more: with it 4096 x 16384 in
+// bf16 takes 235 us.  (Held in the registers of 1024 threads such rows spill: 378 us.)
 template <bool BF16>
 __global__ __launch_bounds__(kThreads) void k_norm_backward_long(NormArgs a)
 {
