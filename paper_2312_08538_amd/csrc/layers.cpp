@@ -100,9 +100,9 @@ int conef_norm_forward(const conef_drop *drop, float eps, int64_t rows, int64_t 
     NormArgs a;
     if (bad_shape(rows, cols, dtype) || !(eps >= 0.0f) || !std::isfinite(eps)) return CONEF_EINVAL;
     if (drop && !drop_args(drop, a.d)) return CONEF_EINVAL;
+    if (rows == 0) return CONEF_OK;                                 // a matrix of no rows may have no address
     if ((drop || residual) && !z_out) return CONEF_EINVAL;          // the backward pass needs what the norm was taken of
     if (!drop && !residual && z_out) return CONEF_EINVAL;
-    if (rows == 0) return CONEF_OK;
     if (bad_rows(x, x_pitch, cols, dtype) || bad_optional(residual, residual_pitch, cols, dtype) ||
         bad_optional(z_out, z_pitch, cols, dtype) || bad_rows(y, y_pitch, cols, dtype) || bad_floats(gamma) || bad_floats(beta) ||
         misaligned(mean_out, 4) || misaligned(rstd_out, 4) || y == z_out)
@@ -139,7 +139,7 @@ int conef_norm_backward(const conef_drop *drop, int64_t rows, int64_t cols, int 
     if (bad_shape(rows, cols, dtype)) return CONEF_EINVAL;
     if (drop && !drop_args(drop, a.d)) return CONEF_EINVAL;
     if (dx && !drop) return CONEF_EINVAL;                           // without a dropout dx is dz
-    if (!dz && !dx && !dgamma && !dbeta) return CONEF_EINVAL;
+    if (rows > 0 && !dz && !dx && !dgamma && !dbeta) return CONEF_EINVAL;
     if (misaligned(dgamma, 4) || misaligned(dbeta, 4)) return CONEF_EINVAL;
     const bool columns = dgamma || dbeta;
     if (rows > 0) {

@@ -609,3 +609,51 @@ def test_every_operator_on_a_stream_of_its_own(env):
     side.synchronize()
     for a, b in zip(got, want):
         assert torch.equal(a, b)
+
+
+def test_matrices_of_no_rows(env):
+    """An empty batch goes through every call; its tensors have no address."""
+    torch, B = env
+    st = B.Model.stream_handle()
+    d = B.conef_drop(p=0.25, site=0, seed=1, step=0)
+    for dtype in (torch.float32, torch.bfloat16):
+        e = torch.empty(0, 40, dtype=dtype, device="cuda:0")
+        g, none = torch.ones(40, device="cuda:0"), torch.empty(0, device="cuda:0")
+        B.conef_dropout_forward(d, e, e, e, st)
+        B.conef_dropout_backward(d, e, e, st)
+        for drop in (d, None):
+            B.conef_norm_forward(drop, 1e-5, e, e, g, g, e, e, none, none, st)
+            B.conef_norm_backward(drop, e, e, g, none, none, e, e, e if drop else None, None, None, None, st)
+        q, qt = B.mx_alloc(0, 40), B.mx_alloc(40, 0)
+        B.conef_mx_quantise(e, B.MX_STOCHASTIC, 1, 0, 0, q, qt, st)
+        B.conef_mx_dequantise(q, e, st)
+        B.conef_mx_product(q, B.mx_alloc(8, 40), 40, 1.0, 0.0, torch.empty(0, 8, dtype=dtype, device="cuda:0"), None, st)
+        c = torch.ones(40, 40, dtype=dtype, device="cuda:0")
+        B.conef_mx_product(qt, qt, 0, 1.0, 0.0, c, None, st)                       # a gradient of no tokens
+        torch.cuda.synchronize()
+        assert (c == 0).all()
+
+
+def test_binding_refuses_device_tensors_that_do_not_fit(env):
+    """None of these reaches a kernel."""
+    torch, B = env
+    st = B.Model.stream_handle()
+    z = lambda *s, **k: torch.zeros(*s, device="cuda:0", **k)                      # noqa: E731
+    d, x, v, m = B.conef_drop(p=0.25, site=0, seed=1, step=0), z(4, 8), z(8), z(4)
+    q = B.mx_alloc(4, 8)
+    bad = [lambda t=t: B.conef_dropout_backward(d, t, x, st) for t in (z(8, 4).t(), z(4, 8).double(), z(32), z(4, 16)[:, ::2], x.cpu())]
+    bad += [lambda t=t: B.conef_dropout_forward(d, x, t, x, st) for t in (z(4, 9), x.bfloat16(), z(8, 4).t(), x.cpu())]
+    bad += [lambda g=g: B.conef_norm_forward(None, 1e-5, x, None, g, v, None, x, None, None, st)
+            for g in (z(7), z(16)[::2], v.bfloat16(), v.cpu(), z(1, 8))]
+    bad += [lambda: B.conef_norm_backward(None, x, x, v, m, m, None, x, None, None, v, z(1), st),
+            lambda: B.conef_norm_backward(None, x, x, v, m, m, None, x, None, None, v, None, st),
+            lambda: B.conef_mx_quantise(z(4, 129), B.MX_NEAREST, 0, 0, 0, q, None, st),
+            lambda: B.conef_mx_quantise(x, B.MX_NEAREST, 0, 0, 0, None, None, st),
+            lambda: B.conef_mx_quantise(x, B.MX_NEAREST, 0, 0, 0, (q[0], q[1].cpu()), None, st),
+            lambda: B.conef_mx_dequantise(q, z(65, 8), st),
+            lambda: B.conef_mx_product(q, q, 129, 1.0, 0.0, z(4, 4), None, st),
+            lambda: B.conef_mx_product(q, q, 8, 1.0, 0.0, z(4, 65), None, st)]
+    for call in bad:
+        with pytest.raises(B.ConefError) as e:
+            call()
+        assert e.value.code == B.EINVAL

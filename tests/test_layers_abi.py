@@ -62,6 +62,7 @@ def test_norm_refuses_bad_arguments():
                 dict(d=drop(), z=P, y=P), dict(d=drop(site=1 << 30), z=P), dict(x=P + 1, dtype=1), dict(cols=9)]:
         assert fwd(**bad) == B.EINVAL, bad
     assert fwd(rows=0, x=0, y=0, gamma=0, beta=0) == B.OK
+    assert fwd(d=drop(), rows=0, x=0, y=0, z=0) == B.OK                           # an empty matrix may have no address
 
     def bwd(d=None, rows=4, cols=8, dtype=0, dy=P, z=P, gamma=P, mean=P, rstd=P, dz_in=0, dz=2 * P, dx=0, dgamma=P, dbeta=P, ws=P):
         return L.conef_norm_backward(d, rows, cols, dtype, dy, 8, z, 8, gamma, mean, rstd, dz_in, 8, dz, 8, dx, 8, dgamma, dbeta, ws, 0)
@@ -70,6 +71,7 @@ def test_norm_refuses_bad_arguments():
                 dict(rstd=0), dict(ws=0), dict(ws=P + 4), dict(dgamma=P + 2), dict(cols=9), dict(dtype=-1), dict(rows=-2)]:
         assert bwd(**bad) == B.EINVAL, bad
     assert bwd(rows=0, dgamma=0, dbeta=0) == B.OK
+    assert bwd(d=drop(), rows=0, dy=0, z=0, mean=0, rstd=0, dz=0, dgamma=0, dbeta=0, ws=0) == B.OK
     v = ctypes.c_size_t()
     assert L.conef_norm_workspace(4, 0, ctypes.byref(v)) == B.EINVAL
     assert L.conef_norm_workspace(4, 8, None) == B.EINVAL
@@ -139,6 +141,22 @@ def test_binding_refuses_tensors_that_do_not_fit():
         B.conef_mx_quantise(torch.zeros(4, 129), B.MX_NEAREST, 0, 0, 0, packed, None, st)       # operand too small
     with pytest.raises(B.ConefError):
         B.conef_mx_product(packed, packed, 129, 1.0, 0.0, torch.zeros(4, 4), None, st)
+
+
+def test_binding_refuses_host_memory():
+    """Everything about these tensors fits but where they are."""
+    import torch
+
+    x, v, m = torch.zeros(4, 8), torch.zeros(8), torch.zeros(4)
+    packed = tuple(torch.zeros(B.conef_mx_sizes(4, 8)[k], dtype=torch.uint8) for k in ("code_bytes", "scale_bytes"))
+    for call in [lambda: B.conef_dropout_forward(drop(), x, None, x, 0), lambda: B.conef_dropout_backward(drop(), x, x, 0),
+                 lambda: B.conef_norm_forward(None, 1e-5, x, None, v, v, None, x.clone(), m, m, 0),
+                 lambda: B.conef_norm_backward(None, x, x, v, m, m, None, x.clone(), None, None, None, None, 0),
+                 lambda: B.conef_mx_quantise(x, B.MX_NEAREST, 0, 0, 0, packed, None, 0), lambda: B.conef_mx_dequantise(packed, x, 0),
+                 lambda: B.conef_mx_product(packed, packed, 8, 1.0, 0.0, torch.zeros(4, 4), None, 0)]:
+        with pytest.raises(B.ConefError) as e:
+            call()
+        assert e.value.code == B.EINVAL and "device" in str(e.value)
 
 
 def test_reference_format_round_trip():
