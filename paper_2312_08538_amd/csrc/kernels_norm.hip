@@ -71,7 +71,7 @@ __device__ __forceinline__ void group_sum(float v[N], float *red, int &turn)
 #pragma unroll
             for (int step = 1; step < W; step *= 2)
 #pragma unroll
-                for (int w = 0; w < W; w += 2 * step) s[w] += s[w + step];
+                for (int w = 0; w + step < W; w += 2 * step) s[w] += s[w + step];
             v[i] = s[0];
         }
     }
@@ -90,7 +90,7 @@ __device__ __forceinline__ void load_columns(const float *p, int cols, int t, fl
 
 // G lanes hold a row, V octets each: octet v of lane t starts at column 8 (t + G v).  The next row's octets are on their way while a row is
 // worked on.  Bound by memory where there are rows enough for that: 16384 x 2048 in bf16 with dropout and residual 54 us, 268 MB at 5.0 TB/s,
-// without them 26 us; 777 x 5003 in fp32, two rows a workgroup at most, 21 us, 62 MB at 2.9 TB/s.
+// without them 26 us; 777 x 5003 in fp32, three rows a CU, 18 us, 62 MB at 3.5 TB/s.
 template <bool BF16, int G, int V, bool FUSED>
 __global__ __launch_bounds__(threads_of(G)) void k_norm_forward(NormArgs a)
 {
@@ -257,7 +257,7 @@ __device__ __forceinline__ void finish_dz(const NormArgs &a, int64_t row, int64_
 // Each workgroup takes every gridDim-th row (or 256 / G of them) and keeps its share of dgamma and dbeta in registers, since a lane
 // sees the same columns in every row; k_norm_columns adds the shares.  The next row's octets are on their way while a row is worked on.
 // Bound by memory: 16384 x 2048 in bf16 with dropout and residual's gradient 60 us, 336 MB and 17 MB of shares at 5.9 TB/s, and 6 us for the
-// shares' sum; 777 x 5003 in fp32 20 us, 88 MB at 4.4 TB/s, and 4 us.
+// shares' sum; 777 x 5003 in fp32 19 us, 88 MB at 4.6 TB/s, and 4 us.
 template <bool BF16, int G, int V>
 __global__ __launch_bounds__(threads_of(G)) void k_norm_backward(NormArgs a)
 {
@@ -460,35 +460,55 @@ __global__ __launch_bounds__(1024) void k_norm_columns(const float *partials, in
     if (out) out[c < cols ? c : c - cols] = (float)s;
 }
 
+// Rows of 2048 columns and more on an octet a lane, as many waves (in twos) as they have octets for.
+template <int G, int MOST, typename F>
+void by_lanes(int64_t cols, F &&go)
+{
+    if (cols <= 8 * G) go(std::integral_constant<int, G>{}, std::integral_constant<int, 1>{});
+    else if constexpr (8 * G < MOST) by_lanes<G + 128, MOST>(cols, go);
+}
+
 // Lanes to a row and octets a lane: at most two, which registers hold together with the next row on its way.  A wave to a row needs no barrier, but
 // four octets a lane (2048 columns) take 256 registers: the backward pass of 16384 x 2048 in bf16 then takes 86 us, with a workgroup to
-// a row 75.
-template <typename F>
+// a row 75.  Rows of 2048 columns to MOST take one octet a lane: up to 8192 in the fused forward pass, 6144 in the backward pass, whose registers hold
+// no more.  us, so / 256 or 512 lanes of two: forward 777 x 5003 fp32 17.8 / 20.7, 8192 x 5120 bf16 65 / 72, 4096 x 7000 fp32 89 / 102, 8192 x 2560
+// bf16 34 / 38, 4096 x 8192 bf16 52 / 50; backward 777 x 5003 fp32 23 / 26, 8192 x 5120 bf16 93 / 106, 16384 x 3000 bf16 100 / 115, 8192 x 4096
+// fp32 133 / 135.  A forward pass that is not fused has little to hold: 777 x 5003 fp32 11.0 / 9.9, 8192 x 5120 bf16 39 / 37.
+constexpr int kFusedLanes = 8192, kBackwardLanes = 6144, kPairs = 0;
+
+template <int MOST, typename F>
 void by_width(int64_t cols, F &&go)
 {
     using std::integral_constant;
     typedef integral_constant<int, 1> One;
     typedef integral_constant<int, 2> Two;
-    typedef integral_constant<int, 64> Wave;
-    typedef integral_constant<int, 256> Group;
-    if (cols <= 512) go(Wave{}, One{});
-    else if (cols <= 1024) go(Wave{}, Two{});
-    else if (cols <= 2048) go(Group{}, One{});
-    else if (cols <= 4096) go(Group{}, Two{});
-    else if (cols <= 8192) go(integral_constant<int, 512>{}, Two{});
-    else go(integral_constant<int, 1024>{}, Two{});
+    if (cols <= 512) go(integral_constant<int, 64>{}, One{});
+    else if (cols <= 1024) go(integral_constant<int, 64>{}, Two{});
+    else if (cols <= 2048) go(integral_constant<int, 256>{}, One{});
+    else if (cols <= MOST) {
+        if constexpr (MOST > 0) by_lanes<384, MOST>(cols, go);
+    } else if (cols <= 4096) {
+        if constexpr (MOST < 4096) go(integral_constant<int, 256>{}, Two{});
+    } else if (cols <= 8192) {
+        if constexpr (MOST < 8192) go(integral_constant<int, 512>{}, Two{});
+    } else {
+        if constexpr (MOST != kBackwardLanes) go(integral_constant<int, 1024>{}, Two{});      // (the backward pass has no rows as wide)
+    }
 }
 
 // Workgroups of the forward pass: about as many as the card holds at a time, so that each works on several rows with the next one on its way.
 // us, so many / 2048: 777 x 5003 fp32 fused 20.6 / 22.9, 8192 x 1024 bf16 13.8 / 15.2, 4096 x 16384 bf16 102 / 118.
-constexpr int forward_groups(int g, int v) { return g >= 512 ? 512 : v == 2 ? 768 : 1536; }
+constexpr int forward_groups(int g, int v) { return g * v > 640 ? 512 : g * v > 256 || v == 2 ? 768 : 1536; }
 
 // Workgroups of the backward pass: as many as the card holds at a time (four, two or one a CU, by their registers).
 int64_t most_parts(int64_t cols)
 {
-    int64_t n = 0;
-    if (!in_registers(cols, kBackwardCols)) return 512;
-    by_width(cols, [&](auto g, auto v) { n = decltype(g)::value > kThreads ? 256 : decltype(v)::value == 1 ? 1024 : 512; });
+    int64_t n = 512;
+    if (!in_registers(cols, kBackwardCols)) return n;
+    by_width<kBackwardLanes>(cols, [&](auto g, auto v) {
+        constexpr int G = decltype(g)::value, V = decltype(v)::value;
+        n = G * V > 512 ? 256 : G > kThreads || V == 2 ? 512 : 1024;
+    });
     return n;
 }
 
@@ -517,7 +537,7 @@ void launch_norm_forward(const NormArgs &a, bool bf16, hipStream_t st)
                 hipLaunchKernelGGL((k_norm_forward_long<decltype(b)::value, decltype(fused)::value>), grid, dim3(kThreads), 0, st, a);
                 return;
             }
-            by_width(a.cols, [&](auto g, auto v) {
+            by_width<decltype(fused)::value ? kFusedLanes : kPairs>(a.cols, [&](auto g, auto v) {
                 constexpr int G = decltype(g)::value;
                 const int64_t per = threads_of(G) / G, groups = (a.rows + per - 1) / per;
                 hipLaunchKernelGGL((k_norm_forward<decltype(b)::value, G, decltype(v)::value, decltype(fused)::value>),
@@ -547,8 +567,8 @@ void launch_norm_backward(const NormArgs &a, bool bf16, hipStream_t st)
                                    dim3(kThreads), 0, st, a);
             return;
         }
-        by_width(a.cols, [&](auto g, auto v) {
-            constexpr int G = decltype(g)::value <= 512 ? decltype(g)::value : 512;         // (wider rows went the other way)
+        by_width<kBackwardLanes>(a.cols, [&](auto g, auto v) {
+            constexpr int G = decltype(g)::value;
             const int64_t per = threads_of(G) / G;
             used = (int)std::min<int64_t>((a.rows + per - 1) / per, parts);
             hipLaunchKernelGGL((k_norm_backward<decltype(b)::value, G, decltype(v)::value>), dim3((unsigned)used), dim3(threads_of(G)), 0, st, a);
