@@ -1,4 +1,4 @@
-"""Thin ctypes face of libconef.so: the functions of include/conef.h under the same names,
+"""Thin face of libconef.so (ctypes, compiled where calls are small): the functions of include/conef.h under the same names,
 plus `Model`, a holder of one context with its buffer sizes and offsets.  Argument
 marshalling only -- every step of the path runs in the library's HIP kernels.  There is no
 fallback: if the compiled library is missing, loading raises.
@@ -6,7 +6,6 @@ fallback: if the compiled library is missing, loading raises.
 from __future__ import annotations
 
 import ctypes
-import functools
 import os
 from typing import List, Sequence, Tuple
 
@@ -482,83 +481,41 @@ def conef_cs_decode_error(ctx, table, e_out, stream=0):
 
 
 # a worker's own step: dropout, layer norm, microscaled 4-bit floating point.  Matrices are torch tensors of two dimensions
-# on the device (rows may be strided); their shape, type and pitch go with their address.  A small call's time is that of its
-# way through here and of the launch, 2 to 3 us each, so a tensor is asked for as little as its check needs.
-_kinds: dict = {}             # element types of matrices, once torch is there
+# on the device (rows may be strided); their shape, type and pitch go with their address.  Their marshalling is compiled
+# (csrc/face.cpp): a small call's time is that of its way through here and of its launch.
+_face = None
 
 
-def _matrix(t) -> Tuple[int, int, tuple, int]:
-    """(address, pitch, (rows, cols), type) of a two-dimensional tensor whose rows are contiguous."""
-    if not _kinds:
-        import torch
+def face():
+    """The compiled marshalling of the calls below, connected with libconef.so (built with it)."""
+    global _face
+    if _face is None:
+        import torch  # noqa: F401  (whose libraries the module needs)
 
-        _kinds.update({torch.float32: F32, torch.bfloat16: BF16})
-    kind, size, stride = _kinds.get(t.dtype, -1), t.shape, t.stride()
-    if len(size) != 2 or kind < 0 or not t.is_cuda or (stride[1] != 1 and size[1] > 1):
-        raise ConefError(EINVAL, f"a matrix of fp32 or bf16 on the device with contiguous rows is wanted, not {tuple(size)} {t.dtype} {stride} {t.device}")
-    return t.data_ptr(), stride[0] if size[0] > 1 else size[1] or 1, size, kind
-
-
-def _like(t, size, dtype) -> Tuple[int, int]:
-    """(address, pitch) of another matrix of that shape and type; 0 for None."""
-    if t is None:
-        return 0, 0
-    stride = t.stride()
-    if t.shape != size or t.dtype is not dtype or not t.is_cuda or (stride[1] != 1 and size[1] > 1):
-        raise ConefError(EINVAL, f"a matrix {tuple(size)} {dtype} on the device with contiguous rows is wanted, not {tuple(t.shape)} {t.dtype} {stride} {t.device}")
-    return t.data_ptr(), stride[0] if size[0] > 1 else size[1] or 1
-
-
-def _vector(t, n: int) -> int:
-    """Address of n contiguous floats; 0 for None."""
-    if t is None:
-        return 0
-    if t.shape != (n,) or _kinds.get(t.dtype) != F32 or not t.is_cuda or not t.is_contiguous():
-        raise ConefError(EINVAL, f"{n} contiguous floats on the device are wanted, not {tuple(t.shape)} {t.dtype} {t.device}")
-    return t.data_ptr()
-
-
-def _room(t, bytes_: int) -> int:
-    """Address of a buffer of at least `bytes_` bytes; 0 for None."""
-    if t is None:
-        return 0
-    if t.nbytes < bytes_ or not t.is_cuda or not t.is_contiguous():
-        raise ConefError(EINVAL, f"a contiguous buffer of {bytes_} bytes on the device is wanted, not {t.nbytes} {t.device}")
-    return t.data_ptr()
-
-
-def _packed(pair, rows: int, cols: int) -> Tuple[int, int]:
-    """Addresses of the codes and scales of a packed rows x cols operand, of conef_mx_sizes() bytes; 0 for None."""
-    if pair is None:
-        return 0, 0
-    elements = (rows + 63) // 64 * ((cols + 127) // 128) * 8192
-    return _room(pair[0], elements // 2), _room(pair[1], elements // 32)
+        try:
+            from . import _face as module
+        except ImportError as e:
+            raise RuntimeError(f"{os.path.join(_HERE, '_face.so')} does not load: build it with `python -m paper_2312_08538_amd.build`; "
+                               "there is no fallback path") from e
+        calls = ("dropout_forward", "dropout_backward", "norm_forward", "norm_workspace", "norm_backward", "mx_quantise",
+                 "mx_dequantise", "mx_product_workspace", "mx_product")
+        module.connect(conef_drop, ConefError, tuple(ctypes.cast(getattr(lib(), "conef_" + c), ctypes.c_void_p).value for c in calls))
+        _face = module
+    return _face
 
 
 def conef_dropout_forward(drop, x, residual, y, stream=0):
-    px, ix, size, kind = _matrix(x)
-    pr, ir = _like(residual, size, x.dtype)
-    py, iy = _like(y, size, x.dtype)
-    _check(lib().conef_dropout_forward(drop, *size, kind, px, ix, pr, ir, py, iy, stream), "conef_dropout_forward")
+    (_face or face()).dropout_forward(drop, x, residual, y, stream)
 
 
 def conef_dropout_backward(drop, dy, dx, stream=0):
-    py, iy, size, kind = _matrix(dy)
-    px, ix = _like(dx, size, dy.dtype)
-    _check(lib().conef_dropout_backward(drop, *size, kind, py, iy, px, ix, stream), "conef_dropout_backward")
+    (_face or face()).dropout_backward(drop, dy, dx, stream)
 
 
 def conef_norm_forward(drop, eps: float, x, residual, gamma, beta, z_out, y, mean_out, rstd_out, stream=0):
-    px, ix, size, kind = _matrix(x)
-    (rows, cols), dtype = size, x.dtype
-    pr, ir = _like(residual, size, dtype)
-    pz, iz = _like(z_out, size, dtype)
-    py, iy = _like(y, size, dtype)
-    _check(lib().conef_norm_forward(drop, eps, rows, cols, kind, px, ix, pr, ir, _vector(gamma, cols), _vector(beta, cols), pz, iz, py,
-                                    iy, _vector(mean_out, rows), _vector(rstd_out, rows), stream), "conef_norm_forward")
+    (_face or face()).norm_forward(drop, eps, x, residual, gamma, beta, z_out, y, mean_out, rstd_out, stream)
 
 
-@functools.lru_cache(maxsize=4096)
 def conef_norm_workspace(rows: int, cols: int) -> int:
     v = ctypes.c_size_t()
     _check(lib().conef_norm_workspace(rows, cols, ctypes.byref(v)), "conef_norm_workspace")
@@ -566,16 +523,7 @@ def conef_norm_workspace(rows: int, cols: int) -> int:
 
 
 def conef_norm_backward(drop, dy, z, gamma, mean, rstd, dz_in, dz, dx, dgamma, dbeta, workspace, stream=0):
-    py, iy, size, kind = _matrix(dy)
-    (rows, cols), dtype = size, dy.dtype
-    pz, iz = _like(z, size, dtype)
-    pi, ii = _like(dz_in, size, dtype)
-    po, io = _like(dz, size, dtype)
-    px, ix = _like(dx, size, dtype)
-    ws = _room(workspace, conef_norm_workspace(rows, cols)) if workspace is not None else 0
-    _check(lib().conef_norm_backward(drop, rows, cols, kind, py, iy, pz, iz, _vector(gamma, cols), _vector(mean, rows),
-                                     _vector(rstd, rows), pi, ii, po, io, px, ix, _vector(dgamma, cols), _vector(dbeta, cols), ws,
-                                     stream), "conef_norm_backward")
+    (_face or face()).norm_backward(drop, dy, z, gamma, mean, rstd, dz_in, dz, dx, dgamma, dbeta, workspace, stream)
 
 
 def conef_mx_sizes(rows: int, cols: int) -> dict:
@@ -594,17 +542,13 @@ def mx_alloc(rows: int, cols: int, device="cuda:0"):
 
 def conef_mx_quantise(x, rounding: int, seed: int, site: int, step: int, packed, packed_t, stream=0):
     """packed: (codes, scales) of x by rows, packed_t: of its transpose by rows; either may be None."""
-    px, ix, (rows, cols), kind = _matrix(x)
-    _check(lib().conef_mx_quantise(px, ix, rows, cols, kind, rounding, seed, site, step, *_packed(packed, rows, cols),
-                                   *_packed(packed_t, cols, rows), stream), "conef_mx_quantise")
+    (_face or face()).mx_quantise(x, rounding, seed, site, step, packed, packed_t, stream)
 
 
 def conef_mx_dequantise(packed, out, stream=0):
-    po, io, (rows, cols), kind = _matrix(out)
-    _check(lib().conef_mx_dequantise(*_packed(packed, rows, cols), rows, cols, po, io, kind, stream), "conef_mx_dequantise")
+    (_face or face()).mx_dequantise(packed, out, stream)
 
 
-@functools.lru_cache(maxsize=4096)
 def conef_mx_product_workspace(m: int, n: int, k: int) -> int:
     v = ctypes.c_size_t()
     _check(lib().conef_mx_product_workspace(m, n, k, ctypes.byref(v)), "conef_mx_product_workspace")
@@ -613,10 +557,7 @@ def conef_mx_product_workspace(m: int, n: int, k: int) -> int:
 
 def conef_mx_product(a, b, k: int, alpha: float, beta: float, c, workspace, stream=0):
     """c [m, n] <- alpha A B^T + beta c of the packed operands a (m x k) and b (n x k)."""
-    pc, ic, (m, n), kind = _matrix(c)
-    ws = _room(workspace, conef_mx_product_workspace(m, n, k)) if workspace is not None else 0
-    _check(lib().conef_mx_product(*_packed(a, m, k), *_packed(b, n, k), m, n, k, alpha, beta, pc, ic, kind, ws, stream),
-           "conef_mx_product")
+    (_face or face()).mx_product(a, b, k, alpha, beta, c, workspace, stream)
 
 
 def conef_set_timing(ctx, on: bool):
