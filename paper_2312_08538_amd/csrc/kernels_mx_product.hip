@@ -211,11 +211,7 @@ __global__ __launch_bounds__(64 * WM * WN, WAVES) void k_mx_product(MxProductArg
         read(after, next);
         unroll<TM>([&](auto i) {
             unroll<TN>([&](auto j) {
-#if defined(EXP_S) || defined(EXP_T)
-                constexpr int I = decltype(i)::value, J = I & 1 ? TN - 1 - decltype(j)::value : decltype(j)::value;
-#else
                 constexpr int I = decltype(i)::value, J = decltype(j)::value;
-#endif
                 acc[J][I] = mfma_mx<J % 4, I % 4>(now.b[J], now.a[I], acc[J][I], now.eb[J / 4], now.ea[I / 4]);
             });
         });
@@ -484,13 +480,7 @@ void launch_mx_product(const MxProductArgs &a, bool bf16, hipStream_t st)
                     constexpr bool PAST = decltype(p)::value;
                     if (c.tiles == kSmall) launch_tiles<B, ADD, PAST, 2, 2, 4, 4, 3, 3>(a, c, st);
                     else if (c.tiles == kWide) launch_tiles<B, ADD, PAST, 2, 2, 8, 4, 3, 2>(a, c, st);
-                    else 
-#ifdef EXP_E
-launch_tiles<B, ADD, PAST, 2, 2, 8, 8, 4, 1>(a, c, st);
-#else
-launch_tiles<B, ADD, PAST, 2, 4, 8, 4, 4, 2>(a, c, st);
-#endif
-
+                    else launch_tiles<B, ADD, PAST, 2, 4, 8, 4, 4, 2>(a, c, st);
                 });
             }
         });
