@@ -7,9 +7,10 @@
 // bank conflict.  The instruction's first operand is B's rows: then a lane holds four consecutive columns of one row of C.
 //
 // What bounds it: the instructions alone, from registers, reach 6.8 PFLOP/s on zeros and 5.8 on random operands, where the card's power sets the
-// clock (the form of 32 x 32 x 64 9.8 and 6.6, but it adds to twice as many accumulators a product, and the same kernel on it took 255 us
-// for 8192 x 8192 x 8192 where this one took 238).  8192 x 8192 x 8192 reaches 4.6 PFLOP/s, 8192 x 2048 x 8192 4.3; with a shorter axis C's bytes and each
-// tile's beginning weigh more: 4096 x 50304 x 2048 3.7.
+// clock (the form of 32 x 32 x 64 9.8 and 6.6, but it adds to twice as many accumulators a product, and the same kernels on it took 259 us
+// for 8192 x 8192 x 8192 where this one took 246, 251 for 4096 x 50304 x 2048 where this one took 235).  8192 x 8192 x 8192 reaches 4.7 PFLOP/s, 8192 x
+// 2048 x 8192 4.4: without its loads to LDS it would take 208 us, without its reads from there 219, without either 189, without the products 126.  With a
+// shorter axis C's bytes and each tile's beginning weigh more: 4096 x 50304 x 2048 4.0, without stores 4.3.
 #include <algorithm>
 #include <type_traits>
 #include <utility>
@@ -312,6 +313,188 @@ __global__ __launch_bounds__(64 * WM * WN, WAVES) void k_mx_product(MxProductArg
     }
 }
 
+// Tiles one after the other by as many workgroups as there are CUs: WM x WN waves of TM x TN tiles of 16 x 16, steps and waits as above.  The last
+// steps of a tile fetch the first of the next one, and a wave writes its part of C while the others go on, by way of 16 rows of 128 bytes in
+// LDS that are its own, so that a store writes whole lines.
+template <bool BF16, bool ADD, bool PAST, int WM, int WN, int TM, int TN, int STAGES>
+__global__ __launch_bounds__(64 * WM * WN, 2) void k_mx_stream(MxProductArgs a, Shape z)
+{
+    constexpr int kM = WM * TM * 16, kN = WN * TN * 16, kWaves = WM * WN, kStage = (kM + kN) * 68;
+    constexpr int kCodeLoads = (kM + kN) / 16 / kWaves, kScaleLoads = ((kM + kN) / 64 + kWaves - 1) / kWaves;
+    constexpr int kLoads = kCodeLoads + kScaleLoads, kSize = BF16 ? 2 : 4, kPitch = 144;
+    static_assert((kM + kN) / 16 % kWaves == 0 && TM % 4 == 0 && TN == 4 && STAGES >= 2 && (STAGES - 1) * kLoads < 64, "");
+    // (one array: with a second one the compiler waits for all loads before it reads either)
+    __shared__ __attribute__((aligned(1024))) uint8_t lds[STAGES * kStage + (ADD ? 0 : kWaves * 16 * kPitch)];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int wm = wave % WM, wn = wave / WM;
+    // (items to dies as above; a die's workgroups take its run in turn)
+    const int die = blockIdx.x & 7, per_die = z.items >> 3, more = z.items & 7;
+    const int end = (die + 1) * per_die + min(die + 1, more), stride = ((int)gridDim.x - die + 7) >> 3;
+    int item = die * per_die + min(die, more) + (int)(blockIdx.x >> 3), m0, n0;
+    struct Sources {
+        const uint8_t *codes[kCodeLoads], *scales[kScaleLoads];
+    } src, next_src;
+    auto point = [&](int to, Sources &p) {
+        const int band = to / (8 * z.tiles_n), in_band = to - band * 8 * z.tiles_n, high = min(z.tiles_m - 8 * band, 8);
+        m0 = (8 * band + in_band % high) * kM;
+        n0 = in_band / high * kN;
+#pragma unroll
+        for (int i = 0; i < kCodeLoads; ++i) {
+            const int g = wave + i * kWaves;
+            const bool is_a = g < kM / 16;
+            const int group = is_a ? min(m0 / 16 + g, z.a_groups - 1) : min(n0 / 16 + g - kM / 16, z.b_groups - 1);
+            p.codes[i] = (is_a ? a.a.codes : a.b.codes) + (int64_t)group * z.pieces * 1024;
+        }
+#pragma unroll
+        for (int i = 0; i < kScaleLoads; ++i) {
+            const int g = (wave + i * kWaves) % ((kM + kN) / 64);
+            const bool is_a = g < kM / 64;
+            const int group = is_a ? min(m0 / 64 + g, z.a_groups / 4 - 1) : min(n0 / 64 + g - kM / 64, z.b_groups / 4 - 1);
+            p.scales[i] = (is_a ? a.a.scales : a.b.scales) + (int64_t)group * z.pieces * 256;
+        }
+    };
+    int left = z.pieces;                // of the tile that is being fetched
+    auto fetch = [&](int slot) {
+        uint8_t *to = lds + slot * kStage;
+#pragma unroll
+        for (int i = 0; i < kCodeLoads; ++i) to_lds<16>(src.codes[i] + lane * 16, to + (wave + i * kWaves) * 1024);
+#pragma unroll
+        for (int i = 0; i < kScaleLoads; ++i) to_lds<4>(src.scales[i] + lane * 4, to + (kM + kN) * 64 + (wave + i * kWaves) % ((kM + kN) / 64) * 256);
+        const bool over = --left == 0;
+        left = over ? z.pieces : left;
+#pragma unroll
+        for (int i = 0; i < kCodeLoads; ++i) src.codes[i] = over ? next_src.codes[i] : src.codes[i] + 1024;
+#pragma unroll
+        for (int i = 0; i < kScaleLoads; ++i) src.scales[i] = over ? next_src.scales[i] : src.scales[i] + 256;
+    };
+    const int la = wm * TM * 1024 + lane * 16, lb = (kM / 16 + wn * TN) * 1024 + lane * 16;
+    const int sa = (kM + kN) * 64 + wm * TM / 4 * 256 + lane * 4, sb = (kM + kN) * 64 + kM * 4 + wn * TN / 4 * 256 + lane * 4;
+    typedef Step<TM, TN> S;
+    auto read = [&](int slot, S &f) {
+        const uint8_t *from = lds + slot * kStage;
+#pragma unroll
+        for (int i = 0; i < TM / 4; ++i) f.ea[i] = *reinterpret_cast<const int *>(from + sa + i * 256);
+#pragma unroll
+        for (int i = 0; i < TN / 4; ++i) f.eb[i] = *reinterpret_cast<const int *>(from + sb + i * 256);
+#pragma unroll
+        for (int i = 0; i < TN; ++i) f.b[i] = *reinterpret_cast<const v4i *>(from + lb + i * 1024);
+#pragma unroll
+        for (int i = 0; i < TM; ++i) f.a[i] = *reinterpret_cast<const v4i *>(from + la + i * 1024);
+    };
+    f32x4 acc[TN][TM];
+    int slot = 0;
+    auto step = [&](const S &now, S &next) {
+        const int after = slot + 1 == STAGES ? 0 : slot + 1;
+        wait_loads<(STAGES - 2) * kLoads>();
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+        fetch(slot);
+        __builtin_amdgcn_sched_barrier(0);
+        read(after, next);
+        unroll<TM>([&](auto i) {
+            unroll<TN>([&](auto j) {
+                constexpr int I = decltype(i)::value, J = decltype(j)::value;
+                acc[J][I] = mfma_mx<J % 4, I % 4>(now.b[J], now.a[I], acc[J][I], now.eb[J / 4], now.ea[I / 4]);
+            });
+        });
+        unroll<TM + TN>([&](auto r) {
+            constexpr int R = decltype(r)::value, kReads = TM + TN, kProducts = TM * TN;
+            __builtin_amdgcn_sched_group_barrier(0x008, (R + 1) * kProducts / kReads - R * kProducts / kReads, 0);
+            __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+        });
+        __builtin_amdgcn_sched_barrier(0);
+        slot = after;
+    };
+
+    point(item, src);
+    for (int s = 0; s < STAGES; ++s) fetch(s);          // (a tile has more pieces)
+    wait_loads<(STAGES - 1) * kLoads>();
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+    S even, odd;
+    read(0, even);
+    for (;;) {
+#pragma unroll
+        for (int j = 0; j < TN; ++j)
+#pragma unroll
+            for (int i = 0; i < TM; ++i) acc[j][i] = f32x4{};
+        const int row0 = m0 + wm * TM * 16, col0 = n0 + wn * TN * 16;
+        item += stride;
+        const bool go_on = item < end;
+        point(go_on ? item : item - stride, next_src);       // (behind the last tile: fetched for nothing)
+        int s = 0;
+        for (; s + 1 < z.pieces; s += 2) {
+            step(even, odd);
+            step(odd, even);
+        }
+        if (s < z.pieces) {
+            step(even, odd);
+            even = odd;
+        }
+        if constexpr (ADD) {
+#pragma unroll
+            for (int i = 0; i < TM; ++i)
+#pragma unroll
+                for (int j = 0; j < TN; j += 2)
+                    store_pair<BF16, ADD, PAST>(a, row0 + i * 16 + (lane & 15), col0 + j * 16, lane >> 4, acc[j][i], acc[j + 1][i]);
+        } else {
+            uint8_t *mine = lds + STAGES * kStage + wave * 16 * kPitch;
+            constexpr int kUnit = 128 / kSize, kUnits = TN * 16 / kUnit, kPairs = kUnit / 32;
+            auto write = [&](auto inside) {
+#pragma unroll
+                for (int i = 0; i < TM; ++i)
+#pragma unroll
+                    for (int h = 0; h < kUnits; ++h) {
+#pragma unroll
+                        for (int q = 0; q < kPairs; ++q) {
+                            const f32x4 u = acc[2 * (h * kPairs + q)][i], v = acc[2 * (h * kPairs + q) + 1][i];
+                            uint8_t *to = mine + (lane & 15) * kPitch + q * 32 * kSize;
+                            if constexpr (BF16) {
+                                uint32_t w[4];
+#pragma unroll
+                                for (int e = 0; e < 2; ++e) {
+                                    auto x = __builtin_amdgcn_permlane16_swap(pack_bf16(a.alpha * u[2 * e], a.alpha * u[2 * e + 1]),
+                                                                              pack_bf16(a.alpha * v[2 * e], a.alpha * v[2 * e + 1]), false, false);
+                                    w[e] = x[0];
+                                    w[2 + e] = x[1];
+                                }
+                                *reinterpret_cast<uint4 *>(to + 32 * ((lane >> 4) & 1) + 16 * (lane >> 5)) = make_uint4(w[0], w[1], w[2], w[3]);
+                            } else {
+                                *reinterpret_cast<float4 *>(to + 16 * (lane >> 4)) = make_float4(a.alpha * u[0], a.alpha * u[1], a.alpha * u[2], a.alpha * u[3]);
+                                *reinterpret_cast<float4 *>(to + 64 + 16 * (lane >> 4)) = make_float4(a.alpha * v[0], a.alpha * v[1], a.alpha * v[2], a.alpha * v[3]);
+                            }
+                        }
+                        __builtin_amdgcn_wave_barrier();
+#pragma unroll
+                        for (int g = 0; g < 2; ++g) {
+                            const int r = 8 * g + (lane >> 3), c = lane & 7;
+                            const int64_t row = row0 + i * 16 + r, col = col0 + h * kUnit + c * (16 / kSize);
+                            const uint4 w = *reinterpret_cast<const uint4 *>(mine + r * kPitch + c * 16);
+                            if (!decltype(inside)::value && (row >= a.m || col >= a.n)) continue;
+                            uint8_t *to = static_cast<uint8_t *>(a.c.data) + (row * a.c.pitch + col) * kSize;
+                            if (decltype(inside)::value || col + 16 / kSize <= a.n) {
+                                store_16<PAST>(to, u32x4_any{w.x, w.y, w.z, w.w});
+                            } else {
+                                const uint32_t e[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+                                for (int x = 0; x < 16 / kSize; ++x) {
+                                    if (col + x >= a.n) continue;
+                                    if constexpr (BF16) reinterpret_cast<uint16_t *>(to)[x] = (uint16_t)(e[x >> 1] >> (16 * (x & 1)));
+                                    else reinterpret_cast<uint32_t *>(to)[x] = e[x];
+                                }
+                            }
+                        }
+                        __builtin_amdgcn_wave_barrier();
+                    }
+            };
+            if (row0 + TM * 16 <= a.m && col0 + TN * 16 <= a.n) write(std::true_type{});
+            else write(std::false_type{});
+        }
+        if (!go_on) break;
+    }
+    wait_loads<0>();                    // what was fetched for nothing is in LDS before that is another workgroup's
+}
+
 // Few rows of A (16 MT at most): a workgroup takes 16 rows of B, read once, straight to registers; its WAVES waves take pieces of the long axis in
 // turn, and their sums are added in order.  8 x 8192 x 2048: 3.3 us with its launch, 9 MB.
 template <bool BF16, bool ADD, int MT, int WAVES>
@@ -383,7 +566,7 @@ void by_bool(bool v, F &&go)
     else go(std::false_type{});
 }
 
-enum Tiles { kRows, kTiny, kSmall, kWide, kLarge };
+enum Tiles { kRows, kTiny, kSmall, kWide, kLarge, kStream };
 
 struct Choice {
     Tiles tiles;
@@ -394,20 +577,22 @@ constexpr int kCus = 256;
 
 // Which kernel, and whether C goes past the caches.  us of a call (bf16 C unless said otherwise), the one taken / the next best:
 //   rows (m <= 64)   8 x 8192 x 2048 2.7 / 4.8 tiny, 1 x 50304 x 2048 11.3 / 11.8 small, 64 x 2048 x 8192 5.4 / 9.8 tiny in 4 parts
-//   large, 256 x 256, eight waves: the fewest reads from LDS, but a CU holds one workgroup, which begins and ends alone; for long sums:
-//                    8192 x 8192 x 8192 242 / 257 wide, 8192 x 2048 x 8192 66 / 71 wide; 4096 x 50304 x 2048 249 wide / 250
-//   wide, 256 x 128, two workgroups a CU:  4096 x 50304 x 2048 249 / 280 small; 8192 x 32768 x 1024 184 small / 190
+//   stream, 256 x 256, one tile after the other, from four to a CU on:  8192 x 8192 x 8192 240 / 249 large, 4096 x 50304 x 2048 215 / 224 wide,
+//                    8192 x 8192 x 1536 53 / 58 wide, 16384 x 8192 x 4096 241 / 261 large; but 6144 x 4096 x 2048 33 / 28 wide
+//   large, 256 x 256, eight waves: the fewest reads, but a CU holds one workgroup, which begins and ends alone; for long sums of fewer
+//                    tiles: 8192 x 2048 x 8192 62 / 71 wide, 64 stream
+//   wide, 256 x 128, two workgroups a CU:  4096 x 8192 x 2048 38.7 / 38.1 stream; 8192 x 32768 x 1024 184 small / 190
 //   small, 128 x 128, three a CU:  2048 x 50304 x 768 65 / 69 wide, 2048 x 2048 x 16384 43 / 56 in 2 parts, 60 tiny; 512 x 8192 x 2048 9.4 / 11.8 tiny
 //   tiny, 64 x 64, where small ones do not reach every CU:  1024 x 1024 x 1024 4.0 / 5.6, 16384 x 16 x 4096 8.4 / 11.7, 128 x 4096 x 1024 3.8 / 5.5
 // The long axis in parts, added up by a launch of its own: 256 x 256 x 8192 9.4 in 4 parts / 12.6, but 200 x 1024 x 4096 8.7 in 2 / 7.6.
 // Past the caches what those of the dies do not hold: 8192 x 32768 x 1024 184 / 270, 8192 x 8192 x 2048 in fp32 88 / 97, 4096 x 8192 x 2048 42 / 43;
-// large tiles only what the card's last cache does not hold either: 4096 x 50304 x 2048 250 / 292, but 8192 x 8192 x 2048 94 / 88.
+// large tiles and streams only what the card's last cache does not hold either: 4096 x 50304 x 2048 205 / 236, but 8192 x 8192 x 2048 75 / 67.
 Choice choose(int64_t m, int64_t n, int64_t k)
 {
     const int64_t pieces = std::max<int64_t>((k + 127) / 128, 1);
     auto tiles = [&](int64_t tm, int64_t tn) { return ((m + tm - 1) / tm) * ((n + tn - 1) / tn); };
     if (m <= 64) return {kRows, 1, (int)pieces};
-    if (tiles(256, 256) >= 192 && pieces >= 12) return {pieces >= 32 ? kLarge : kWide, 1, (int)pieces};
+    if (tiles(256, 256) >= 192 && pieces >= 12) return {tiles(256, 256) >= 4 * kCus ? kStream : pieces >= 32 ? kLarge : kWide, 1, (int)pieces};
     if (tiles(128, 128) >= 200) return {kSmall, 1, (int)pieces};
     const int64_t parts = pieces < 64 ? 1 : std::max<int64_t>(std::min<int64_t>(kCus / tiles(64, 64), pieces / 16), 1);
     const int64_t per = (pieces + parts - 1) / parts;
@@ -427,6 +612,19 @@ void launch_tiles(const MxProductArgs &a, const Choice &c, hipStream_t st)
     z.per_part = c.per_part;
     z.items = z.tiles_m * z.tiles_n * c.parts;
     hipLaunchKernelGGL((k_mx_product<BF16, ADD, PAST, WM, WN, TM, TN, STAGES, WAVES>), dim3((unsigned)z.items), dim3(64 * WM * WN), 0, st, a, z);
+}
+
+template <bool BF16, bool ADD, bool PAST>
+void launch_stream(const MxProductArgs &a, hipStream_t st)
+{
+    Shape z;
+    z.pieces = z.per_part = (int)((a.k + 127) / 128);
+    z.a_groups = (int)((a.m + 63) / 64 * 4);
+    z.b_groups = (int)((a.n + 63) / 64 * 4);
+    z.tiles_m = (int)((a.m + 255) / 256);
+    z.tiles_n = (int)((a.n + 255) / 256);
+    z.items = z.tiles_m * z.tiles_n;
+    hipLaunchKernelGGL((k_mx_stream<BF16, ADD, PAST, 2, 4, 8, 4, 4>), dim3((unsigned)std::min(z.items, kCus)), dim3(512), 0, st, a, z);
 }
 
 template <bool BF16, bool ADD>
@@ -463,7 +661,7 @@ void launch_mx_product(const MxProductArgs &a, bool bf16, hipStream_t st)
         p.alpha = 1.0f;                     // (beta is for the launch that adds the parts)
         launch_tiles<false, false, false, 2, 2, 2, 2, 4, 4>(p, c, st);
     }
-    const bool past = a.m * a.n * (bf16 ? 2 : 4) > (int64_t)(c.tiles == kLarge ? 256 : 32) << 20;
+    const bool past = a.m * a.n * (bf16 ? 2 : 4) > (int64_t)(c.tiles >= kLarge ? 256 : 32) << 20;
     by_bool(bf16, [&](auto b) {
         by_bool(a.beta != 0.0f, [&](auto add) {
             constexpr bool B = decltype(b)::value, ADD = decltype(add)::value;
@@ -479,6 +677,7 @@ void launch_mx_product(const MxProductArgs &a, bool bf16, hipStream_t st)
                 by_bool(past, [&](auto p) {
                     constexpr bool PAST = decltype(p)::value;
                     if (c.tiles == kSmall) launch_tiles<B, ADD, PAST, 2, 2, 4, 4, 3, 3>(a, c, st);
+                    else if (c.tiles == kStream) launch_stream<B, ADD, PAST>(a, st);
                     else if (c.tiles == kWide) launch_tiles<B, ADD, PAST, 2, 2, 8, 4, 3, 2>(a, c, st);
                     else launch_tiles<B, ADD, PAST, 2, 4, 8, 4, 4, 2>(a, c, st);
                 });

@@ -436,6 +436,32 @@ def test_product(env, m, n, k, bf16, alpha, beta):
     c.check_canary()
 
 
+@pytest.mark.parametrize("m,n,k", [(2000, 1700, 300), (3500, 3600, 1537), (3500, 3600, 4200), (8200, 8190, 1537), (1000, 65700, 1700)])
+@pytest.mark.parametrize("bf16", [False, True])
+@pytest.mark.parametrize("alpha,beta", [(1.0, 0.0), (0.125, 1.0)])
+def test_large_product(env, m, n, k, bf16, alpha, beta):
+    """As above, with the sums in 64 bits on the device: every tile size, odd and even numbers of pieces, several tiles a workgroup."""
+    torch, B = env
+    a, b = product_inputs(m, n, k)
+    A, W = (torch.from_numpy(R.mx_decode(*v)).cuda().double() for v in (a, b))
+    c = torch.full((m, n + 3), float("nan"), dtype=torch.bfloat16 if bf16 else torch.float32, device="cuda:0")
+    if beta:
+        c.normal_()
+    out, old = c[:, :n], c.double()
+    room = B.conef_mx_product_workspace(m, n, k)
+    ws = torch.full((room,), 0xFF, dtype=torch.uint8, device="cuda:0") if room else None
+    B.conef_mx_product(on_gpu(torch, a), on_gpu(torch, b), k, alpha, beta, out, ws, B.Model.stream_handle())
+    want = alpha * torch.mm(A, W.t())
+    far = alpha * torch.mm(A.abs(), W.abs().t()) * ((5 * (-(-k // 128)) + 24) * 2.0 ** -23)
+    if beta:
+        want += beta * old[:, :n]
+        far += 2 * U * old[:, :n].abs()
+    far += want.abs() * (2 * U + (R.U16 * 1.01 if bf16 else 0))
+    assert bool(((out.double() - want).abs() <= far).all())
+    rest, was = c[:, n:].double(), old[:, n:]
+    assert bool(((rest == was) | (rest.isnan() & was.isnan())).all())
+
+
 def test_product_of_nothing(env):
     torch, B = env
     empty = tuple(torch.empty(0, dtype=torch.uint8, device="cuda:0") for _ in range(2))

@@ -12,7 +12,7 @@ def of(kernels, name):  # noqa: F811
 
 def test_no_kernel_spills(kernels):  # noqa: F811
     for name in ("k_dropout", "k_norm_forward", "k_norm_backward", "k_norm_forward_long", "k_norm_backward_long", "k_norm_column_parts",
-                 "k_norm_columns", "k_mx_quantise", "k_mx_dequantise", "k_mx_product", "k_mx_rows", "k_mx_join"):
+                 "k_norm_columns", "k_mx_quantise", "k_mx_dequantise", "k_mx_product", "k_mx_stream", "k_mx_rows", "k_mx_join"):
         for k, v in of(kernels, name).items():
             assert v["spills"] == 0, (k, v)
 
