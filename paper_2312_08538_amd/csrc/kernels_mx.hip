@@ -159,22 +159,23 @@ struct Turned {
 // the tile in LDS, turned, the four octets of a block 16 lanes apart.
 // 8192 x 8192 in bf16 both ways: to nearest 45 us, 205 MB at 4.5 TB/s (by rows alone 32 us at 5.2), bound by memory; stochastically 65 us, bound by
 // its vector instructions, 113 an octet and way: 40 for the Philox call, eight conversions, which take 16 cycles each, 19 around
-// them.  (The same with the codes computed from integers: 100 us.)  64 columns and not 128 in the tile: 1203 x 1000 in fp32 4.7 / 6.0 us.
-template <bool BF16, bool STOCHASTIC, bool BY_ROWS, bool BY_COLS>
-__global__ __launch_bounds__(kThreads) void k_mx_quantise(MxQuantArgs a, int64_t row_pieces, int64_t col_pieces, int64_t col_tiles,
+// them.  (The same with the codes computed from integers: 100 us.)  64 columns and not 128 in the tile (of four waves): 1203 x 1000 in fp32 4.7 / 6.0 us.
+template <bool BF16, bool STOCHASTIC, bool BY_ROWS, bool BY_COLS, int WAVES>
+__global__ __launch_bounds__(64 * WAVES) void k_mx_quantise(MxQuantArgs a, int64_t row_pieces, int64_t col_pieces, int64_t col_tiles,
                                                           int64_t padded_rows, int64_t padded_cols)
 {
-    constexpr int kRows = BY_COLS ? 128 : 64, kCols = BY_COLS ? 64 : 128, kBlocks = kCols / 32;
+    constexpr int kRows = BY_COLS ? 128 : 64, kCols = BY_COLS ? 64 : 128, kBlocks = kCols / 32, kTurns = kRows / 16 / WAVES;
+    static_assert(kTurns * WAVES * 16 == kRows, "");
     __shared__ __attribute__((aligned(16))) std::conditional_t<BY_COLS, Turned<BF16>, char> tile;
     __shared__ __attribute__((aligned(4))) uint8_t scales[2][256];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r = lane >> 2, q = lane & 3;
     const int64_t row0 = blockIdx.x / col_tiles * kRows, col0 = blockIdx.x % col_tiles * kCols;
     const uint32_t per_row = (uint32_t)((a.cols + 7) >> 3), per_col = (uint32_t)((a.rows + 7) >> 3);
-    Octet<BF16> o[kRows / 64][kBlocks];
+    Octet<BF16> o[kTurns][kBlocks];
     auto fetch = [&](bool whole) {
 #pragma unroll
-        for (int h = 0; h < kRows / 64; ++h) {
-            const int64_t row = row0 + 16 * (wave + 4 * h) + r;
+        for (int h = 0; h < kTurns; ++h) {
+            const int64_t row = row0 + 16 * (wave + WAVES * h) + r;
 #pragma unroll
             for (int b = 0; b < kBlocks; ++b) {
                 const int64_t col = col0 + 32 * b + 8 * q;
@@ -186,16 +187,16 @@ __global__ __launch_bounds__(kThreads) void k_mx_quantise(MxQuantArgs a, int64_t
     else fetch(false);
     if constexpr (BY_COLS) {
 #pragma unroll
-        for (int h = 0; h < kRows / 64; ++h)
+        for (int h = 0; h < kTurns; ++h)
 #pragma unroll
-            for (int b = 0; b < kBlocks; ++b) tile.put(16 * (wave + 4 * h) + r, 32 * b + 8 * q, o[h][b]);
+            for (int b = 0; b < kBlocks; ++b) tile.put(16 * (wave + WAVES * h) + r, 32 * b + 8 * q, o[h][b]);
     }
     if constexpr (BY_ROWS) {
         const int64_t piece0 = row0 / 16 * col_pieces + col0 / 128;
         const int block0 = BY_COLS ? (int)(col0 >> 5 & 3) : 0;               // of the piece
 #pragma unroll
-        for (int h = 0; h < kRows / 64; ++h) {
-            const int group = wave + 4 * h;
+        for (int h = 0; h < kTurns; ++h) {
+            const int group = wave + WAVES * h;
             const int64_t row = row0 + 16 * group + r;
             if (row0 + 16 * group >= padded_rows) continue;
 #pragma unroll
@@ -206,7 +207,7 @@ __global__ __launch_bounds__(kThreads) void k_mx_quantise(MxQuantArgs a, int64_t
                 const uint32_t octet = (uint32_t)row * per_row + (uint32_t)((col0 + 32 * b + 8 * q) >> 3);
                 const uint32_t c = quantise_octet<STOCHASTIC>(v, quad_largest(largest(v)), a.draws, octet, byte);
                 *reinterpret_cast<uint32_t *>(a.by_rows.codes + (piece0 + group * col_pieces) * 1024 + (block0 + b) * 256 + lane * 4) = c;
-                if (q == 0) scales[0][h * 64 * kBlocks + b * 64 + r * 4 + wave] = (uint8_t)byte;
+                if (q == 0) scales[0][(group >> 2) * 64 * kBlocks + b * 64 + r * 4 + (group & 3)] = (uint8_t)byte;
             }
         }
     }
@@ -214,19 +215,20 @@ __global__ __launch_bounds__(kThreads) void k_mx_quantise(MxQuantArgs a, int64_t
     if constexpr (BY_COLS) {
         Draws d = a.draws;
         d.word += kMxColWord - kMxRowWord;
-        const int c16 = lane & 15, q16 = lane >> 4;
-        const int64_t col = col0 + 16 * wave + c16;                          // a row of the turned matrix
+        const int c16 = lane & 15, q16 = lane >> 4, strip = wave & 3;
+        const int64_t col = col0 + 16 * strip + c16;                          // a row of the turned matrix
         if (col0 < padded_cols) {
-            uint8_t *codes = a.by_cols.codes + ((col0 / 16 + wave) * row_pieces + row0 / 128) * 1024 + c16 * 16 + q16 * 4;
+            uint8_t *codes = a.by_cols.codes + ((col0 / 16 + strip) * row_pieces + row0 / 128) * 1024 + c16 * 16 + q16 * 4;
 #pragma unroll
-            for (int b = 0; b < 4; ++b) {
+            for (int i = 0; i < 16 / WAVES; ++i) {
+                const int b = (wave >> 2) * (16 / WAVES) + i;
                 Values v;
-                tile.get(32 * b + 8 * q16, 16 * wave, lane, v);
+                tile.get(32 * b + 8 * q16, 16 * strip, lane, v);
                 uint32_t byte;
                 const uint32_t octet = (uint32_t)col * per_col + (uint32_t)((row0 + 32 * b + 8 * q16) >> 3);
                 const uint32_t c = quantise_octet<STOCHASTIC>(v, rows_largest(largest(v)), d, octet, byte);
                 *reinterpret_cast<uint32_t *>(codes + b * 256) = c;
-                if (q16 == 0) scales[1][b * 64 + c16 * 4 + wave] = (uint8_t)byte;
+                if (q16 == 0) scales[1][b * 64 + c16 * 4 + strip] = (uint8_t)byte;
             }
         }
         __syncthreads();
@@ -294,13 +296,21 @@ void launch_mx_quantise(const MxQuantArgs &a, bool bf16, hipStream_t st)
     const dim3 grid((unsigned)((a.by_cols.codes ? row_pieces : padded_rows / 64) * col_tiles));
     by_bool(bf16, [&](auto b) {
         by_bool(a.stochastic != 0, [&](auto s) {
-            auto go = [&](auto rows, auto cols) {
-                hipLaunchKernelGGL((k_mx_quantise<decltype(b)::value, decltype(s)::value, decltype(rows)::value, decltype(cols)::value>),
-                                   grid, dim3(kThreads), 0, st, a, row_pieces, col_pieces, col_tiles, padded_rows, padded_cols);
+            auto go = [&](auto rows, auto cols, auto waves) {
+                constexpr int W = decltype(waves)::value;
+                hipLaunchKernelGGL((k_mx_quantise<decltype(b)::value, decltype(s)::value, decltype(rows)::value, decltype(cols)::value, W>),
+                                   grid, dim3(64 * W), 0, st, a, row_pieces, col_pieces, col_tiles, padded_rows, padded_cols);
             };
-            if (!a.by_cols.codes) go(std::true_type{}, std::false_type{});
-            else if (!a.by_rows.codes) go(std::false_type{}, std::true_type{});
-            else go(std::true_type{}, std::true_type{});
+            const std::integral_constant<int, 4> four;
+            auto by_cols = [&](auto waves) {
+                if (a.by_rows.codes) go(std::true_type{}, std::true_type{}, waves);
+                else go(std::false_type{}, std::true_type{}, waves);
+            };
+            // Eight waves to a tile while there are at most two tiles a CU, which is when a tile's latency counts.  us: 1000 x 515 fp32 3.1 / 3.8, stochastically
+            // 4.3 / 5.0, 2048 x 2048 bf16 6.3 / 6.5; but 8192 x 8192 bf16 64.8 / 60.2.
+            if (!a.by_cols.codes) go(std::true_type{}, std::false_type{}, four);
+            else if (grid.x <= 512) by_cols(std::integral_constant<int, 8>{});
+            else by_cols(four);
         });
     });
 }

@@ -315,7 +315,7 @@ def test_norm_gradient_against_differences(env, rows, cols):
 
 # ---------------------------------------------------------------------------------------------- 4-bit floating point
 MX_SHAPES = [(1, 1), (1, 31), (3, 32), (2, 33), (15, 64), (16, 127), (17, 128), (63, 129), (64, 256), (65, 100), (130, 515), (1, 2048),
-             (300, 7), (128, 128), (129, 384)]
+             (300, 7), (128, 128), (129, 384), (1300, 3500)]
 
 
 def mx_input(rows, cols, bf16):
