@@ -256,7 +256,7 @@ __device__ __forceinline__ void finish_dz(const NormArgs &a, int64_t row, int64_
 
 // Each workgroup takes every gridDim-th row (or 256 / G of them) and keeps its share of dgamma and dbeta in registers, since a lane
 // sees the same columns in every row; k_norm_columns adds the shares.  The next row's octets are on their way while a row is worked on.
-// Bound by memory: 16384 x 2048 in bf16 with dropout and residual's gradient 60 us, 336 MB and 17 MB of shares at 5.9 TB/s, and 6 us for the
+// Bound by memory: 16384 x 2048 in bf16 with dropout and residual's gradient 58 us, 336 MB and 8 MB of shares at 5.9 TB/s, and 4 us for the
 // shares' sum; 777 x 5003 in fp32 19 us, 88 MB at 4.6 TB/s, and 4 us.
 template <bool BF16, int G, int V>
 __global__ __launch_bounds__(threads_of(G)) void k_norm_backward(NormArgs a)
@@ -500,16 +500,22 @@ void by_width(int64_t cols, F &&go)
 // us, so many / 2048: 777 x 5003 fp32 fused 20.6 / 22.9, 8192 x 1024 bf16 13.8 / 15.2, 4096 x 16384 bf16 102 / 118.
 constexpr int forward_groups(int g, int v) { return g * v > 640 ? 512 : g * v > 256 || v == 2 ? 768 : 1536; }
 
-// Workgroups of the backward pass: as many as the card holds at a time (four, two or one a CU, by their registers).
-int64_t most_parts(int64_t cols)
+// Workgroups of the backward pass of rows of that width: as many as the card holds at a time (four or two of 256 threads a CU, else two or one), but
+// four rows each (two of the widest) where that leaves one for a CU (every other one): their shares of dgamma and dbeta are written and read
+// again.  us with both kernels, so / with a row each: 1024 x 2048 bf16 11.3 / 18.0, 500 x 4000 bf16 12.5 / 17.6, 256 x 5003 fp32 12.8 / 15.8.  At most
+// 512 of 256 threads, or 1024: 16384 x 2048 bf16 fused 65 / 73 (not fused 42 / 41), fp32 134 / 139; 256 of 512 threads, or 512: 4096 x 4096
+// fp32 66 / 69, 16384 x 3500 fp32 208 / 228.
+int64_t parts_of(int64_t rows, int64_t cols)
 {
-    int64_t n = 512;
-    if (!in_registers(cols, kBackwardCols)) return n;
+    int64_t most = 512, few = 256, least = 4;
+    if (!in_registers(cols, kBackwardCols)) return std::min(rows, most);
     by_width<kBackwardLanes>(cols, [&](auto g, auto v) {
         constexpr int G = decltype(g)::value, V = decltype(v)::value;
-        n = G * V > 512 ? 256 : G > kThreads || V == 2 ? 512 : 1024;
+        if (G == 64) few = most = V == 1 ? 1024 : 512;
+        if (G >= 512) most = 256;
+        if (G * V > 512) few = 128, least = 2;
     });
-    return n;
+    return std::min({rows, std::max((rows + least - 1) / least, few), most});
 }
 
 template <typename F>
@@ -549,7 +555,7 @@ void launch_norm_forward(const NormArgs &a, bool bf16, hipStream_t st)
 
 int64_t norm_partials(int64_t rows, int64_t cols)
 {
-    return std::min(rows, most_parts(cols));
+    return parts_of(rows, cols);
 }
 
 void launch_norm_backward(const NormArgs &a, bool bf16, hipStream_t st)

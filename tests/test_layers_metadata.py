@@ -25,11 +25,11 @@ def test_tiles_of_the_product_leave_room_for_the_workgroups_that_a_cu_is_to_hold
 
 
 def test_backward_pass_of_the_norm_fits_its_workgroups(kernels):  # noqa: F811
-    """Launched as many workgroups to a CU as its registers allow in bf16: four of 256 threads with an octet a lane, one of more than 512
-    lanes' octets, else two; fp32 may take a wave less to a SIMD."""
+    """Launched as many workgroups to a CU as its registers allow in bf16: four of 256 threads with a wave and an octet a lane to a row, one of 512
+    threads and more, else two; fp32 may take a wave less to a SIMD."""
     for k, v in of(kernels, "k_norm_backward").items():
         bf16, lanes, octets = re.findall(r"[\w]+", k.split("<")[1])
         lanes, octets = int(lanes), int(octets)
-        groups = 1 if lanes * octets > 512 else 2 if lanes > 256 or octets == 2 else 4
+        groups = 1 if lanes >= 512 else 2 if lanes > 64 or octets == 2 else 4
         waves = -(-groups * max(lanes, 256) // 256)
         assert v["vgprs"] <= 512 // (waves if bf16 == "true" else max(2, waves - 1)) // 8 * 8, (k, v)
