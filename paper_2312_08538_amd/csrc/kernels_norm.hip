@@ -18,9 +18,9 @@ namespace conef {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kForwardCols = 16384, kBackwardCols = 8192;       // the widest rows that a workgroup holds in registers
+constexpr int kForwardCols = 16384, kBackwardCols = 12288;      // the widest rows that a workgroup holds in registers
 
-inline bool in_registers(int64_t cols, int most) { return cols >= 8 && cols <= most; }
+inline bool in_registers(int64_t cols, int most) { return cols <= most; }
 
 // threads of a workgroup in which G share a row
 constexpr int threads_of(int g) { return g > kThreads ? g : kThreads; }
@@ -54,7 +54,7 @@ template <int G, int N>
 __device__ __forceinline__ void group_sum(float v[N], float *red, int &turn)
 {
 #pragma unroll
-    for (int i = 0; i < N; ++i) v[i] = lanes_sum(v[i]);
+    for (int i = 0; i < N; ++i) v[i] = lanes_sum<(G < 64 ? G : 64)>(v[i]);
     if constexpr (G > 64) {
         constexpr int W = G / 64;
         float *slot = red + turn * W * N;
@@ -77,15 +77,29 @@ __device__ __forceinline__ void group_sum(float v[N], float *red, int &turn)
     }
 }
 
+// A row's octets, begun and finished.  Rows of fewer than 8 columns, which have eight lanes, are loaded element by element.
+template <bool BF16, int G>
+__device__ __forceinline__ void begin(Octet<BF16> &o, const void *data, int64_t at, int left, int cols)
+{
+    if (G == 8 && cols < 8) o = fetch_octet<BF16>(data, at, left);
+    else begin_octet<BF16>(o, data, at, left);
+}
+template <bool BF16, int G>
+__device__ __forceinline__ void finish(const Octet<BF16> &o, int left, int cols, float v[8])
+{
+    if (G == 8 && cols < 8) widen<BF16>(o, v);
+    else finish_octet<BF16>(o, left, v);
+}
+
 // a row's gamma or beta, laid out like the row
 template <int G, int V>
 __device__ __forceinline__ void load_columns(const float *p, int cols, int t, float out[V][8])
 {
     Octet<false> o[V] = {};
 #pragma unroll
-    for (int v = 0; v < V; ++v) begin_octet<false>(o[v], p, 8 * (t + G * v), cols - 8 * (t + G * v));
+    for (int v = 0; v < V; ++v) begin<false, G>(o[v], p, 8 * (t + G * v), cols - 8 * (t + G * v), cols);
 #pragma unroll
-    for (int v = 0; v < V; ++v) finish_octet<false>(o[v], cols - 8 * (t + G * v), out[v]);
+    for (int v = 0; v < V; ++v) finish<false, G>(o[v], cols - 8 * (t + G * v), cols, out[v]);
 }
 
 // G lanes hold a row, V octets each: octet v of lane t starts at column 8 (t + G v).  The next row's octets are on their way while a row is
@@ -107,8 +121,8 @@ __global__ __launch_bounds__(threads_of(G)) void k_norm_forward(NormArgs a)
 #pragma unroll
         for (int v = 0; v < V; ++v) {
             const int col = 8 * (t + G * v), left = from < a.rows ? a.cols - col : 0;
-            begin_octet<BF16>(x[v], a.x.data, from * a.x.pitch + col, left);
-            if (FUSED && a.residual.data) begin_octet<BF16>(r[v], a.residual.data, from * a.residual.pitch + col, left);
+            begin<BF16, G>(x[v], a.x.data, from * a.x.pitch + col, left, a.cols);
+            if (FUSED && a.residual.data) begin<BF16, G>(r[v], a.residual.data, from * a.residual.pitch + col, left, a.cols);
         }
     };
     fetch(row);
@@ -120,12 +134,12 @@ __global__ __launch_bounds__(threads_of(G)) void k_norm_forward(NormArgs a)
 #pragma unroll
         for (int v = 0; v < V; ++v) {
             const int col = 8 * (t + G * v);
-            finish_octet<BF16>(x[v], a.cols - col, z[v]);
+            finish<BF16, G>(x[v], a.cols - col, a.cols, z[v]);
             if constexpr (FUSED) {
                 if (a.drop) drop_octet(a.d, (uint32_t)row * per_row + (uint32_t)(t + G * v), z[v]);
                 if (a.residual.data) {
                     float add[8];
-                    finish_octet<BF16>(r[v], a.cols - col, add);
+                    finish<BF16, G>(r[v], a.cols - col, a.cols, add);
 #pragma unroll
                     for (int i = 0; i < 8; ++i) z[v][i] = add[i] + z[v][i];
                 }
@@ -263,7 +277,9 @@ __global__ __launch_bounds__(threads_of(G)) void k_norm_backward(NormArgs a)
 {
     constexpr int kRows = threads_of(G) / G;
     __shared__ float red[G > 64 ? 4 * G / 64 : 1];
-    __shared__ float share[G > 64 ? 1 : 2 * 8 * G * V];
+    constexpr bool kInLds = G >= 768 && V == 2;         // the shares, which registers do not hold; nor,
+    constexpr bool kAhead = !kInLds || (BF16 && G == 768);          // of these but some, the next row
+    __shared__ float share[G > 64 && !kInLds ? 1 : 2 * 8 * G * V];
     int turn = 0;
     const int t = threadIdx.x % G;
     const float inv = 1.0f / (float)a.cols;
@@ -280,15 +296,23 @@ __global__ __launch_bounds__(threads_of(G)) void k_norm_backward(NormArgs a)
 #pragma unroll
         for (int v = 0; v < V; ++v) {
             const int col = 8 * (t + G * v), left = from < a.rows ? a.cols - col : 0;
-            begin_octet<BF16>(z_next[v], a.z_in.data, from * a.z_in.pitch + col, left);
-            begin_octet<BF16>(dy_next[v], a.dy.data, from * a.dy.pitch + col, left);
-            if (a.dz_in.data) begin_octet<BF16>(in_next[v], a.dz_in.data, from * a.dz_in.pitch + col, left);
+            begin<BF16, G>(z_next[v], a.z_in.data, from * a.z_in.pitch + col, left, a.cols);
+            begin<BF16, G>(dy_next[v], a.dy.data, from * a.dy.pitch + col, left, a.cols);
+            if (a.dz_in.data) begin<BF16, G>(in_next[v], a.dz_in.data, from * a.dz_in.pitch + col, left, a.cols);
         }
     };
-    fetch(row);
+    if constexpr (kAhead) fetch(row);
     float gamma[V][8], dgamma[V][8] = {}, dbeta[V][8] = {};
     load_columns<G, V>(a.gamma, a.cols, t, gamma);
+    // (element i of lane t's octet v in place (8 v + i) G + t, so that neighbours lie in neighbouring banks)
+    auto place = [&](int v, int i) -> float * { return share + (v * 8 + i) * G + t; };
+    if constexpr (kInLds)
+#pragma unroll
+        for (int v = 0; v < V; ++v)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) place(v, i)[0] = place(v, i)[8 * G * V] = 0.0f;
     for (; row < a.rows; row += stride) {
+        if constexpr (!kAhead) fetch(row);
         Octet<BF16> z[V], dy[V], in[V];
         const float mean = mean_next, rstd = rstd_next;
 #pragma unroll
@@ -297,22 +321,28 @@ __global__ __launch_bounds__(threads_of(G)) void k_norm_backward(NormArgs a)
             dy[v] = dy_next[v];
             in[v] = in_next[v];
         }
-        fetch(row + stride);
+        if constexpr (kAhead) fetch(row + stride);
         float sums[2] = {0.0f, 0.0f};
 #pragma unroll
         for (int v = 0; v < V; ++v) {
             float zv[8], dv[8], hat[8], w[8];
             const int left = a.cols - 8 * (t + G * v);
-            finish_octet<BF16>(z[v], left, zv);
-            finish_octet<BF16>(dy[v], left, dv);
+            finish<BF16, G>(z[v], left, a.cols, zv);
+            finish<BF16, G>(dy[v], left, a.cols, dv);
             hat_and_a(zv, dv, gamma[v], mean, rstd, hat, w);
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 // (columns beyond the row's end have dy = gamma = 0)
                 sums[0] += w[i];
                 sums[1] = __builtin_fmaf(w[i], hat[i], sums[1]);
-                dgamma[v][i] = __builtin_fmaf(dv[i], hat[i], dgamma[v][i]);
-                dbeta[v][i] += dv[i];
+                if constexpr (kInLds) {
+                    float *p = place(v, i);
+                    p[0] = __builtin_fmaf(dv[i], hat[i], p[0]);
+                    p[8 * G * V] += dv[i];
+                } else {
+                    dgamma[v][i] = __builtin_fmaf(dv[i], hat[i], dgamma[v][i]);
+                    dbeta[v][i] += dv[i];
+                }
             }
         }
         if (a.dz.data || a.dx.data) {
@@ -322,12 +352,12 @@ __global__ __launch_bounds__(threads_of(G)) void k_norm_backward(NormArgs a)
             for (int v = 0; v < V; ++v) {
                 float zv[8], dv[8], hat[8], w[8], add[8];
                 const int col = 8 * (t + G * v), left = a.cols - col;
-                finish_octet<BF16>(z[v], left, zv);
-                finish_octet<BF16>(dy[v], left, dv);
+                finish<BF16, G>(z[v], left, a.cols, zv);
+                finish<BF16, G>(dy[v], left, a.cols, dv);
                 hat_and_a(zv, dv, gamma[v], mean, rstd, hat, w);
 #pragma unroll
                 for (int i = 0; i < 8; ++i) w[i] = rstd * ((w[i] - m0) - hat[i] * m1);
-                if (a.dz_in.data) finish_octet<BF16>(in[v], left, add);
+                if (a.dz_in.data) finish<BF16, G>(in[v], left, a.cols, add);
                 finish_dz<BF16>(a, row, col, left, (uint32_t)row * per_row + (uint32_t)(t + G * v), add, w);
             }
         }
@@ -338,19 +368,31 @@ __global__ __launch_bounds__(threads_of(G)) void k_norm_backward(NormArgs a)
 #pragma unroll
         for (int v = 0; v < V; ++v) {
             const int col = 8 * (t + G * v);
+            if constexpr (kInLds)
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    dgamma[v][i] = place(v, i)[0];
+                    dbeta[v][i] = place(v, i)[8 * G * V];
+                }
             store_octet<false>(out, col, a.cols - col, dgamma[v]);
             store_octet<false>(out + a.cols, col, a.cols - col, dbeta[v]);
         }
     } else {
-        // the workgroup's groups one after the other, then columns of the sum by all threads
-        for (int g = 0; g < kRows; ++g) {
-            if ((int)threadIdx.x / G == g)
+        // the rows of a wave, the workgroup's waves one after the other, then columns of the sum by all threads
+#pragma unroll
+        for (int v = 0; v < V; ++v)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                dgamma[v][i] = places_sum<G>(dgamma[v][i]);
+                dbeta[v][i] = places_sum<G>(dbeta[v][i]);
+            }
+        for (int g = 0; g < kThreads / 64; ++g) {
+            if ((int)threadIdx.x / 64 == g && (threadIdx.x & 63) < G)
 #pragma unroll
                 for (int v = 0; v < V; ++v)
 #pragma unroll
                     for (int i = 0; i < 8; ++i) {
-                        // (a row's octets: element i of lane t in place i G + t, so that neighbours lie in neighbouring banks)
-                        float *p = share + (v * 8 + i) * G + t, *q = p + 8 * G * V;
+                        float *p = place(v, i), *q = p + 8 * G * V;
                         *p = g ? *p + dgamma[v][i] : dgamma[v][i];
                         *q = g ? *q + dbeta[v][i] : dbeta[v][i];
                     }
@@ -364,8 +406,8 @@ __global__ __launch_bounds__(threads_of(G)) void k_norm_backward(NormArgs a)
     }
 }
 
-// Rows of any length: two sweeps by a workgroup; the sums over rows are k_norm_column_parts's, which reads dy and z once more: with it 4096 x 16384 in
-// bf16 takes 235 us.  (Held in the registers of 1024 threads such rows spill: 378 us.)
+// Rows of more than 12288 columns: two sweeps by a workgroup; the sums over rows are k_norm_column_parts's, which reads dy and z once more: with it 4096 x 16384 in
+// bf16 takes 235 us.  (1024 threads have 128 registers each, too few for an fp32 row of 16384 even with the shares in LDS.)
 template <bool BF16>
 __global__ __launch_bounds__(kThreads) void k_norm_backward_long(NormArgs a)
 {
@@ -468,12 +510,16 @@ void by_lanes(int64_t cols, F &&go)
     else if constexpr (8 * G < MOST) by_lanes<G + 128, MOST>(cols, go);
 }
 
-// Lanes to a row and octets a lane: at most two, which registers hold together with the next row on its way.  A wave to a row needs no barrier, but
+// Lanes to a row and octets a lane.  Rows of up to 256 columns share a wave, 8 to 32 lanes each: 32768 x 100 in bf16 forward 9.0 us, backward 16.3 with both
+// kernels, a wave to a row 19 and 29; 32768 x 7, which eight lanes load element by element, 5.7 and 14, by a workgroup to a row 78 and 118.
+// Otherwise two octets a lane at most, which registers hold together with the next row on its way.  A wave to a row needs no barrier, but
 // four octets a lane (2048 columns) take 256 registers: the backward pass of 16384 x 2048 in bf16 then takes 86 us, with a workgroup to
 // a row 75.  Rows of 2048 columns to MOST take one octet a lane: up to 8192 in the fused forward pass, 6144 in the backward pass, whose registers hold
 // no more.  us, so / 256 or 512 lanes of two: forward 777 x 5003 fp32 17.8 / 20.7, 8192 x 5120 bf16 65 / 72, 4096 x 7000 fp32 89 / 102, 8192 x 2560
 // bf16 34 / 38, 4096 x 8192 bf16 52 / 50; backward 777 x 5003 fp32 23 / 26, 8192 x 5120 bf16 93 / 106, 16384 x 3000 bf16 100 / 115, 8192 x 4096
 // fp32 133 / 135.  A forward pass that is not fused has little to hold: 777 x 5003 fp32 11.0 / 9.9, 8192 x 5120 bf16 39 / 37.
+// Beyond 8192 768 lanes or 1024: forward 3000 x 10000 bf16 51 / 58, 2000 x 10000 fp32 70 / 69, 300 x 12000 fp32 17.6 / 20.0; backward, with shares in LDS,
+// 768 or, as any other length, in two sweeps: 3000 x 10000 bf16 71 / 119, 2000 x 10000 fp32 95 / 149.
 constexpr int kFusedLanes = 8192, kBackwardLanes = 6144, kPairs = 0;
 
 template <int MOST, typename F>
@@ -482,7 +528,10 @@ void by_width(int64_t cols, F &&go)
     using std::integral_constant;
     typedef integral_constant<int, 1> One;
     typedef integral_constant<int, 2> Two;
-    if (cols <= 512) go(integral_constant<int, 64>{}, One{});
+    if (cols <= 64) go(integral_constant<int, 8>{}, One{});
+    else if (cols <= 128) go(integral_constant<int, 16>{}, One{});
+    else if (cols <= 256) go(integral_constant<int, 32>{}, One{});
+    else if (cols <= 512) go(integral_constant<int, 64>{}, One{});
     else if (cols <= 1024) go(integral_constant<int, 64>{}, Two{});
     else if (cols <= 2048) go(integral_constant<int, 256>{}, One{});
     else if (cols <= MOST) {
@@ -491,6 +540,8 @@ void by_width(int64_t cols, F &&go)
         if constexpr (MOST < 4096) go(integral_constant<int, 256>{}, Two{});
     } else if (cols <= 8192) {
         if constexpr (MOST < 8192) go(integral_constant<int, 512>{}, Two{});
+    } else if (cols <= 12288) {
+        go(integral_constant<int, 768>{}, Two{});
     } else {
         if constexpr (MOST != kBackwardLanes) go(integral_constant<int, 1024>{}, Two{});      // (the backward pass has no rows as wide)
     }
@@ -501,7 +552,7 @@ void by_width(int64_t cols, F &&go)
 constexpr int forward_groups(int g, int v) { return g * v > 640 ? 512 : g * v > 256 || v == 2 ? 768 : 1536; }
 
 // Workgroups of the backward pass of rows of that width: as many as the card holds at a time (four or two of 256 threads a CU, else two or one), but
-// four rows each (two of the widest) where that leaves one for a CU (every other one): their shares of dgamma and dbeta are written and read
+// four rows each (two of more than 512 lanes) where that leaves one for a CU (every other one): their shares of dgamma and dbeta are written and read
 // again.  us with both kernels, so / with a row each: 1024 x 2048 bf16 11.3 / 18.0, 500 x 4000 bf16 12.5 / 17.6, 256 x 5003 fp32 12.8 / 15.8.  At most
 // 512 of 256 threads, or 1024: 16384 x 2048 bf16 fused 65 / 73 (not fused 42 / 41), fp32 134 / 139; 256 of 512 threads, or 512: 4096 x 4096
 // fp32 66 / 69, 16384 x 3500 fp32 208 / 228.
@@ -512,6 +563,7 @@ int64_t parts_of(int64_t rows, int64_t cols)
     by_width<kBackwardLanes>(cols, [&](auto g, auto v) {
         constexpr int G = decltype(g)::value, V = decltype(v)::value;
         if (G == 64) few = most = V == 1 ? 1024 : 512;
+        if (G < 64) few = most;
         if (G >= 512) most = 256;
         if (G * V > 512) few = 128, least = 2;
     });

@@ -199,17 +199,40 @@ __device__ __forceinline__ float dpp(float v)
     return __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(v), CTRL, 0xF, 0xF, true));
 }
 
-// sum over the 64 lanes of a wave, in every lane: quads, halves and wholes of a row of 16, then across the rows
+// sum over each G lanes of a wave, in every one of them: quads, halves and wholes of a row of 16, then across the rows
+template <int G>
 __device__ __forceinline__ float lanes_sum(float v)
 {
+    static_assert(G == 8 || G == 16 || G == 32 || G == 64, "");
     v += dpp<0xB1>(v);          // lane ^ 1
     v += dpp<0x4E>(v);          // lane ^ 2
     v += dpp<0x141>(v);         // the other quad of a half row
-    v += dpp<0x140>(v);         // the other half row
-    auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-    v = __uint_as_float(r[0]) + __uint_as_float(r[1]);
-    r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-    return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+    if constexpr (G >= 16) v += dpp<0x140>(v);         // the other half row
+    if constexpr (G >= 32) {
+        auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+        v = __uint_as_float(r[0]) + __uint_as_float(r[1]);
+    }
+    if constexpr (G == 64) {
+        auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+        v = __uint_as_float(r[0]) + __uint_as_float(r[1]);
+    }
+    return v;
+}
+
+// sum over the 64 / G lanes of a wave with the same place in their G, in every one of them
+template <int G>
+__device__ __forceinline__ float places_sum(float v)
+{
+    if constexpr (G <= 8) v += dpp<0x128>(v);          // half a row on
+    if constexpr (G <= 16) {
+        auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+        v = __uint_as_float(r[0]) + __uint_as_float(r[1]);
+    }
+    if constexpr (G <= 32) {
+        auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+        v = __uint_as_float(r[0]) + __uint_as_float(r[1]);
+    }
+    return v;
 }
 
 }  // namespace conef

@@ -115,7 +115,8 @@ def test_dropout_keeps_its_share_and_changes_with_site_step_and_seed(env):
 # ---------------------------------------------------------------------------------------------- layer norm
 NORM_SHAPES = [(1, 1), (3, 2), (5, 7), (4, 8), (7, 9), (2, 63), (300, 64), (9, 65), (5, 511), (6, 512), (1030, 513), (1, 768), (33, 1001),
                (4, 1024), (3, 1025), (1, 2048), (700, 2049), (2, 4096), (3, 5003), (5, 8192), (2, 8193), (3, 16384), (2, 16385), (3, 20001),
-               (600, 3071), (2, 3073), (3, 4097), (2, 5120), (5, 5121), (2, 6144), (300, 6145), (3, 7168), (800, 7169), (1100, 1500), (1500, 2500)]
+               (600, 3071), (2, 3073), (3, 4097), (2, 5120), (5, 5121), (2, 6144), (300, 6145), (3, 7168), (800, 7169), (1100, 1500), (1500, 2500),
+               (20000, 5), (17001, 33), (16, 128), (9000, 129), (2049, 255), (40, 257), (300, 12288), (3, 12289)]
 
 
 def norm_inputs(rows, cols, bf16, key=0):

@@ -30,6 +30,6 @@ def test_backward_pass_of_the_norm_fits_its_workgroups(kernels):  # noqa: F811
     for k, v in of(kernels, "k_norm_backward").items():
         bf16, lanes, octets = re.findall(r"[\w]+", k.split("<")[1])
         lanes, octets = int(lanes), int(octets)
-        groups = 1 if lanes >= 512 else 2 if lanes > 64 or octets == 2 else 4
+        groups = 1 if lanes >= 512 else 4 if (lanes, octets) == (64, 1) else 2
         waves = -(-groups * max(lanes, 256) // 256)
         assert v["vgprs"] <= 512 // (waves if bf16 == "true" else max(2, waves - 1)) // 8 * 8, (k, v)
