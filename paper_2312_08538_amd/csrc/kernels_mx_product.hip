@@ -576,13 +576,16 @@ struct Choice {
 constexpr int kCus = 256;
 
 // Which kernel, and whether C goes past the caches.  us of a call (bf16 C unless said otherwise), the one taken / the next best:
-//   rows (m <= 64)   8 x 8192 x 2048 2.7 / 4.8 tiny, 1 x 50304 x 2048 11.3 / 11.8 small, 64 x 2048 x 8192 5.4 / 9.8 tiny in 4 parts
+//   rows (m <= 64)   8 x 8192 x 2048 2.7 / 4.8 tiny, 1 x 50304 x 2048 11.3 / 11.8 small, 64 x 2048 x 8192 5.4 / 9.8 tiny in 4 parts; but more
+//                    than 16 rows are read once a workgroup, which with enough of these costs more than a tile's waste: 64 x 50304 x 16384 166 / 86
+//                    small, 32 x 16384 x 8192 15.1 / 13.3, 64 x 50304 x 2048 21.6 / 19.4 (32 x 50304 x 2048 14.5 / 17.7)
 //   stream, 256 x 256, one tile after the other, from four to a CU on:  8192 x 8192 x 8192 240 / 249 large, 4096 x 50304 x 2048 215 / 224 wide,
 //                    8192 x 8192 x 1536 53 / 58 wide, 16384 x 8192 x 4096 241 / 261 large; but 6144 x 4096 x 2048 33 / 28 wide
 //   large, 256 x 256, eight waves: the fewest reads, but a CU holds one workgroup, which begins and ends alone; for long sums of fewer
 //                    tiles: 8192 x 2048 x 8192 62 / 71 wide, 64 stream
 //   wide, 256 x 128, two workgroups a CU:  4096 x 8192 x 2048 38.7 / 38.1 stream; 8192 x 32768 x 1024 184 small / 190
-//   small, 128 x 128, three a CU:  2048 x 50304 x 768 65 / 69 wide, 2048 x 2048 x 16384 43 / 56 in 2 parts, 60 tiny; 512 x 8192 x 2048 9.4 / 11.8 tiny
+//   small, 128 x 128, three a CU:  2048 x 50304 x 768 65 / 69 wide, 2048 x 2048 x 16384 43 / 56 in 2 parts, 60 tiny; 512 x 8192 x 2048 9.4 / 11.8 tiny; and where half
+//                    of a larger one would be beyond the rows: 128 x 50304 x 8192 37 / 50 large
 //   tiny, 64 x 64, where small ones do not reach every CU:  1024 x 1024 x 1024 4.0 / 5.6, 16384 x 16 x 4096 8.4 / 11.7, 128 x 4096 x 1024 3.8 / 5.5
 // The long axis in parts, added up by a launch of its own: 256 x 256 x 8192 9.4 in 4 parts / 12.6, but 200 x 1024 x 4096 8.7 in 2 / 7.6.
 // Past the caches what those of the dies do not hold: 8192 x 32768 x 1024 184 / 270, 8192 x 8192 x 2048 in fp32 88 / 97, 4096 x 8192 x 2048 42 / 43;
@@ -591,8 +594,9 @@ Choice choose(int64_t m, int64_t n, int64_t k)
 {
     const int64_t pieces = std::max<int64_t>((k + 127) / 128, 1);
     auto tiles = [&](int64_t tm, int64_t tn) { return ((m + tm - 1) / tm) * ((n + tn - 1) / tn); };
-    if (m <= 64) return {kRows, 1, (int)pieces};
-    if (tiles(256, 256) >= 192 && pieces >= 12) return {tiles(256, 256) >= 4 * kCus ? kStream : pieces >= 32 ? kLarge : kWide, 1, (int)pieces};
+    const bool deep = m > 16 && tiles(64, 64) >= kCus && (m + 15) / 16 * pieces >= 64;
+    if (m <= 64 && !deep) return {kRows, 1, (int)pieces};
+    if (std::min(m, n) > 128 && tiles(256, 256) >= 192 && pieces >= 12) return {tiles(256, 256) >= 4 * kCus ? kStream : pieces >= 32 ? kLarge : kWide, 1, (int)pieces};
     if (tiles(128, 128) >= 200) return {kSmall, 1, (int)pieces};
     const int64_t parts = pieces < 64 ? 1 : std::max<int64_t>(std::min<int64_t>(kCus / tiles(64, 64), pieces / 16), 1);
     const int64_t per = (pieces + parts - 1) / parts;

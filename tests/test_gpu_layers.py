@@ -437,7 +437,8 @@ def test_product(env, m, n, k, bf16, alpha, beta):
     c.check_canary()
 
 
-@pytest.mark.parametrize("m,n,k", [(2000, 1700, 300), (3500, 3600, 1537), (3500, 3600, 4200), (8200, 8190, 1537), (1000, 65700, 1700)])
+@pytest.mark.parametrize("m,n,k", [(2000, 1700, 300), (3500, 3600, 1537), (3500, 3600, 4200), (8200, 8190, 1537), (1000, 65700, 1700),
+                                   (60, 16400, 1990)])
 @pytest.mark.parametrize("bf16", [False, True])
 @pytest.mark.parametrize("alpha,beta", [(1.0, 0.0), (0.125, 1.0)])
 def test_large_product(env, m, n, k, bf16, alpha, beta):
