@@ -257,25 +257,39 @@ __device__ __forceinline__ void values(uint32_t c, uint32_t byte, float v[8])
         for (int i = 0; i < 8; ++i) v[i] = __uint_as_float(0x7FC00000u);
 }
 
-// What a packed operand stands for: 16 rows a wave, 128 columns, four lanes a block.  Bound by memory: 8192 x 8192 in bf16 28 us, 170 MB at 6.0 TB/s.
+// What a packed operand stands for: 16 rows a wave, 128 columns, so that a store writes whole lines (four lanes a block, 64 bytes of a line at a time: 29 us, in
+// fp32 111).  Bound by memory: 8192 x 8192 in bf16 26 us, 170 MB at 6.6 TB/s, in fp32 48, 304 MB at 6.3.
 template <bool BF16, bool PAST>
 __global__ __launch_bounds__(kThreads) void k_mx_dequantise(MxDequantArgs a, int64_t pieces, int64_t groups)
 {
     const int64_t p = (int64_t)blockIdx.x * (kThreads / 64) + (threadIdx.x >> 6);
     if (p >= groups * pieces) return;
     const int64_t group = p / pieces, tc = p - group * pieces;
-    const int lane = threadIdx.x & 63, r = lane >> 2, q = lane & 3;
-    const int64_t row = group * 16 + r;
-    const uint8_t *scales = a.in.scales + ((group >> 2) * pieces + tc) * 256 + r * 4 + (group & 3);
+    // a store: 8 rows of 128 bytes, 16 a lane
+    constexpr int kElements = BF16 ? 8 : 4, kAcross = 8 * kElements;
+    const int lane = threadIdx.x & 63, q = lane & 7;
 #pragma unroll
-    for (int b = 0; b < 4; ++b) {
-        const uint32_t c = *reinterpret_cast<const uint32_t *>(a.in.codes + p * 1024 + b * 256 + lane * 4);
-        const uint32_t byte = scales[b * 64];
-        const int64_t col = tc * 128 + 32 * b + 8 * q;
+    for (int i = 0; i < 2 * 128 / kAcross; ++i) {
+        const int r = (i & 1) * 8 + (lane >> 3), in_piece = (i >> 1) * kAcross + q * kElements, b = in_piece >> 5;
+        const uint8_t *at = a.in.codes + p * 1024 + b * 256 + r * 16 + (in_piece & 31) / 2;
+        const uint32_t c = BF16 ? *reinterpret_cast<const uint32_t *>(at) : *reinterpret_cast<const uint16_t *>(at);
+        const uint32_t byte = a.in.scales[((group >> 2) * pieces + tc) * 256 + b * 64 + r * 4 + (group & 3)];
+        const int64_t row = group * 16 + r, col = tc * 128 + in_piece, place = row * a.out.pitch + col;
         float v[8];
         values(c, byte, v);
-        if (row < a.rows && col < a.cols)
-            store_octet<BF16, PAST>(a.out.data, row * a.out.pitch + col, octet_left(a.cols - col), v);
+        if (row >= a.rows || col >= a.cols) continue;
+        if constexpr (BF16) {
+            store_octet<true, PAST>(a.out.data, place, octet_left(a.cols - col), v);
+        } else {
+            float *to = static_cast<float *>(a.out.data) + place;
+            if (col + 4 <= a.cols) {
+                store_16<PAST>(to, u32x4_any{__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3])});
+            } else {
+#pragma unroll
+                for (int e = 0; e < 3; ++e)
+                    if (col + e < a.cols) to[e] = v[e];
+            }
+        }
     }
 }
 
@@ -319,8 +333,11 @@ void launch_mx_dequantise(const MxDequantArgs &a, bool bf16, hipStream_t st)
 {
     const int64_t pieces = (a.cols + 127) / 128, groups = (a.rows + 15) / 16;
     const dim3 grid((unsigned)((pieces * groups + 3) / 4));
-    // values that the dies' caches do not hold go past them: 8192 x 8192 in bf16, another buffer each time, 29 / 54 us
-    const bool past = a.rows * a.cols * (bf16 ? 2 : 4) > (int64_t)32 << 20;
+    // Values that the dies' caches do not hold go past them: 8192 x 8192 in bf16, another buffer each time, 26 / 36 us; but not rows that end
+    // within 64 bytes, of which halves would be written twice: 16384 x 3000 in bf16 27 / 62.
+    const int64_t size = bf16 ? 2 : 4;
+    const bool whole = a.out.pitch * size % 64 == 0 && reinterpret_cast<uintptr_t>(a.out.data) % 64 == 0;
+    const bool past = whole && a.rows * a.cols * size > (int64_t)32 << 20;
     by_bool(bf16, [&](auto b) {
         by_bool(past, [&](auto p) {
             hipLaunchKernelGGL((k_mx_dequantise<decltype(b)::value, decltype(p)::value>), grid, dim3(kThreads), 0, st, a, pieces, groups);

@@ -590,6 +590,8 @@ constexpr int kCus = 256;
 // The long axis in parts, added up by a launch of its own: 256 x 256 x 8192 9.4 in 4 parts / 12.6, but 200 x 1024 x 4096 8.7 in 2 / 7.6.
 // Past the caches what those of the dies do not hold: 8192 x 32768 x 1024 184 / 270, 8192 x 8192 x 2048 in fp32 88 / 97, 4096 x 8192 x 2048 42 / 43;
 // large tiles and streams only what the card's last cache does not hold either: 4096 x 50304 x 2048 205 / 236, but 8192 x 8192 x 2048 75 / 67.
+// And not rows that end within 64 bytes, of which halves would be written twice (within 16 if the last cache does not hold C): 2000 x 50300 x 300
+// 46 / 89, 4096 x 50303 x 2048 290 / 336, 8192 x 16001 x 700 87 / 128; but 8192 x 32760 x 1024 218 past the caches / 280.
 Choice choose(int64_t m, int64_t n, int64_t k)
 {
     const int64_t pieces = std::max<int64_t>((k + 127) / 128, 1);
@@ -665,7 +667,9 @@ void launch_mx_product(const MxProductArgs &a, bool bf16, hipStream_t st)
         p.alpha = 1.0f;                     // (beta is for the launch that adds the parts)
         launch_tiles<false, false, false, 2, 2, 2, 2, 4, 4>(p, c, st);
     }
-    const bool past = a.m * a.n * (bf16 ? 2 : 4) > (int64_t)(c.tiles >= kLarge ? 256 : 32) << 20;
+    const int64_t size = bf16 ? 2 : 4, bytes = a.m * a.n * size, last = (int64_t)256 << 20;
+    const int64_t ends = (a.c.pitch * size) | (int64_t)reinterpret_cast<uintptr_t>(a.c.data);
+    const bool past = bytes > (c.tiles >= kLarge ? last : last / 8) && (ends % 64 == 0 || (ends % 16 == 0 && bytes > last));
     by_bool(bf16, [&](auto b) {
         by_bool(a.beta != 0.0f, [&](auto add) {
             constexpr bool B = decltype(b)::value, ADD = decltype(add)::value;
