@@ -476,7 +476,7 @@ __global__ __launch_bounds__(1024) void k_norm_columns(const float *partials, in
 {
     __shared__ double red[16][64];
     const int lane = threadIdx.x & 63, part = threadIdx.x >> 6;
-    const int64_t c = (int64_t)blockIdx.x * 64 + lane, n = 2 * (int64_t)cols;
+    const int64_t c = (int64_t)group_index() * 64 + lane, n = 2 * (int64_t)cols;
     double s = 0.0;
     if (c < n) {
         int p = part;
@@ -633,7 +633,7 @@ void launch_norm_backward(const NormArgs &a, bool bf16, hipStream_t st)
         });
     });
     if (a.dgamma || a.dbeta)
-        hipLaunchKernelGGL(k_norm_columns, dim3((unsigned)((2 * (int64_t)a.cols + 63) / 64)), dim3(1024), 0, st, a.partials, used, a.cols,
+        hipLaunchKernelGGL(k_norm_columns, grid_of((2 * (int64_t)a.cols + 63) / 64), dim3(1024), 0, st, a.partials, used, a.cols,
                            a.dgamma, a.dbeta);
 }
 

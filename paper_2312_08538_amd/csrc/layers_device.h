@@ -8,6 +8,16 @@
 
 namespace conef {
 
+// Workgroups of a launch that may need more of them than one axis of a grid counts (fewer than 2^32 threads): rows of 2^21, of up to 1024
+// threads each.  The last row may have some that are nobody's.
+constexpr int kGridRow = 21;
+inline dim3 grid_of(int64_t groups)
+{
+    const int64_t row = (int64_t)1 << kGridRow;
+    return groups <= row ? dim3((unsigned)groups) : dim3((unsigned)row, (unsigned)((groups + row - 1) >> kGridRow));
+}
+__device__ __forceinline__ uint32_t group_index() { return blockIdx.x + (blockIdx.y << kGridRow); }
+
 // Sixteen bytes at any address that an element may have: the hardware takes them in one access.
 typedef uint32_t u32x4_any __attribute__((ext_vector_type(4), aligned(2)));
 

@@ -186,6 +186,21 @@ def test_backward_outputs_in_the_place_of_their_inputs_and_alone(env, rows, cols
             assert torch.equal(got[k], want[k]), (columns, k)
 
 
+def test_sums_over_rows_of_more_than_2_27_columns(env):  # noqa: F811
+    """Two rows, of which every column's sums are two products and one addition."""
+    torch, B = env
+    cols = (1 << 27) + 40
+    g = torch.Generator(device="cuda:0").manual_seed(9)
+    dy, z = (torch.randn(2, cols, device="cuda:0", generator=g).bfloat16() for _ in range(2))
+    mean, rstd = torch.tensor([0.25, -0.5], device="cuda:0"), torch.tensor([2.0, 0.75], device="cuda:0")
+    dgamma, dbeta = torch.full((cols,), 7.0, device="cuda:0"), torch.full((cols,), 7.0, device="cuda:0")
+    ws = torch.empty(B.conef_norm_workspace(2, cols), dtype=torch.uint8, device="cuda:0")
+    B.conef_norm_backward(None, dy, z, torch.ones(cols, device="cuda:0"), mean, rstd, None, None, None, dgamma, dbeta, ws, B.Model.stream_handle())
+    term = dy.double() * ((z.double() - mean.double()[:, None]) * rstd.double()[:, None])
+    assert bool(((dgamma - term.sum(0)).abs() <= 4 * U * term.abs().sum(0)).all())
+    assert bool(((dbeta - dy.double().sum(0)).abs() <= U * dy.double().abs().sum(0)).all())
+
+
 # ---------------------------------------------------------------------------------------------- refusals
 def test_each_refusal_says_what_does_not_fit(env):  # noqa: F811
     """None of these reaches a kernel."""

@@ -1,0 +1,67 @@
+"""Launches of a training step's operators at the ends of their documented ranges, without a GPU: a library that stands in for the
+runtime's launch calls records them (tests/launch_probe.cpp).  A launch counts fewer than 2^32 threads along each axis."""
+import json
+import os
+import subprocess
+import sys
+
+import pytest
+
+HERE = os.path.dirname(os.path.abspath(__file__))
+P = 4096           # an address that is never read: nothing is launched
+
+RECORD = """
+import ctypes, json, sys
+probe = ctypes.CDLL(sys.argv[1], mode=ctypes.RTLD_GLOBAL)
+sys.path.insert(0, sys.argv[2])
+from paper_2312_08538_amd import binding as B
+L = B.lib()
+assert probe.probe_kernels() > 100          # the library's kernels are known to the probe, so its launches go there too
+probe.probe_launch.restype = ctypes.c_char_p
+out = []
+for name, args in json.loads(sys.stdin.read()):
+    probe.probe_clear()
+    d = B.conef_drop(p=0.25, site=0, seed=1, step=0)
+    code = getattr(L, name)(*[ctypes.byref(d) if a == "drop" else a for a in args])
+    v = (ctypes.c_uint32 * 6)()
+    launches = [(probe.probe_launch(i, v).decode(), *v) for i in range(probe.probe_launches())]
+    out.append([code, launches])
+print(json.dumps(out))
+"""
+
+
+@pytest.fixture(scope="module")
+def record(tmp_path_factory):
+    """record([(call, arguments), ...]): [(code, [(kernel, grid x, y, z, block x, y, z), ...]), ...]"""
+    so = tmp_path_factory.mktemp("probe") / "launch_probe.so"
+    subprocess.run(["g++", "-std=c++17", "-O1", "-shared", "-fPIC", "-o", str(so), os.path.join(HERE, "launch_probe.cpp")], check=True)
+
+    def go(calls):
+        run = subprocess.run([sys.executable, "-c", RECORD, str(so), os.path.dirname(HERE)], input=json.dumps(calls), check=True,
+                             capture_output=True, text=True)
+        return json.loads(run.stdout)
+
+    return go
+
+
+def groups(launch):
+    _, gx, gy, gz, bx, by, bz = launch
+    for g, b in ((gx, bx), (gy, by), (gz, bz)):
+        assert 0 < g * b < 1 << 32, launch
+    return gx * gy * gz
+
+
+def launches_of(record, call, kernel):
+    (code, seen), = record([call])
+    assert code == 0
+    sizes = [groups(launch) for launch in seen]
+    found = [n for n, launch in zip(sizes, seen) if kernel in launch[0]]
+    assert found, seen
+    return found
+
+
+@pytest.mark.parametrize("cols", [1, 64, 1 << 20, (1 << 27) - 32, 1 << 27, (1 << 27) + 5, (1 << 31) - 1])
+def test_sums_over_rows_of_any_width(record, cols):
+    n, = launches_of(record, ("conef_norm_backward", [None, 1, cols, 0, P, cols, P, cols, P, P, P, 0, 0, P, cols, 0, 0, P, P, P, 0]),
+                     "k_norm_columns")
+    assert n * 64 >= 2 * cols
