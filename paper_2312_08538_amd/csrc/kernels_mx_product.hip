@@ -502,7 +502,8 @@ __global__ __launch_bounds__(64 * WAVES) void k_mx_rows(MxProductArgs a, int pie
 {
     __shared__ f32x4 sums[WAVES][MT][64];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int64_t group = blockIdx.x;
+    const int64_t group = group_index();
+    if (group * 16 >= a.n) return;
     const uint8_t *b = a.b.codes + group * pieces * 1024 + lane * 16, *eb = a.b.scales + (group >> 2) * pieces * 256 + lane * 4;
     const uint8_t *ac = a.a.codes + lane * 16, *ea = a.a.scales + lane * 4;
     const int shift = (int)(group & 3) * 8;
@@ -640,7 +641,7 @@ void launch_rows(const MxProductArgs &a, hipStream_t st)
     const int pieces = (int)((a.k + 127) / 128);
     auto go = [&](auto mt, auto waves) {
         constexpr int W = decltype(waves)::value;
-        hipLaunchKernelGGL((k_mx_rows<BF16, ADD, decltype(mt)::value, W>), dim3((unsigned)groups), dim3(64 * W), 0, st, a, pieces);
+        hipLaunchKernelGGL((k_mx_rows<BF16, ADD, decltype(mt)::value, W>), grid_of(groups), dim3(64 * W), 0, st, a, pieces);
     };
     auto by_waves = [&](auto mt) {
         if (pieces > 4 && (groups < 2 * kCus || pieces >= 64)) go(mt, std::integral_constant<int, 8>{});

@@ -72,6 +72,28 @@ def test_product_over_a_vocabulary(env, m, n, k):  # noqa: F811
     assert bool(((c.double() - want).abs() <= product_error(torch, A, W, k, want, 1.0, None, False)).all())
 
 
+def test_product_of_one_row_and_more_than_2_28_columns(env):  # noqa: F811
+    """B is zero but for its last rows and some at a distance: 17 GB of codes."""
+    torch, B = env
+    n, k = (1 << 28) + 24, 96
+    (a, A, _), (tail, W, _) = operand(torch, 1, k, 10), operand(torch, 64, k, 11)
+    sizes = B.conef_mx_sizes(n, k)
+    b = tuple(torch.zeros(sizes[s], dtype=torch.uint8, device="cuda:0") for s in ("code_bytes", "scale_bytes"))
+    places = [0, 1 << 25, (1 << 28) - 64, -(-n // 64) * 64 - 64]
+    for at in places:
+        for whole, part in zip(b, tail):
+            whole[at // 64 * part.numel():at // 64 * part.numel() + part.numel()] = part
+    c = torch.full((1, n), 7.0, dtype=torch.bfloat16, device="cuda:0")
+    B.conef_mx_product(a, b, k, 1.0, 0.0, c, None, B.Model.stream_handle())
+    want = torch.mm(A, W.t())
+    far = product_error(torch, A, W, k, want, 1.0, None, True)
+    for at in places:
+        got = c[:, at:at + 64]
+        assert bool(((got.double() - want[:, :got.shape[1]]).abs() <= far[:, :got.shape[1]]).all()), at
+        got.zero_()
+    assert not bool(c.any())
+
+
 @pytest.mark.parametrize("m,n,k", [(2000, 1700, 300), (3500, 3600, 1537), (3500, 3600, 4200), (8200, 8190, 1537)])
 def test_scales_of_nan_in_every_size_of_tile(env, m, n, k):  # noqa: F811
     """A row of A and one of B with a block that is NaN: that row and that column of C are, and nothing else is."""

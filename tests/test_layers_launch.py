@@ -65,3 +65,14 @@ def test_sums_over_rows_of_any_width(record, cols):
     n, = launches_of(record, ("conef_norm_backward", [None, 1, cols, 0, P, cols, P, cols, P, P, P, 0, 0, P, cols, 0, 0, P, P, P, 0]),
                      "k_norm_columns")
     assert n * 64 >= 2 * cols
+
+
+@pytest.mark.parametrize("m", [1, 16, 17, 33, 64])
+@pytest.mark.parametrize("n", [50304, (1 << 26) + 8, (1 << 28) - 16, 1 << 28, (1 << 28) + 24, (1 << 30) - 1])
+@pytest.mark.parametrize("k", [24, 96])
+def test_products_of_few_rows_and_any_width(record, m, n, k):
+    call = ("conef_mx_product", [P, P, P, P, m, n, k, 1.0, 0.0, P, n, 1, 0, 0])
+    if max(m * -(-n // 8), n * -(-k // 8)) >= 1 << 32:                              # beyond the documented range
+        assert record([call]) == [[-1, []]]
+        return
+    launches_of(record, call, "k_mx_")
