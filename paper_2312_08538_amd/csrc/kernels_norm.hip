@@ -31,7 +31,7 @@ constexpr int threads_of(int g) { return g > kThreads ? g : kThreads; }
 template <bool BF16>
 __global__ __launch_bounds__(kThreads) void k_dropout(DropoutArgs a, uint32_t octets, uint32_t per_row)
 {
-    const uint32_t o = blockIdx.x * kThreads + threadIdx.x;
+    const uint32_t o = group_index() * kThreads + threadIdx.x;
     if (o >= octets) return;
     const uint32_t row = o / per_row;
     const int col = (int)(o - row * per_row) * 8, left = a.cols - col;
@@ -582,7 +582,7 @@ void by_bool(bool v, F &&go)
 void launch_dropout(const DropoutArgs &a, bool bf16, hipStream_t st)
 {
     const uint32_t per_row = ((uint32_t)a.cols + 7) / 8, octets = (uint32_t)a.rows * per_row;
-    const dim3 grid((unsigned)(((uint64_t)octets + kThreads - 1) / kThreads));
+    const dim3 grid = grid_of(((int64_t)octets + kThreads - 1) / kThreads);
     by_bool(bf16, [&](auto b) { hipLaunchKernelGGL((k_dropout<decltype(b)::value>), grid, dim3(kThreads), 0, st, a, octets, per_row); });
 }
 

@@ -123,6 +123,21 @@ def test_values_past_the_caches(env, bf16):  # noqa: F811
     assert bool((out[:, cols:] == 77.0).all())
 
 
+# ---------------------------------------------------------------------------------------------- dropout
+def test_dropout_of_all_the_octets_that_a_counter_counts(env):  # noqa: F811
+    """2^32 - 2 of them, in place: 39 GB."""
+    torch, B = env
+    rows, cols, p, tail = (1 << 31) - 1, 9, 0.25, 40
+    x = torch.ones(rows, cols, dtype=torch.bfloat16, device="cuda:0")
+    B.conef_dropout_backward(B.conef_drop(p=p, site=0, seed=SEED, step=STEP), x, x, B.Model.stream_handle())
+    t = int(np.floor(p * 65536 + 0.5))
+    for first in (0, (1 << 28) - tail // 2, rows - tail):
+        u = np.array([[R.philox((2 * i + o, R.DROP, STEP & 0xFFFFFFFF, STEP >> 32), (SEED & 0xFFFFFFFF, SEED >> 32)) for o in (0, 1)]
+                      for i in range(first, first + tail)], dtype=np.uint64)
+        halves = np.stack([u & np.uint64(0xFFFF), u >> np.uint64(16)], -1).reshape(tail, 16)[:, :cols].astype(np.int64)
+        T.same_bits(x[first:first + tail].float().cpu().numpy(), R.bf16(np.where(halves >= t, np.float32(65536.0 / (65536 - t)), np.float32(0))))
+
+
 # ---------------------------------------------------------------------------------------------- norms
 WIDE = [(1100, 9001), (1100, 12288), (1100, 12289), (1100, 16384), (1100, 16385)]
 

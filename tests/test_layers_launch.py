@@ -76,3 +76,13 @@ def test_products_of_few_rows_and_any_width(record, m, n, k):
         assert record([call]) == [[-1, []]]
         return
     launches_of(record, call, "k_mx_")
+
+
+@pytest.mark.parametrize("rows,cols", [(1, 8), (1021, 1001), ((1 << 26) - 1, 512), ((1 << 31) - 1, 9), ((1 << 31) - 2, 16), (1 << 17, (1 << 18) - 8),
+                                       (2, (1 << 31) - 1)])
+def test_dropout_of_every_size(record, rows, cols):
+    octets = rows * -(-cols // 8)
+    for call in (("conef_dropout_forward", ["drop", rows, cols, 1, P, cols, P, cols, P, cols, 0]),
+                 ("conef_dropout_backward", ["drop", rows, cols, 1, P, cols, P, cols, 0])):
+        n, = launches_of(record, call, "k_dropout")
+        assert n * 256 >= octets
