@@ -169,7 +169,9 @@ __global__ __launch_bounds__(64 * WAVES) void k_mx_quantise(MxQuantArgs a, int64
     __shared__ __attribute__((aligned(16))) std::conditional_t<BY_COLS, Turned<BF16>, char> tile;
     __shared__ __attribute__((aligned(4))) uint8_t scales[2][256];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r = lane >> 2, q = lane & 3;
-    const int64_t row0 = blockIdx.x / col_tiles * kRows, col0 = blockIdx.x % col_tiles * kCols;
+    const uint32_t group = group_index();
+    const int64_t row0 = group / col_tiles * kRows, col0 = group % col_tiles * kCols;
+    if (row0 >= a.rows) return;
     const uint32_t per_row = (uint32_t)((a.cols + 7) >> 3), per_col = (uint32_t)((a.rows + 7) >> 3);
     Octet<BF16> o[kTurns][kBlocks];
     auto fetch = [&](bool whole) {
@@ -196,9 +198,9 @@ __global__ __launch_bounds__(64 * WAVES) void k_mx_quantise(MxQuantArgs a, int64
         const int block0 = BY_COLS ? (int)(col0 >> 5 & 3) : 0;               // of the piece
 #pragma unroll
         for (int h = 0; h < kTurns; ++h) {
-            const int group = wave + WAVES * h;
-            const int64_t row = row0 + 16 * group + r;
-            if (row0 + 16 * group >= padded_rows) continue;
+            const int group16 = wave + WAVES * h;
+            const int64_t row = row0 + 16 * group16 + r;
+            if (row0 + 16 * group16 >= padded_rows) continue;
 #pragma unroll
             for (int b = 0; b < kBlocks; ++b) {
                 Values v;
@@ -206,8 +208,8 @@ __global__ __launch_bounds__(64 * WAVES) void k_mx_quantise(MxQuantArgs a, int64
                 uint32_t byte;
                 const uint32_t octet = (uint32_t)row * per_row + (uint32_t)((col0 + 32 * b + 8 * q) >> 3);
                 const uint32_t c = quantise_octet<STOCHASTIC>(v, quad_largest(largest(v)), a.draws, octet, byte);
-                *reinterpret_cast<uint32_t *>(a.by_rows.codes + (piece0 + group * col_pieces) * 1024 + (block0 + b) * 256 + lane * 4) = c;
-                if (q == 0) scales[0][(group >> 2) * 64 * kBlocks + b * 64 + r * 4 + (group & 3)] = (uint8_t)byte;
+                *reinterpret_cast<uint32_t *>(a.by_rows.codes + (piece0 + group16 * col_pieces) * 1024 + (block0 + b) * 256 + lane * 4) = c;
+                if (q == 0) scales[0][(group16 >> 2) * 64 * kBlocks + b * 64 + r * 4 + (group16 & 3)] = (uint8_t)byte;
             }
         }
     }
@@ -262,7 +264,7 @@ __device__ __forceinline__ void values(uint32_t c, uint32_t byte, float v[8])
 template <bool BF16, bool PAST>
 __global__ __launch_bounds__(kThreads) void k_mx_dequantise(MxDequantArgs a, int64_t pieces, int64_t groups)
 {
-    const int64_t p = (int64_t)blockIdx.x * (kThreads / 64) + (threadIdx.x >> 6);
+    const int64_t p = (int64_t)group_index() * (kThreads / 64) + (threadIdx.x >> 6);
     if (p >= groups * pieces) return;
     const int64_t group = p / pieces, tc = p - group * pieces;
     // a store: 8 rows of 128 bytes, 16 a lane
@@ -307,7 +309,7 @@ void launch_mx_quantise(const MxQuantArgs &a, bool bf16, hipStream_t st)
     const int64_t row_pieces = (a.rows + 127) / 128, col_pieces = (a.cols + 127) / 128;
     const int64_t padded_rows = (a.rows + 63) / 64 * 64, padded_cols = (a.cols + 63) / 64 * 64;
     const int64_t col_tiles = a.by_cols.codes ? 2 * col_pieces : col_pieces;
-    const dim3 grid((unsigned)((a.by_cols.codes ? row_pieces : padded_rows / 64) * col_tiles));
+    const dim3 grid = grid_of((a.by_cols.codes ? row_pieces : padded_rows / 64) * col_tiles);
     by_bool(bf16, [&](auto b) {
         by_bool(a.stochastic != 0, [&](auto s) {
             auto go = [&](auto rows, auto cols, auto waves) {
@@ -332,7 +334,7 @@ void launch_mx_quantise(const MxQuantArgs &a, bool bf16, hipStream_t st)
 void launch_mx_dequantise(const MxDequantArgs &a, bool bf16, hipStream_t st)
 {
     const int64_t pieces = (a.cols + 127) / 128, groups = (a.rows + 15) / 16;
-    const dim3 grid((unsigned)((pieces * groups + 3) / 4));
+    const dim3 grid = grid_of((pieces * groups + 3) / 4);
     // Values that the dies' caches do not hold go past them: 8192 x 8192 in bf16, another buffer each time, 26 / 36 us; but not rows that end
     // within 64 bytes, of which halves would be written twice: 16384 x 3000 in bf16 27 / 62.
     const int64_t size = bf16 ? 2 : 4;

@@ -123,6 +123,23 @@ def test_values_past_the_caches(env, bf16):  # noqa: F811
     assert bool((out[:, cols:] == 77.0).all())
 
 
+@pytest.mark.parametrize("by_cols", [False, True])
+def test_quantisation_of_the_longest_side(env, by_cols):  # noqa: F811
+    """2^30 - 1 elements, one a row or all of them one row: 64 or 32 GiB of codes and back."""
+    torch, B = env
+    st, n = B.Model.stream_handle(), (1 << 30) - 1
+    x = torch.zeros(n, 1, dtype=torch.bfloat16, device="cuda:0")
+    x.normal_(generator=torch.Generator(device="cuda:0").manual_seed(12))
+    q = B.mx_alloc(*((1, n) if by_cols else (n, 1)))
+    B.conef_mx_quantise(x, B.MX_NEAREST, 0, 0, 0, None if by_cols else q, q if by_cols else None, st)
+    out = torch.full((1, n) if by_cols else (n, 1), 7.0, device="cuda:0")
+    B.conef_mx_dequantise(q, out, st)
+    for first in (0, 1 << 27, (1 << 29) - 64, (1 << 30) - 192):
+        part = x[first:first + 192].float().cpu().numpy()
+        want = R.mx_decode(*R.mx_encode(part.T if by_cols else part))
+        T.same_bits(out.view(-1)[first:first + 192].cpu().numpy(), want.reshape(-1))
+
+
 # ---------------------------------------------------------------------------------------------- dropout
 def test_dropout_of_all_the_octets_that_a_counter_counts(env):  # noqa: F811
     """2^32 - 2 of them, in place: 39 GB."""

@@ -86,3 +86,26 @@ def test_dropout_of_every_size(record, rows, cols):
                  ("conef_dropout_backward", ["drop", rows, cols, 1, P, cols, P, cols, 0])):
         n, = launches_of(record, call, "k_dropout")
         assert n * 256 >= octets
+
+
+MX_SIDES = [(16, 768), (8192, 8192), ((1 << 30) - 1, 1), ((1 << 30) - 64, 32), ((1 << 30) - 128, 8), (1, (1 << 30) - 1), (8, (1 << 30) - 127),
+            ((1 << 27) + 3, 200)]
+
+
+@pytest.mark.parametrize("rows,cols", MX_SIDES)
+def test_quantisation_of_every_size(record, rows, cols):
+    """A workgroup takes 64 rows of 128 columns, or 128 of 64 if it quantises by columns too."""
+    for by_rows, by_cols in ((P, 0), (0, P), (P, P)):
+        for rounding in (0, 1):
+            n, = launches_of(record, ("conef_mx_quantise", [P, cols, rows, cols, 1, rounding, 1, 0, 0, by_rows, by_rows, by_cols, by_cols, 0]),
+                             "k_mx_quantise")
+            padded = (-(-rows // 128) * 2 * -(-cols // 128)) if by_cols else -(-rows // 64) * -(-cols // 128)
+            assert n >= padded
+
+
+@pytest.mark.parametrize("rows,cols", MX_SIDES)
+def test_values_of_every_size(record, rows, cols):
+    """A wave takes 16 rows of 128 columns."""
+    for dtype in (0, 1):
+        n, = launches_of(record, ("conef_mx_dequantise", [P, P, rows, cols, P, cols, dtype, 0]), "k_mx_dequantise")
+        assert n * 4 >= -(-rows // 16) * -(-cols // 128)
