@@ -240,6 +240,28 @@ def test_backward_outputs_in_the_place_of_their_inputs_and_alone(env, rows, cols
             assert torch.equal(got[k], want[k]), (columns, k)
 
 
+@pytest.mark.parametrize("bf16", [False, True])
+@pytest.mark.parametrize("cols", [7, 33, 100, 250, 300, 700, 1001, 2001, 2049, 5003, 6145, 9001, 12290])
+def test_gradients_of_constant_rows_far_from_zero(env, cols, bf16):  # noqa: F811
+    """Rows of 2^110 at eps = 1e-12: (z - mean) rstd is 0 everywhere, and (0 - mean) rstd would be beyond fp32."""
+    torch, B = env
+    rows = 3
+    g, _, gamma, _ = norm_inputs(rows, cols, bf16, 6)
+    dy, z = R.rounded(g.standard_normal((rows, cols)), bf16), np.full((rows, cols), 2.0 ** 110, np.float32)
+    mean, rstd = z[:, 0].copy(), np.full(rows, 1e6, np.float32)
+    D = {k: Strided(torch, rows, cols, bf16, 1, 3, v) for k, v in (("dy", dy), ("z", z), ("dz", None))}
+    dgamma, dbeta = torch.full((cols,), 7.0, device="cuda:0"), torch.full((cols,), 7.0, device="cuda:0")
+    room = B.conef_norm_workspace(rows, cols)
+    ws = torch.full((room,), 0xFF, dtype=torch.uint8, device="cuda:0")
+    B.conef_norm_backward(None, D["dy"].t, D["z"].t, column_vector(torch, gamma), column_vector(torch, mean), column_vector(torch, rstd), None, D["dz"].t,
+                          None, dgamma, dbeta, ws, B.Model.stream_handle())
+    want, wg, wb, hat, a = R.norm_back(dy, z, gamma, mean, rstd)
+    tz, tg, tb = T.back_tolerance(dy, hat, a, gamma, rstd, want, rows, cols, room // (8 * cols), bf16)
+    assert (np.abs(D["dz"].numpy() - want) <= tz).all()
+    assert (np.abs(dgamma.cpu().numpy() - wg) <= tg).all() and (np.abs(dbeta.cpu().numpy() - wb) <= tb).all()
+    D["dz"].check_canary()
+
+
 def test_sums_over_rows_of_more_than_2_27_columns(env):  # noqa: F811
     """Two rows, of which every column's sums are two products and one addition."""
     torch, B = env
