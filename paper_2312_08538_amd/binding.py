@@ -481,7 +481,7 @@ def conef_cs_decode_error(ctx, table, e_out, stream=0):
 
 
 # a worker's own step: dropout, layer norm, microscaled 4-bit floating point.  Matrices are torch tensors of two dimensions
-# on the device (rows may be strided); their shape, type and pitch go with their address.  Their marshalling is compiled
+# on the stream's device (rows may be strided); their shape, type and pitch go with their address.  Their marshalling is compiled
 # (csrc/face.cpp): a small call's time is that of its way through here and of its launch.
 _face = None
 
@@ -499,7 +499,9 @@ def face():
                                "there is no fallback path") from e
         calls = ("dropout_forward", "dropout_backward", "norm_forward", "norm_workspace", "norm_backward", "mx_quantise",
                  "mx_dequantise", "mx_product_workspace", "mx_product")
-        module.connect(conef_drop, ConefError, tuple(ctypes.cast(getattr(lib(), "conef_" + c), ctypes.c_void_p).value for c in calls))
+        # (hipStreamGetDevice: of the runtime that the library is linked to)
+        addresses = (ctypes.cast(getattr(lib(), c), ctypes.c_void_p).value for c in (*("conef_" + c for c in calls), "hipStreamGetDevice"))
+        module.connect(conef_drop, ConefError, tuple(addresses))
         _face = module
     return _face
 

@@ -1,7 +1,7 @@
 // Python's way into the operators of a training step (conef_dropout_*, conef_norm_*, conef_mx_*): reads shapes, types, pitches and
-// addresses off torch tensors, refuses those that do not fit, and calls the library by the addresses that it was given.  A small
-// operator's time is that of its call: a dropout of one row takes 3.1 us, of which 2.9 are the launch (marshalled in Python and by ctypes 5.0), a layer
-// norm of one row 4.0 with what its caller does around it (7.6).
+// addresses off torch tensors, refuses those that do not fit or are on another device than the stream, and calls the library by the
+// addresses that it was given.  A small operator's time is that of its call: a dropout of one row takes 3.1 us, of which 2.9 are the launch
+// (marshalled in Python and by ctypes 5.0), a layer norm of one row 4.0 with what its caller does around it (7.6).
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <ATen/core/Tensor.h>
@@ -23,6 +23,7 @@ struct Library {
     decltype(&conef_mx_dequantise) mx_dequantise;
     decltype(&conef_mx_product_workspace) mx_product_workspace;
     decltype(&conef_mx_product) mx_product;
+    int (*stream_device)(void *stream, int *device);            // the runtime's hipStreamGetDevice
 } L;
 
 PyObject *drop_type, *error_type;       // conef_drop and ConefError of the binding
@@ -71,10 +72,16 @@ float real(PyObject *o)
     return (float)v;
 }
 
-void *stream(PyObject *o)
-{
-    return o == Py_None ? nullptr : reinterpret_cast<void *>(bits(o));
-}
+// a stream (none: the current device's default one) and the device that it belongs to, which all of a call's tensors have to be on
+struct Stream {
+    void *handle;
+    int device = -1;
+
+    explicit Stream(PyObject *o) : handle(o == Py_None ? nullptr : reinterpret_cast<void *>(bits(o)))
+    {
+        if (L.stream_device(handle, &device) != 0) device = -1;
+    }
+};
 
 // a description's copy, or none
 struct Drop {
@@ -117,13 +124,21 @@ int kind_of(const at::Tensor &t)
 
 bool on_device(const at::Tensor &t) { return t.is_cuda() && t.layout() == at::kStrided; }
 
+void check_place(const Stream &st, const at::Tensor &t)
+{
+    if (t.device().index() == st.device) return;
+    if (st.device < 0) refuse("the stream is none of this process's");
+    refuse("tensors on cuda:" + std::to_string(st.device) + ", the stream's device, are wanted, not on " + t.device().str());
+}
+
 struct Matrix {
     void *data = nullptr;
     int64_t pitch = 0, rows = 0, cols = 0;
     int kind = 0;
 
-    void take(const at::Tensor &t)
+    void take(const Stream &st, const at::Tensor &t)
     {
+        check_place(st, t);
         rows = t.size(0);
         cols = t.size(1);
         pitch = rows > 1 ? t.stride(0) : cols ? cols : 1;
@@ -135,42 +150,44 @@ struct Matrix {
         return on_device(t) && t.dim() == 2 && kind_of(t) >= 0 && (t.stride(1) == 1 || t.size(1) <= 1);
     }
 
-    explicit Matrix(PyObject *o)
+    Matrix(const Stream &st, PyObject *o)
     {
         const at::Tensor &t = tensor(o);
         if (!fits(t)) refuse("a matrix of fp32 or bf16 on the device with contiguous rows is wanted, not " + about(t));
         kind = kind_of(t);
-        take(t);
+        take(st, t);
     }
     // another of the same shape and type, or none
-    Matrix(PyObject *o, const Matrix &of) : kind(of.kind)
+    Matrix(const Stream &st, PyObject *o, const Matrix &of) : kind(of.kind)
     {
         if (o == Py_None) return;
         const at::Tensor &t = tensor(o);
         if (!fits(t) || t.size(0) != of.rows || t.size(1) != of.cols || kind_of(t) != of.kind)
             refuse("a matrix (" + std::to_string(of.rows) + ", " + std::to_string(of.cols) + (of.kind == CONEF_F32 ? ") of fp32" : ") of bf16") +
                    " on the device with contiguous rows is wanted, not " + about(t));
-        take(t);
+        take(st, t);
     }
 };
 
 // n contiguous floats, or none
-float *vector(PyObject *o, int64_t n)
+float *vector(const Stream &st, PyObject *o, int64_t n)
 {
     if (o == Py_None) return nullptr;
     const at::Tensor &t = tensor(o);
     if (!on_device(t) || t.dim() != 1 || t.size(0) != n || t.scalar_type() != at::kFloat || !t.is_contiguous())
         refuse(std::to_string(n) + " contiguous floats on the device are wanted, not " + about(t));
+    check_place(st, t);
     return static_cast<float *>(t.data_ptr());
 }
 
 // a buffer of at least so many bytes, or none
-void *room(PyObject *o, size_t bytes)
+void *room(const Stream &st, PyObject *o, size_t bytes)
 {
     if (o == Py_None) return nullptr;
     const at::Tensor &t = tensor(o);
     if (!on_device(t) || !t.is_contiguous() || t.nbytes() < bytes)
         refuse("a contiguous buffer of " + std::to_string(bytes) + " bytes on the device is wanted, not " + about(t));
+    check_place(st, t);
     return t.data_ptr();
 }
 
@@ -178,7 +195,7 @@ void *room(PyObject *o, size_t bytes)
 struct Packed {
     uint8_t *codes = nullptr, *scales = nullptr;
 
-    Packed(PyObject *o, int64_t rows, int64_t cols)
+    Packed(const Stream &st, PyObject *o, int64_t rows, int64_t cols)
     {
         if (o == Py_None) return;
         PyObject *both[2] = {};
@@ -194,8 +211,8 @@ struct Packed {
         // (in 128 bits: the library refuses sides that 64 bits could not count)
         const unsigned __int128 elements = (unsigned __int128)(((uint64_t)rows + 63) / 64) * (((uint64_t)cols + 127) / 128) * 8192;
         if (rows < 0 || cols < 0 || elements >> 62) refuse("sides out of range");
-        codes = static_cast<uint8_t *>(room(both[0], (size_t)(elements / 2)));
-        scales = static_cast<uint8_t *>(room(both[1], (size_t)(elements / 32)));
+        codes = static_cast<uint8_t *>(room(st, both[0], (size_t)(elements / 2)));
+        scales = static_cast<uint8_t *>(room(st, both[1], (size_t)(elements / 32)));
     }
 };
 
@@ -229,11 +246,11 @@ int unlocked(F &&f)
 PyObject *dropout_forward(PyObject *, PyObject *const *p, Py_ssize_t n)
 {
     return call("conef_dropout_forward", n, 5, [&] {
+        const Stream st(p[4]);
         const Drop d(p[0]);
-        const Matrix x(p[1]), r(p[2], x), y(p[3], x);
-        void *st = stream(p[4]);
+        const Matrix x(st, p[1]), r(st, p[2], x), y(st, p[3], x);
         return unlocked([&] {
-            return L.dropout_forward(d.there, x.rows, x.cols, x.kind, x.data, x.pitch, r.data, r.pitch, y.data, y.pitch, st);
+            return L.dropout_forward(d.there, x.rows, x.cols, x.kind, x.data, x.pitch, r.data, r.pitch, y.data, y.pitch, st.handle);
         });
     });
 }
@@ -241,25 +258,25 @@ PyObject *dropout_forward(PyObject *, PyObject *const *p, Py_ssize_t n)
 PyObject *dropout_backward(PyObject *, PyObject *const *p, Py_ssize_t n)
 {
     return call("conef_dropout_backward", n, 4, [&] {
+        const Stream st(p[3]);
         const Drop d(p[0]);
-        const Matrix dy(p[1]), dx(p[2], dy);
-        void *st = stream(p[3]);
-        return unlocked([&] { return L.dropout_backward(d.there, dy.rows, dy.cols, dy.kind, dy.data, dy.pitch, dx.data, dx.pitch, st); });
+        const Matrix dy(st, p[1]), dx(st, p[2], dy);
+        return unlocked([&] { return L.dropout_backward(d.there, dy.rows, dy.cols, dy.kind, dy.data, dy.pitch, dx.data, dx.pitch, st.handle); });
     });
 }
 
 PyObject *norm_forward(PyObject *, PyObject *const *p, Py_ssize_t n)
 {
     return call("conef_norm_forward", n, 11, [&] {
+        const Stream st(p[10]);
         const Drop d(p[0]);
         const float eps = real(p[1]);
-        const Matrix x(p[2]), r(p[3], x), z(p[6], x), y(p[7], x);
-        const float *gamma = vector(p[4], x.cols), *beta = vector(p[5], x.cols);
-        float *mean = vector(p[8], x.rows), *rstd = vector(p[9], x.rows);
-        void *st = stream(p[10]);
+        const Matrix x(st, p[2]), r(st, p[3], x), z(st, p[6], x), y(st, p[7], x);
+        const float *gamma = vector(st, p[4], x.cols), *beta = vector(st, p[5], x.cols);
+        float *mean = vector(st, p[8], x.rows), *rstd = vector(st, p[9], x.rows);
         return unlocked([&] {
             return L.norm_forward(d.there, eps, x.rows, x.cols, x.kind, x.data, x.pitch, r.data, r.pitch, gamma, beta, z.data, z.pitch, y.data,
-                                  y.pitch, mean, rstd, st);
+                                  y.pitch, mean, rstd, st.handle);
         });
     });
 }
@@ -267,16 +284,17 @@ PyObject *norm_forward(PyObject *, PyObject *const *p, Py_ssize_t n)
 PyObject *norm_backward(PyObject *, PyObject *const *p, Py_ssize_t n)
 {
     return call("conef_norm_backward", n, 13, [&] {
+        const Stream st(p[12]);
         const Drop d(p[0]);
-        const Matrix dy(p[1]), z(p[2], dy), in(p[6], dy), dz(p[7], dy), dx(p[8], dy);
-        const float *gamma = vector(p[3], dy.cols), *mean = vector(p[4], dy.rows), *rstd = vector(p[5], dy.rows);
-        float *dgamma = vector(p[9], dy.cols), *dbeta = vector(p[10], dy.cols);
+        const Matrix dy(st, p[1]), z(st, p[2], dy), in(st, p[6], dy), dz(st, p[7], dy), dx(st, p[8], dy);
+        const float *gamma = vector(st, p[3], dy.cols), *mean = vector(st, p[4], dy.rows), *rstd = vector(st, p[5], dy.rows);
+        float *dgamma = vector(st, p[9], dy.cols), *dbeta = vector(st, p[10], dy.cols);
         size_t bytes = 0;
         if (p[11] != Py_None && L.norm_workspace(dy.rows, dy.cols, &bytes) != CONEF_OK) return (int)CONEF_EINVAL;
-        void *ws = room(p[11], bytes), *st = stream(p[12]);
+        void *ws = room(st, p[11], bytes);
         return unlocked([&] {
             return L.norm_backward(d.there, dy.rows, dy.cols, dy.kind, dy.data, dy.pitch, z.data, z.pitch, gamma, mean, rstd, in.data, in.pitch,
-                                   dz.data, dz.pitch, dx.data, dx.pitch, dgamma, dbeta, ws, st);
+                                   dz.data, dz.pitch, dx.data, dx.pitch, dgamma, dbeta, ws, st.handle);
         });
     });
 }
@@ -284,15 +302,15 @@ PyObject *norm_backward(PyObject *, PyObject *const *p, Py_ssize_t n)
 PyObject *mx_quantise(PyObject *, PyObject *const *p, Py_ssize_t n)
 {
     return call("conef_mx_quantise", n, 8, [&] {
-        const Matrix x(p[0]);
+        const Stream st(p[7]);
+        const Matrix x(st, p[0]);
         const int rounding = (int)integer(p[1]);
         const uint64_t seed = bits(p[2]), site = bits(p[3]), step = bits(p[4]);
         if (site >> 32) refuse("a site below 2^27 is wanted");
-        const Packed q(p[5], x.rows, x.cols), t(p[6], x.cols, x.rows);
-        void *st = stream(p[7]);
+        const Packed q(st, p[5], x.rows, x.cols), t(st, p[6], x.cols, x.rows);
         return unlocked([&] {
             return L.mx_quantise(x.data, x.pitch, x.rows, x.cols, x.kind, rounding, seed, (uint32_t)site, step, q.codes, q.scales, t.codes,
-                                 t.scales, st);
+                                 t.scales, st.handle);
         });
     });
 }
@@ -300,25 +318,26 @@ PyObject *mx_quantise(PyObject *, PyObject *const *p, Py_ssize_t n)
 PyObject *mx_dequantise(PyObject *, PyObject *const *p, Py_ssize_t n)
 {
     return call("conef_mx_dequantise", n, 3, [&] {
-        const Matrix out(p[1]);
-        const Packed q(p[0], out.rows, out.cols);
-        void *st = stream(p[2]);
-        return unlocked([&] { return L.mx_dequantise(q.codes, q.scales, out.rows, out.cols, out.data, out.pitch, out.kind, st); });
+        const Stream st(p[2]);
+        const Matrix out(st, p[1]);
+        const Packed q(st, p[0], out.rows, out.cols);
+        return unlocked([&] { return L.mx_dequantise(q.codes, q.scales, out.rows, out.cols, out.data, out.pitch, out.kind, st.handle); });
     });
 }
 
 PyObject *mx_product(PyObject *, PyObject *const *p, Py_ssize_t n)
 {
     return call("conef_mx_product", n, 8, [&] {
-        const Matrix c(p[5]);
+        const Stream st(p[7]);
+        const Matrix c(st, p[5]);
         const int64_t k = integer(p[2]);
-        const Packed a(p[0], c.rows, k), b(p[1], c.cols, k);
+        const Packed a(st, p[0], c.rows, k), b(st, p[1], c.cols, k);
         const float alpha = real(p[3]), beta = real(p[4]);
         size_t bytes = 0;
         if (p[6] != Py_None && L.mx_product_workspace(c.rows, c.cols, k, &bytes) != CONEF_OK) return (int)CONEF_EINVAL;
-        void *ws = room(p[6], bytes), *st = stream(p[7]);
+        void *ws = room(st, p[6], bytes);
         return unlocked([&] {
-            return L.mx_product(a.codes, a.scales, b.codes, b.scales, c.rows, c.cols, k, alpha, beta, c.data, c.pitch, c.kind, ws, st);
+            return L.mx_product(a.codes, a.scales, b.codes, b.scales, c.rows, c.cols, k, alpha, beta, c.data, c.pitch, c.kind, ws, st.handle);
         });
     });
 }
@@ -327,10 +346,11 @@ PyObject *mx_product(PyObject *, PyObject *const *p, Py_ssize_t n)
 PyObject *connect(PyObject *, PyObject *args)
 {
     PyObject *drop, *error;
-    unsigned long long at[9];
-    if (!PyArg_ParseTuple(args, "OO(KKKKKKKKK)", &drop, &error, at, at + 1, at + 2, at + 3, at + 4, at + 5, at + 6, at + 7, at + 8)) return nullptr;
+    unsigned long long at[10];
+    if (!PyArg_ParseTuple(args, "OO(KKKKKKKKKK)", &drop, &error, at, at + 1, at + 2, at + 3, at + 4, at + 5, at + 6, at + 7, at + 8,
+                          at + 9)) return nullptr;
     if (!PyType_Check(drop) || !PyType_Check(error)) {
-        PyErr_SetString(PyExc_TypeError, "two types and nine addresses");
+        PyErr_SetString(PyExc_TypeError, "two types and ten addresses");
         return nullptr;
     }
     L.dropout_forward = reinterpret_cast<decltype(L.dropout_forward)>(at[0]);
@@ -342,6 +362,7 @@ PyObject *connect(PyObject *, PyObject *args)
     L.mx_dequantise = reinterpret_cast<decltype(L.mx_dequantise)>(at[6]);
     L.mx_product_workspace = reinterpret_cast<decltype(L.mx_product_workspace)>(at[7]);
     L.mx_product = reinterpret_cast<decltype(L.mx_product)>(at[8]);
+    L.stream_device = reinterpret_cast<decltype(L.stream_device)>(at[9]);
     Py_INCREF(drop);
     Py_INCREF(error);
     Py_XSETREF(drop_type, drop);

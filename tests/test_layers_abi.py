@@ -167,3 +167,56 @@ def test_reference_format_round_trip():
     step = np.repeat(2.0 ** (s.astype(float) - 127), 32, 1)[:, :77]
     assert (np.abs(v - x) <= np.where(np.abs(x) >= 6 * step, 2.0, np.where(np.abs(x) >= 4 * step, 1.0, np.where(np.abs(x) >= 2 * step, 0.5, 0.25))) * step).all()
     assert (R.mx_decode(*R.mx_encode(v)) == v).all()                               # values of the format are kept
+
+
+def test_binding_refuses_tensors_on_another_device_than_the_stream_s():
+    """Tensors of two devices that are not there (no memory, no device behind them), and the library's calls as functions that do nothing:
+    what is taken is taken, what is refused is refused by its device alone."""
+    import torch
+    from torch._subclasses.fake_tensor import FakeTensorMode
+
+    calls, on = [], {0: 0, 7: 1}                        # stream 0 belongs to device 0, stream 7 to device 1
+    nothing = ctypes.CFUNCTYPE(ctypes.c_int)(lambda: calls.append(1) or B.OK)
+    sizes = ctypes.CFUNCTYPE(ctypes.c_int)(lambda: B.OK)
+
+    @ctypes.CFUNCTYPE(ctypes.c_int, ctypes.c_size_t, ctypes.POINTER(ctypes.c_int))
+    def device_of(stream, device):
+        device[0] = on[stream]
+        return 0
+
+    at = lambda f: ctypes.cast(f, ctypes.c_void_p).value                           # noqa: E731
+    face = B.face()
+    face.connect(B.conef_drop, B.ConefError, (*(at(sizes if i in (3, 7) else nothing) for i in range(9)), at(device_of)))
+    try:
+        with FakeTensorMode():
+            def args(d):
+                z = lambda *s, **k: torch.empty(*s, device=f"cuda:{d}", **k)       # noqa: E731
+                n = [z(B.conef_mx_sizes(4, 8)[k], dtype=torch.uint8) for k in ("code_bytes", "scale_bytes")]
+                return {"x": z(4, 8), "v": z(8), "m": z(4), "q": tuple(n), "c": z(4, 4), "w": z(64, dtype=torch.uint8)}
+
+            t = args(0), args(1)
+        d = drop()
+        forms = [  # every call, its tensors by name
+            (lambda a, s: B.conef_dropout_forward(d, a[0], a[1], a[2], s), "xxx"), (lambda a, s: B.conef_dropout_backward(d, a[0], a[1], s), "xx"),
+            (lambda a, s: B.conef_norm_forward(d, 1e-5, *a, s), "xxvvxxmm"), (lambda a, s: B.conef_norm_backward(d, *a, s), "xxvmmxxxvvw"),
+            (lambda a, s: B.conef_mx_quantise(a[0], B.MX_NEAREST, 0, 0, 0, a[1], None, s), "xq"), (lambda a, s: B.conef_mx_dequantise(a[0], a[1], s), "qx"),
+            (lambda a, s: B.conef_mx_product(a[0], a[1], 8, 1.0, 0.0, a[2], a[3], s), "qqcw")]
+        for call, names in forms:
+            for stream, device in on.items():
+                before = len(calls)
+                call([t[device][n] for n in names], stream)
+                assert len(calls) == before + 1, names
+                for i in range(len(names)):                                        # one of them elsewhere, and all of them
+                    for wrong in ({i}, set(range(len(names)))):
+                        with pytest.raises(B.ConefError) as e:
+                            call([t[1 - device if k in wrong else device][n] for k, n in enumerate(names)], stream)
+                        assert e.value.code == B.EINVAL and f"cuda:{device}" in str(e.value), (names, i)
+                # codes and scales apart
+                if "q" in names:
+                    mixed = (t[device]["q"][0], t[1 - device]["q"][1])
+                    with pytest.raises(B.ConefError):
+                        call([mixed if n == "q" else t[device][n] for n in names], stream)
+                assert len(calls) == before + 1
+    finally:
+        B._face = None
+        B.face()
