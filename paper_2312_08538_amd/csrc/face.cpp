@@ -304,12 +304,13 @@ PyObject *mx_quantise(PyObject *, PyObject *const *p, Py_ssize_t n)
     return call("conef_mx_quantise", n, 8, [&] {
         const Stream st(p[7]);
         const Matrix x(st, p[0]);
-        const int rounding = (int)integer(p[1]);
+        const int64_t rounding = integer(p[1]);
+        if (rounding != CONEF_MX_NEAREST && rounding != CONEF_MX_STOCHASTIC) refuse("CONEF_MX_NEAREST or CONEF_MX_STOCHASTIC is wanted");
         const uint64_t seed = bits(p[2]), site = bits(p[3]), step = bits(p[4]);
         if (site >> 32) refuse("a site below 2^27 is wanted");
         const Packed q(st, p[5], x.rows, x.cols), t(st, p[6], x.cols, x.rows);
         return unlocked([&] {
-            return L.mx_quantise(x.data, x.pitch, x.rows, x.cols, x.kind, rounding, seed, (uint32_t)site, step, q.codes, q.scales, t.codes,
+            return L.mx_quantise(x.data, x.pitch, x.rows, x.cols, x.kind, (int)rounding, seed, (uint32_t)site, step, q.codes, q.scales, t.codes,
                                  t.scales, st.handle);
         });
     });

@@ -306,3 +306,12 @@ def test_each_refusal_says_what_does_not_fit(env):  # noqa: F811
         with pytest.raises(B.ConefError) as e:
             call()
         assert e.value.code == B.EINVAL and why in str(e.value), (why, str(e.value))
+
+
+@pytest.mark.parametrize("rounding", [2, -1, 1 << 32, (1 << 32) + 1, -(1 << 32)])
+def test_a_rounding_that_is_none_is_refused(env, rounding):  # noqa: F811
+    torch, B = env
+    q = B.mx_alloc(4, 8)
+    with pytest.raises(B.ConefError) as e:
+        B.conef_mx_quantise(torch.zeros(4, 8, device="cuda:0"), rounding, 0, 0, 0, q, None, B.Model.stream_handle())
+    assert e.value.code == B.EINVAL
