@@ -590,7 +590,8 @@ constexpr int kCus = 256;
 //   tiny, 64 x 64, where small ones do not reach every CU:  1024 x 1024 x 1024 4.0 / 5.6, 16384 x 16 x 4096 8.4 / 11.7, 128 x 4096 x 1024 3.8 / 5.5
 // The long axis in parts, added up by a launch of its own: 256 x 256 x 8192 9.4 in 4 parts / 12.6, but 200 x 1024 x 4096 8.7 in 2 / 7.6.
 // Past the caches what those of the dies do not hold: 8192 x 32768 x 1024 184 / 270, 8192 x 8192 x 2048 in fp32 88 / 97, 4096 x 8192 x 2048 42 / 43;
-// large tiles and streams only what the card's last cache does not hold either: 4096 x 50304 x 2048 205 / 236, but 8192 x 8192 x 2048 75 / 67.
+// streams only what the card's last cache does not hold either: 4096 x 50304 x 2048 205 / 236, but 8192 x 8192 x 2048 75 / 67; large tiles nothing, as
+// fewer than 1024 of them are a C of less than that cache.
 // And not rows that end within 64 bytes, of which halves would be written twice (within 16 if the last cache does not hold C): 2000 x 50300 x 300
 // 46 / 89, 4096 x 50303 x 2048 290 / 336, 8192 x 16001 x 700 87 / 128; but 8192 x 32760 x 1024 218 past the caches / 280.
 Choice choose(int64_t m, int64_t n, int64_t k)
@@ -670,7 +671,7 @@ void launch_mx_product(const MxProductArgs &a, bool bf16, hipStream_t st)
     }
     const int64_t size = bf16 ? 2 : 4, bytes = a.m * a.n * size, last = (int64_t)256 << 20;
     const int64_t ends = (a.c.pitch * size) | (int64_t)reinterpret_cast<uintptr_t>(a.c.data);
-    const bool past = bytes > (c.tiles >= kLarge ? last : last / 8) && (ends % 64 == 0 || (ends % 16 == 0 && bytes > last));
+    const bool past = bytes > (c.tiles == kStream ? last : last / 8) && (ends % 64 == 0 || (ends % 16 == 0 && bytes > last));
     by_bool(bf16, [&](auto b) {
         by_bool(a.beta != 0.0f, [&](auto add) {
             constexpr bool B = decltype(b)::value, ADD = decltype(add)::value;
@@ -682,13 +683,14 @@ void launch_mx_product(const MxProductArgs &a, bool bf16, hipStream_t st)
                                    fours);
             } else if (c.tiles == kTiny) {
                 launch_tiles<B, ADD, false, 2, 2, 2, 2, 4, 4>(a, c, st);
+            } else if (c.tiles == kLarge) {
+                launch_tiles<B, ADD, false, 2, 4, 8, 4, 4, 2>(a, c, st);
             } else {
                 by_bool(past, [&](auto p) {
                     constexpr bool PAST = decltype(p)::value;
                     if (c.tiles == kSmall) launch_tiles<B, ADD, PAST, 2, 2, 4, 4, 3, 3>(a, c, st);
                     else if (c.tiles == kStream) launch_stream<B, ADD, PAST>(a, st);
-                    else if (c.tiles == kWide) launch_tiles<B, ADD, PAST, 2, 2, 8, 4, 3, 2>(a, c, st);
-                    else launch_tiles<B, ADD, PAST, 2, 4, 8, 4, 4, 2>(a, c, st);
+                    else launch_tiles<B, ADD, PAST, 2, 2, 8, 4, 3, 2>(a, c, st);
                 });
             }
         });

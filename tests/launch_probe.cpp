@@ -48,5 +48,13 @@ const char *probe_launch(int i, uint32_t *out)
     for (int k = 0; k < 6; ++k) out[k] = v[k];
     return l.name.c_str();
 }
+// kernels' names, one a line
+const char *probe_names()
+{
+    static std::string all;
+    all.clear();
+    for (const auto &n : names) all += n.second + "\n";
+    return all.c_str();
+}
 void probe_clear() { launches.clear(); }
 }

@@ -26,13 +26,14 @@ for name, args in json.loads(sys.stdin.read()):
     v = (ctypes.c_uint32 * 6)()
     launches = [(probe.probe_launch(i, v).decode(), *v) for i in range(probe.probe_launches())]
     out.append([code, launches])
-print(json.dumps(out))
+probe.probe_names.restype = ctypes.c_char_p
+print(json.dumps([out, probe.probe_names().decode().split()]))
 """
 
 
 @pytest.fixture(scope="module")
 def record(tmp_path_factory):
-    """record([(call, arguments), ...]): [(code, [(kernel, grid x, y, z, block x, y, z), ...]), ...]"""
+    """record([(call, arguments), ...]): [(code, [(kernel, grid x, y, z, block x, y, z), ...]), ...]; record.names(): all kernels"""
     so = tmp_path_factory.mktemp("probe") / "launch_probe.so"
     subprocess.run(["g++", "-std=c++17", "-O1", "-shared", "-fPIC", "-o", str(so), os.path.join(HERE, "launch_probe.cpp")], check=True)
 
@@ -41,7 +42,11 @@ def record(tmp_path_factory):
                              capture_output=True, text=True)
         return json.loads(run.stdout)
 
-    return go
+    def calls_only(calls):
+        return go(calls)[0]
+
+    calls_only.names = lambda: go([])[1]
+    return calls_only
 
 
 def groups(launch):
@@ -109,3 +114,37 @@ def test_values_of_every_size(record, rows, cols):
     for dtype in (0, 1):
         n, = launches_of(record, ("conef_mx_dequantise", [P, P, rows, cols, P, cols, dtype, 0]), "k_mx_dequantise")
         assert n * 4 >= -(-rows // 16) * -(-cols // 128)
+
+
+def test_every_kernel_is_reached(record, tmp_path):
+    """Calls of every kind on sizes on both sides of every rule; what they launch are all the kernels that there are."""
+    calls = []
+    for dtype in (0, 1):
+        calls.append(("conef_dropout_backward", ["drop", 4, 8, dtype, P, 8, P, 8, 0]))
+        for cols in (8, 100, 200, 400, 800, 1500, 2500, 3500, 4500, 5500, 6500, 7500, 10000, 15000, 20000):
+            norm = [1e-5, 2000, cols, dtype, P, cols]
+            calls += [("conef_norm_forward", [None, *norm, 0, 0, P, P, 0, 0, 2 * P, cols, 0, 0, 0]),
+                      ("conef_norm_forward", ["drop", *norm, P, cols, P, P, P, cols, 2 * P, cols, 0, 0, 0]),
+                      ("conef_norm_backward", [None, 2000, cols, dtype, P, cols, P, cols, P, P, P, 0, 0, 2 * P, cols, 0, 0, P, P, P, 0])]
+        for rounding in (0, 1):
+            for rows in (100, 16384):
+                for q, qt in ((P, 0), (0, P), (P, P)):
+                    calls.append(("conef_mx_quantise", [P, 8192, rows, 8192, dtype, rounding, 1, 0, 0, q, q, qt, qt, 0]))
+        for rows in (100, 16384):
+            calls.append(("conef_mx_dequantise", [P, P, rows, 8192, P, 8192, dtype, 0]))
+        for beta in (0.0, 1.0):
+            # rows of few, of 32, of 64, on four and eight waves; tiny whole and in parts; small, wide, large, streamed
+            for m, n, k in ((1, 8192, 128), (1, 50304, 2048), (1, 8192, 2048), (1, 2048, 8192), (32, 8192, 128), (32, 8192, 2048), (32, 2048, 8192),
+                            (64, 8192, 128), (64, 2048, 2048), (64, 2048, 8192), (512, 512, 512), (256, 256, 8192), (4096, 4096, 512), (8192, 8192, 512),
+                            (4096, 4096, 2048), (4096, 8192, 2048), (4096, 4096, 8192), (8192, 2048, 8192), (8160, 8192, 8192), (8192, 8192, 2048),
+                            (8192, 16392, 2048), (16384, 16384, 2048)):
+                for c in (P, P + 4):
+                    calls.append(("conef_mx_product", [P, P, P, P, m, n, k, 1.0, beta, c, n, dtype, P, 0]))
+    reached = set()
+    for code, seen in record(calls):
+        assert code == 0
+        for launch in seen:
+            groups(launch)
+            reached.add(launch[0])
+    there = {n for n in record.names() if any(k in n for k in ("k_dropout", "k_norm_", "k_mx_"))}
+    assert reached == there, sorted(there - reached)
