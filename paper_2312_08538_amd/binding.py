@@ -629,6 +629,7 @@ class Model:
             current = torch.cuda.current_device
             _raw_stream = (lambda: raw(current())) if raw else (lambda: torch.cuda.current_stream().cuda_stream)
         return _raw_stream()
+
     def step(self, buf, step: int, Q_out=None):
         conef_step(self.ctx, buf["grads"], buf["codes"], buf["scales"], buf["Q"], buf["P"],
                    buf["Q"] if Q_out is None else Q_out, buf["ws"], step, self.stream_handle())

@@ -157,8 +157,8 @@ struct Turned {
 // A workgroup takes 64 rows of 128 columns, or 128 rows of 64 columns if it quantises by columns too.  By rows: a wave takes 16 rows, of which
 // its lanes read 32 columns at a time, four lanes a block, and writes the 256 bytes of that piece together.  By columns: the same on
 // the tile in LDS, turned, the four octets of a block 16 lanes apart.
-// 8192 x 8192 in bf16 both ways: to nearest 45 us, 205 MB at 4.5 TB/s (by rows alone 32 us at 5.2), bound by memory; stochastically 65 us, bound by
-// its vector instructions, 113 an octet and way: 40 for the Philox call, eight conversions, which take 16 cycles each, 19 around
+// 8192 x 8192 in bf16 both ways: to nearest 45 us, 205 MB at 4.5 TB/s (by rows alone 32 us, 170 MB at 5.3, by columns alone 37), bound by memory;
+// stochastically 60 us (35 by rows, 39 by columns), both ways bound by its vector instructions, 113 an octet and way: 40 for the Philox call, eight conversions, which take 16 cycles each, 19 around
 // them.  (The same with the codes computed from integers: 100 us.)  64 columns and not 128 in the tile (of four waves): 1203 x 1000 in fp32 4.7 / 6.0 us.
 template <bool BF16, bool STOCHASTIC, bool BY_ROWS, bool BY_COLS, int WAVES>
 __global__ __launch_bounds__(64 * WAVES) void k_mx_quantise(MxQuantArgs a, int64_t row_pieces, int64_t col_pieces, int64_t col_tiles,
@@ -260,7 +260,8 @@ __device__ __forceinline__ void values(uint32_t c, uint32_t byte, float v[8])
 }
 
 // What a packed operand stands for: 16 rows a wave, 128 columns, so that a store writes whole lines (four lanes a block, 64 bytes of a line at a time: 29 us, in
-// fp32 111).  Bound by memory: 8192 x 8192 in bf16 26 us, 170 MB at 6.6 TB/s, in fp32 48, 304 MB at 6.3.
+// fp32 111).  Bound by memory: 8192 x 8192 in bf16 22 us, 170 MB at 7.8 TB/s, of which a part stays in the last cache, in fp32 48, 304 MB at 6.3.  A store's 128 bytes
+// are cut where the tile is, so rows that do not begin on a line have two lines to each: 8192 x 8191 takes 55 us, in fp32 136, 16384 x 3000 in fp32 84 (bf16 23).
 template <bool BF16, bool PAST>
 __global__ __launch_bounds__(kThreads) void k_mx_dequantise(MxDequantArgs a, int64_t pieces, int64_t groups)
 {

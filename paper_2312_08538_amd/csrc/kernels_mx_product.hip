@@ -8,9 +8,10 @@
 //
 // What bounds it: the instructions alone, from registers, reach 6.8 PFLOP/s on zeros and 5.8 on random operands, where the card's power sets the
 // clock (the form of 32 x 32 x 64 9.8 and 6.6, but it adds to twice as many accumulators a product, and the same kernels on it took 259 us
-// for 8192 x 8192 x 8192 where this one took 246, 251 for 4096 x 50304 x 2048 where this one took 235).  8192 x 8192 x 8192 reaches 4.7 PFLOP/s, 8192 x
-// 2048 x 8192 4.4: without its loads to LDS it would take 208 us, without its reads from there 219, without either 189, without the products 126.  With a
-// shorter axis C's bytes and each tile's beginning weigh more: 4096 x 50304 x 2048 4.0, without stores 4.3.
+// for 8192 x 8192 x 8192 where this one then took 246, 251 for 4096 x 50304 x 2048 where this one took 235: both before tiles streamed).  8192 x 8192 x 8192
+// reaches 4.7 PFLOP/s (231 to 240 us: the clock goes by the box), 8192 x 2048 x 8192 4.5.  Of those 240 us, without its loads to LDS it would take 208, without its
+// reads from there 219, without either 189, without the products 126.  With a shorter axis C's bytes and each tile's beginning weigh more: 4096 x 50304 x 2048
+// 3.9 (213 to 218 us), without stores 10 us less.  Its 3152 tiles are 12.3 for each of 256 workgroups, so a thirteenth turn, with 80 of them at work, is some 5 % of it.
 #include <algorithm>
 #include <type_traits>
 #include <utility>
@@ -63,7 +64,8 @@ __device__ __forceinline__ void wait_loads()
     asm volatile("" ::: "memory");
 }
 
-// alpha v (+ beta c) to N neighbours of a row of C
+// alpha v (+ beta c) to N neighbours of a row of C.  Old elements of C are read one at a time, behind the last product, and in large tiles what is written then
+// does not go by way of LDS: with beta = 1 4096 x 50304 x 2048 takes 619 us (beta = 0: 213), 4096 x 8192 x 2048 93 (40), 8192 x 2048 x 8192 85 (61).
 template <bool BF16, bool ADD, bool PAST, int N>
 __device__ __forceinline__ void store_row(const MxProductArgs &a, int64_t row, int64_t col, const float *v)
 {
@@ -496,7 +498,7 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void k_mx_stream(MxProductArgs a, 
 }
 
 // Few rows of A (16 MT at most): a workgroup takes 16 rows of B, read once, straight to registers; its WAVES waves take pieces of the long axis in
-// turn, and their sums are added in order.  8 x 8192 x 2048: 3.3 us with its launch, 9 MB.
+// turn, and their sums are added in order.  8 x 8192 x 2048, 9 MB: 2.8 us in a graph, 3.3 with the host's launch.
 template <bool BF16, bool ADD, int MT, int WAVES>
 __global__ __launch_bounds__(64 * WAVES) void k_mx_rows(MxProductArgs a, int pieces)
 {
@@ -576,14 +578,16 @@ struct Choice {
 
 constexpr int kCus = 256;
 
-// Which kernel, and whether C goes past the caches.  us of a call (bf16 C unless said otherwise), the one taken / the next best:
-//   rows (m <= 64)   8 x 8192 x 2048 2.7 / 4.8 tiny, 1 x 50304 x 2048 11.3 / 11.8 small, 64 x 2048 x 8192 5.4 / 9.8 tiny in 4 parts; but more
+// Which kernel, and whether C goes past the caches.  us of a call (bf16 C, beta = 0 unless said otherwise; two kernels' times are of one session, and between
+// sessions and boxes a kernel's differs by some 4 %), the one taken / the next best:
+//   rows (m <= 64)   8 x 8192 x 2048 2.7 / 4.8 tiny (in graphs), 1 x 50304 x 2048 11.3 / 11.8 small, 64 x 2048 x 8192 5.4 / 9.8 tiny in 4 parts; but more
 //                    than 16 rows are read once a workgroup, which with enough of these costs more than a tile's waste: 64 x 50304 x 16384 166 / 86
 //                    small, 32 x 16384 x 8192 15.1 / 13.3, 64 x 50304 x 2048 21.6 / 19.4 (32 x 50304 x 2048 14.5 / 17.7)
 //   stream, 256 x 256, one tile after the other, from four to a CU on:  8192 x 8192 x 8192 240 / 249 large, 4096 x 50304 x 2048 215 / 224 wide,
 //                    8192 x 8192 x 1536 53 / 58 wide, 16384 x 8192 x 4096 241 / 261 large; but 6144 x 4096 x 2048 33 / 28 wide
 //   large, 256 x 256, eight waves: the fewest reads, but a CU holds one workgroup, which begins and ends alone; for long sums of fewer
-//                    tiles: 8192 x 2048 x 8192 62 / 71 wide, 64 stream
+//                    tiles: 8192 x 2048 x 8192, one tile a CU, 60 / 66 wide, 63 stream.  No rule here looks at what is left of tiles over CUs: a little more than one
+//                    a CU are two turns, and there wide ones would be better: 8448 x 2048 x 8192 99 / 88 wide, 100 stream; 9984 x 2048 x 8192 101 / 91 wide
 //   wide, 256 x 128, two workgroups a CU:  4096 x 8192 x 2048 38.7 / 38.1 stream; 8192 x 32768 x 1024 184 small / 190
 //   small, 128 x 128, three a CU:  2048 x 50304 x 768 65 / 69 wide, 2048 x 2048 x 16384 43 / 56 in 2 parts, 60 tiny; 512 x 8192 x 2048 9.4 / 11.8 tiny; and where half
 //                    of a larger one would be beyond the rows: 128 x 50304 x 8192 37 / 50 large

@@ -26,7 +26,7 @@ inline bool in_registers(int64_t cols, int most) { return cols <= most; }
 constexpr int threads_of(int g) { return g > kThreads ? g : kThreads; }
 
 // ---------------------------------------------------------------- dropout
-// An octet a thread, which takes one Philox call.  Bound by memory: 16384 x 4096 in bf16 with a residual 67 us, 403 MB at 6.0 TB/s (a copy of
+// An octet a thread, which takes one Philox call.  Bound by memory: 16384 x 4096 in bf16 with a residual 68 us, 403 MB at 5.9 TB/s (a copy of
 // a gigabyte reaches 5.1; some of this comes from the card's last cache); the 150 vector instructions of an octet hide behind the loads.
 template <bool BF16>
 __global__ __launch_bounds__(kThreads) void k_dropout(DropoutArgs a, uint32_t octets, uint32_t per_row)
@@ -104,7 +104,7 @@ __device__ __forceinline__ void load_columns(const float *p, int cols, int t, fl
 
 // G lanes hold a row, V octets each: octet v of lane t starts at column 8 (t + G v).  The next row's octets are on their way while a row is
 // worked on.  Bound by memory where there are rows enough for that: 16384 x 2048 in bf16 with dropout and residual 54 us, 268 MB at 5.0 TB/s,
-// without them 26 us; 777 x 5003 in fp32, three rows a CU, 18 us, 62 MB at 3.5 TB/s.
+// without them 26 us; 777 x 5003 in fp32, three rows a CU, 17 us, 62 MB at 3.7 TB/s: as many rows again as are worked on are on their way, and no more.
 template <bool BF16, int G, int V, bool FUSED>
 __global__ __launch_bounds__(threads_of(G)) void k_norm_forward(NormArgs a)
 {
@@ -270,8 +270,8 @@ __device__ __forceinline__ void finish_dz(const NormArgs &a, int64_t row, int64_
 
 // Each workgroup takes every gridDim-th row (or 256 / G of them) and keeps its share of dgamma and dbeta in registers, since a lane
 // sees the same columns in every row; k_norm_columns adds the shares.  The next row's octets are on their way while a row is worked on.
-// Bound by memory: 16384 x 2048 in bf16 with dropout and residual's gradient 58 us, 336 MB and 8 MB of shares at 5.9 TB/s, and 4 us for the
-// shares' sum; 777 x 5003 in fp32 19 us, 88 MB at 4.6 TB/s, and 4 us.
+// Bound by memory: 16384 x 2048 in bf16 with dropout and residual's gradient 68 us with the shares' sum, of which that is 4: 336 MB, and 8 MB of
+// shares written and read, at 5.2 TB/s; 777 x 5003 in fp32 23 us with 4 of them, 88 MB and twice 10 at 4.7 TB/s.
 template <bool BF16, int G, int V>
 __global__ __launch_bounds__(threads_of(G)) void k_norm_backward(NormArgs a)
 {
@@ -408,7 +408,8 @@ __global__ __launch_bounds__(threads_of(G)) void k_norm_backward(NormArgs a)
 }
 
 // Rows of more than 12288 columns: two sweeps by a workgroup; the sums over rows are k_norm_column_parts's, which reads dy and z once more: with it 4096 x 16384 in
-// bf16 takes 235 us.  (1024 threads have 128 registers each, too few for an fp32 row of 16384 even with the shares in LDS.)
+// bf16 takes 233 us, where its bytes, read once, are 134 at a copy's rate.  (1024 threads have 128 registers each, too few for an fp32 row of 16384 even with the
+// shares in LDS.  A bf16 row might fit; the bound is the same for both types, and a kernel for it alone was not tried.)
 template <bool BF16>
 __global__ __launch_bounds__(kThreads) void k_norm_backward_long(NormArgs a)
 {
@@ -511,8 +512,8 @@ void by_lanes(int64_t cols, F &&go)
     else if constexpr (8 * G < MOST) by_lanes<G + 128, MOST>(cols, go);
 }
 
-// Lanes to a row and octets a lane.  Rows of up to 256 columns share a wave, 8 to 32 lanes each: 32768 x 100 in bf16 forward 9.0 us, backward 16.3 with both
-// kernels, a wave to a row 19 and 29; 32768 x 7, which eight lanes load element by element, 5.7 and 14, by a workgroup to a row 78 and 118.
+// Lanes to a row and octets a lane.  Rows of up to 256 columns share a wave, 8 to 32 lanes each: 32768 x 100 in bf16 forward 8.8 us, backward 15.3 with both
+// kernels, a wave to a row 19 and 29; 32768 x 7, which eight lanes load element by element, 5.4 and 12.2, by a workgroup to a row 78 and 118 (all fused).
 // Otherwise two octets a lane at most, which registers hold together with the next row on its way.  A wave to a row needs no barrier, but
 // four octets a lane (2048 columns) take 256 registers: the backward pass of 16384 x 2048 in bf16 then takes 86 us, with a workgroup to
 // a row 75.  Rows of 2048 columns to MOST take one octet a lane: up to 8192 in the fused forward pass, 6144 in the backward pass, whose registers hold
@@ -549,12 +550,12 @@ void by_width(int64_t cols, F &&go)
 }
 
 // Workgroups of the forward pass: about as many as the card holds at a time, so that each works on several rows with the next one on its way.
-// us, so many / 2048: 777 x 5003 fp32 fused 20.6 / 22.9, 8192 x 1024 bf16 13.8 / 15.2, 4096 x 16384 bf16 102 / 118.
+// us, so many / 2048, all fused: 777 x 5003 fp32 16.7 / 18.6, 8192 x 1024 bf16 14.0 / 14.9, 4096 x 16384 bf16 100 / 117, 16384 x 2048 bf16 53 / 53.
 constexpr int forward_groups(int g, int v) { return g * v > 640 ? 512 : g * v > 256 || v == 2 ? 768 : 1536; }
 
 // Workgroups of the backward pass of rows of that width: as many as the card holds at a time (four or two of 256 threads a CU, else two or one), but
 // four rows each (two of more than 512 lanes) where that leaves one for a CU (every other one): their shares of dgamma and dbeta are written and read
-// again.  us with both kernels, so / with a row each: 1024 x 2048 bf16 11.3 / 18.0, 500 x 4000 bf16 12.5 / 17.6, 256 x 5003 fp32 12.8 / 15.8.  At most
+// again.  us with both kernels, not fused, so / with a row each: 1024 x 2048 bf16 11.3 / 18.0, 500 x 4000 bf16 12.5 / 17.6, 256 x 5003 fp32 12.8 / 15.8.  At most
 // 512 of 256 threads, or 1024: 16384 x 2048 bf16 fused 65 / 73 (not fused 42 / 41), fp32 134 / 139; 256 of 512 threads, or 512: 4096 x 4096
 // fp32 66 / 69, 16384 x 3500 fp32 208 / 228.
 int64_t parts_of(int64_t rows, int64_t cols)
