@@ -153,7 +153,7 @@ __global__ __launch_bounds__(threads_of(G)) void k_norm_forward(NormArgs a)
 #pragma unroll
             for (int i = 0; i < 8; ++i) sum[0] += z[v][i];
         group_sum<G, 1>(sum, red, turn);
-        const float mean = sum[0] * inv;
+        const float mean = sum[0] / (float)a.cols;          // (not times inv: a constant row's mean is its value, and 1 / sqrt(eps) multiplies what it is off by)
         sum[0] = 0.0f;
 #pragma unroll
         for (int v = 0; v < V; ++v)
@@ -209,7 +209,7 @@ __global__ __launch_bounds__(kThreads) void k_norm_forward_long(NormArgs a)
                 if (i < left) sum[0] += z[i];
         }
         group_sum<kThreads, 1>(sum, red, turn);
-        const float mean = sum[0] * inv;
+        const float mean = sum[0] / (float)a.cols;          // (as above)
         sum[0] = 0.0f;
         for (int64_t col = 8 * threadIdx.x; col < a.cols; col += 8 * kThreads) {
             const int left = (int)(a.cols - col < 8 ? a.cols - col : 8);

@@ -315,3 +315,20 @@ def test_a_rounding_that_is_none_is_refused(env, rounding):  # noqa: F811
     with pytest.raises(B.ConefError) as e:
         B.conef_mx_quantise(torch.zeros(4, 8, device="cuda:0"), rounding, 0, 0, 0, q, None, B.Model.stream_handle())
     assert e.value.code == B.EINVAL
+
+
+@pytest.mark.parametrize("bf16", [False, True])
+@pytest.mark.parametrize("cols", [5, 7, 15, 49, 63, 126, 255, 510, 784, 1020, 2041, 4095, 8190, 12286, 16381, 25088, 25998])
+def test_constant_rows_have_their_value_as_their_mean(env, cols, bf16):  # noqa: F811
+    """Sums of these values are exact in fp32 in any order (cols 125 < 2^24), so the mean is too, and the norm is beta."""
+    torch, B = env
+    v = torch.tensor([1000.0, -2000.0, 16000.0, 1.0], device="cuda:0")
+    x = v[:, None].expand(4, cols).contiguous().to(torch.bfloat16 if bf16 else torch.float32)
+    v = x[:, 0].float()
+    gamma, beta = (column_vector(torch, t) for t in norm_inputs(1, cols, False, 7)[2:])
+    y, z, mean, rstd = torch.empty_like(x), torch.empty_like(x), torch.empty_like(v), torch.empty_like(v)
+    for fused in (False, True):
+        B.conef_norm_forward(None, 1e-5, x, torch.zeros_like(x) if fused else None, gamma, beta, z if fused else None, y, mean, rstd, B.Model.stream_handle())
+        assert torch.equal(mean, v)
+        assert torch.equal(y, beta.to(x.dtype)[None, :].expand(4, cols))
+        assert bool(((rstd.double() - 1e-5 ** -0.5).abs() <= 4 * U * rstd).all())
