@@ -157,15 +157,14 @@ def _packed_room(rows, cols):
 
 def _packed(codes, scales, rows, cols):
     """8-bit codes [rows, cols] and scale bytes [rows, ceil(cols / 128)] in the packed layout: codes in squares of 16 rows by 16
-    columns, eight squares of a block of 128 columns one after the other, block by block; scales 64 rows of a block together, the four
-    rows r, r + 16, r + 32, r + 48 next to each other."""
+    columns, eight squares of a block of 128 columns one after the other, block by block; scales block by block, all rows together."""
     r, c = _padded(rows, cols)
     full = torch.zeros(r, c, dtype=torch.uint8, device=codes.device)
     full[:rows, :cols] = codes
     out = full.view(r // 16, 16, c // 128, 8, 16).permute(0, 2, 3, 1, 4).contiguous().view(-1)
     sc = torch.zeros(r, c // 128, dtype=torch.uint8, device=codes.device)
     sc[:rows] = scales
-    return out, sc.view(r // 64, 4, 16, c // 128).permute(0, 3, 2, 1).contiguous().view(-1)
+    return out, sc.t().contiguous().view(-1)
 
 
 def prepare(case, seed):
@@ -253,7 +252,7 @@ def _unpacked(packed, rows, cols):
     """Codes and scale bytes of a packed operand, row by row."""
     r, c = _padded(rows, cols)
     codes = packed[0].view(r // 16, c // 128, 8, 16, 16).permute(0, 3, 1, 2, 4).reshape(r, c)[:rows, :cols]
-    return codes, packed[1].view(r // 64, c // 128, 16, 4).permute(0, 3, 2, 1).reshape(r, c // 128)[:rows]
+    return codes, packed[1].view(c // 128, r).t()[:rows]
 
 
 def _rounded(x, form):
@@ -423,7 +422,7 @@ def exact(case, seed):
             r, c = _padded(rows, cols)
             i, j = torch.arange(r, device=_device())[:, None], torch.arange(c, device=_device())[None, :]
             byte = packed[0][(i // 16 * (c // 128) + j // 128) * 2048 + j // 16 % 8 * 256 + i % 16 * 16 + j % 16]
-            scale = packed[1][(i // 64 * (c // 128) + j // 128) * 64 + i % 16 * 4 + i % 64 // 16]
+            scale = packed[1][j // 128 * r + i]
             return (torch.from_numpy(table).to(_device())[byte.long()] * torch.exp2(scale.double() - 127))[:rows, :cols]
 
         return values(s["a"], case["m"], case["k"], case["form"]) @ values(s["b"], case["n"], case["k"], "e4m3").t()
