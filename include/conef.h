@@ -509,6 +509,80 @@ int conef_mx_product(const uint8_t *a_codes, const uint8_t *a_scales, const uint
                      int64_t n, int64_t k, float alpha, float beta, void *c, int64_t c_pitch, int dtype, void *workspace,
                      void *hip_stream);
 
+/* ---- A language model's step in 8 bits: quantisation and products, root-mean-square norm, and the loss of its vocabulary.
+ * What is said above of a worker's own step holds for these calls, too (no context, matrices, strides, streams, errors).
+ *
+ * 8-bit floating point with a scale for each block of 128: 128 consecutive elements of a row share a scale 2^(b - 127), b a byte
+ * (255: all of them are NaN); an element is a byte of OCP 8-bit floating point, CONEF_E4M3 (largest value 448) or CONEF_E5M2 (57344).  b is the
+ * smallest byte for which a block's largest magnitude over the scale is no larger than the format's, so nothing is cut off; elements
+ * over the scale are rounded to nearest, ties to even.  A block with an infinity or a NaN gets b = 255 and codes 0.
+ * A packed operand holds rows in 64s and columns in 128s, the rest filled with zeros; with P = ceil(cols / 128) and R the rows rounded
+ * up, element (i, j) is in
+ *   code byte   ((i / 16) P + j / 128) 2048 + (j / 16 % 8) 256 + (i % 16) 16 + j % 16          scale byte   (j / 128) R + i
+ * conef_q8_sizes       bytes of the two buffers (either pointer may be null), 16-byte aligned; sides as for conef_mx_sizes
+ * conef_q8_quantise    x by rows into codes / scales, and by columns (the rows of x's transpose) into codes_t / scales_t, sized for
+ *                      cols x rows; either pair may be null
+ * conef_q8_dequantise  the values of a packed operand, rounded to nearest where they are no values of dtype (below its normal range) */
+enum { CONEF_E4M3 = 0, CONEF_E5M2 = 1 };
+int conef_q8_sizes(int64_t rows, int64_t cols, size_t *code_bytes, size_t *scale_bytes);
+int conef_q8_quantise(const void *x, int64_t x_pitch, int64_t rows, int64_t cols, int dtype, int format, uint8_t *codes, uint8_t *scales,
+                      uint8_t *codes_t, uint8_t *scales_t, void *hip_stream);
+int conef_q8_dequantise(const uint8_t *codes, const uint8_t *scales, int64_t rows, int64_t cols, int format, void *out, int64_t out_pitch,
+                        int dtype, void *hip_stream);
+
+/* C <- alpha A B^T + beta C for packed A (m x k, of a_format) and B (n x k, of CONEF_E4M3), summed in fp32; the rest as for
+ * conef_mx_product.  A linear layer takes CONEF_E4M3 for activations and weights and CONEF_E5M2 for the gradient that comes back, which
+ * is A of both backward products. */
+int conef_q8_product_workspace(int64_t m, int64_t n, int64_t k, size_t *bytes);
+int conef_q8_product(const uint8_t *a_codes, const uint8_t *a_scales, int a_format, const uint8_t *b_codes, const uint8_t *b_scales, int64_t m,
+                     int64_t n, int64_t k, float alpha, float beta, void *c, int64_t c_pitch, int dtype, void *workspace,
+                     void *hip_stream);
+
+/* Root-mean-square norm over each row, with a residual in front of it and its output in 8 bits:
+ *   z = residual + x     y = z rstd gamma,  rstd = 1 / sqrt(mean(z^2) + eps)
+ * The sum is rounded to dtype; the rest is computed from that in 64 bits and rounded once, to y, to the codes and to rstd_out, so that codes are those of
+ * the norm itself.
+ * residual, z_out  both or neither; without them z is x
+ * gamma            device, in, cols floats          rstd_out   device, out, rows floats, may be null
+ * y                device, out, may be null          codes, scales   device, out, both or neither: y by rows as a packed operand of CONEF_E4M3
+ *                  (sides as for conef_q8_sizes).  One of the two is needed.  y and z_out must not be the same buffer. */
+int conef_rms_forward(float eps, int64_t rows, int64_t cols, int dtype, const void *x, int64_t x_pitch, const void *residual,
+                      int64_t residual_pitch, const float *gamma, void *z_out, int64_t z_pitch, void *y, int64_t y_pitch, uint8_t *codes,
+                      uint8_t *scales, float *rstd_out, void *hip_stream);
+
+/* Its backward pass.  With hat = z rstd, a = dy gamma and the mean over a row:
+ *   dz = rstd (a - hat mean(a hat)) + dz_in          dgamma = sum over rows of dy hat
+ * z, rstd          what the forward pass was taken of (z_out, or x) and left
+ * dz_in            device, in, may be null: a gradient that reaches z past the norm (the residual stream's)
+ * dz               device, out: the gradient of x, and of the residual      dgamma   device, out, cols floats.  Either may be null, not both.
+ * workspace        device, conef_rms_workspace() bytes, 16-byte aligned; may be null if dgamma is */
+int conef_rms_workspace(int64_t rows, int64_t cols, size_t *bytes);
+int conef_rms_backward(int64_t rows, int64_t cols, int dtype, const void *dy, int64_t dy_pitch, const void *z, int64_t z_pitch,
+                       const float *gamma, const float *rstd, const void *dz_in, int64_t dz_in_pitch, void *dz, int64_t dz_pitch,
+                       float *dgamma, void *workspace, void *hip_stream);
+
+/* Softmax cross entropy of a vocabulary's logits l = x w^T, which are never stored:
+ *   lse_i = log(sum over v of exp(l_iv))      loss_i = lse_i - l_(i, target_i)
+ * and its gradient: with d_iv = dloss_i (exp(l_iv - lse_i) - [v = target_i])
+ *   dx = d w                                  dw <- alpha d^T x + beta dw
+ * A target outside 0 .. vocab - 1 is none: its loss is 0 and it adds nothing to the gradients.
+ * x                device, in, tokens x width of dtype                 w         device, in, vocab x width of dtype
+ * targets          device, in, tokens 64-bit integers
+ * loss, lse        device, out, tokens floats each; lse is what the backward pass takes (either may be null, not both)
+ * dloss            device, in, tokens floats, the loss's gradient, may be null: 1 each
+ * dx               device, out, tokens x width of dtype      dw   device, out (beta = 0: not read), vocab x width of dtype.  Either may be null, not both.
+ *                  They must not overlap an input.
+ * Logits and all sums are fp32; the backward pass makes the logits again, a piece of the vocabulary at a time, and rounds d to dtype for the products that
+ * take it.
+ * workspace        device, conef_loss_workspace() bytes (of either pass), 256-byte aligned
+ * tokens, vocab, width < 2^30, width and vocab at least 1; also tokens ceil(vocab / 8), tokens ceil(width / 8), vocab ceil(width / 8) < 2^32 */
+int conef_loss_workspace(int64_t tokens, int64_t vocab, int64_t width, int dtype, size_t *bytes);
+int conef_loss_forward(int64_t tokens, int64_t vocab, int64_t width, int dtype, const void *x, int64_t x_pitch, const void *w, int64_t w_pitch,
+                       const int64_t *targets, float *loss, float *lse, void *workspace, void *hip_stream);
+int conef_loss_backward(int64_t tokens, int64_t vocab, int64_t width, int dtype, const void *x, int64_t x_pitch, const void *w, int64_t w_pitch,
+                        const int64_t *targets, const float *lse, const float *dloss, float alpha, float beta, void *dx, int64_t dx_pitch,
+                        void *dw, int64_t dw_pitch, void *workspace, void *hip_stream);
+
 #ifdef __cplusplus
 }
 #endif

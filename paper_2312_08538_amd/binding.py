@@ -30,7 +30,10 @@ EXPORTS = ["conef_init", "conef_sizes", "conef_offsets", "conef_step", "conef_st
            "conef_cs_init", "conef_csc_init", "conef_cs_sizes", "conef_cs_offsets", "conef_cs_hash", "conef_cs_step",
            "conef_cs_step_p", "conef_cs_step_q", "conef_cs_step_err", "conef_cs_decode_error",
            "conef_dropout_forward", "conef_dropout_backward", "conef_norm_forward", "conef_norm_workspace", "conef_norm_backward",
-           "conef_mx_sizes", "conef_mx_quantise", "conef_mx_dequantise", "conef_mx_product_workspace", "conef_mx_product"]
+           "conef_mx_sizes", "conef_mx_quantise", "conef_mx_dequantise", "conef_mx_product_workspace", "conef_mx_product",
+           "conef_q8_sizes", "conef_q8_quantise", "conef_q8_dequantise", "conef_q8_product_workspace", "conef_q8_product", "conef_rms_forward",
+           "conef_rms_workspace", "conef_rms_backward", "conef_loss_workspace", "conef_loss_forward", "conef_loss_backward"]
+E4M3, E5M2 = 0, 1
 MX_NEAREST, MX_STOCHASTIC = 0, 1
 
 
@@ -128,6 +131,17 @@ def lib() -> ctypes.CDLL:
     L.conef_mx_dequantise.argtypes = [vp, vp, i64, i64, vp, i64, i32, vp]
     L.conef_mx_product_workspace.argtypes = [i64, i64, i64, szp]
     L.conef_mx_product.argtypes = [vp, vp, vp, vp, i64, i64, i64, f32, f32, vp, i64, i32, vp, vp]
+    L.conef_q8_sizes.argtypes = [i64, i64, szp, szp]
+    L.conef_q8_quantise.argtypes = [vp, i64, i64, i64, i32, i32, vp, vp, vp, vp, vp]
+    L.conef_q8_dequantise.argtypes = [vp, vp, i64, i64, i32, vp, i64, i32, vp]
+    L.conef_q8_product_workspace.argtypes = [i64, i64, i64, szp]
+    L.conef_q8_product.argtypes = [vp, vp, i32, vp, vp, i64, i64, i64, f32, f32, vp, i64, i32, vp, vp]
+    L.conef_rms_forward.argtypes = [f32, i64, i64, i32, vp, i64, vp, i64, vp, vp, i64, vp, i64, vp, vp, vp, vp]
+    L.conef_rms_workspace.argtypes = [i64, i64, szp]
+    L.conef_rms_backward.argtypes = [i64, i64, i32, vp, i64, vp, i64, vp, vp, vp, i64, vp, i64, vp, vp, vp]
+    L.conef_loss_workspace.argtypes = [i64, i64, i64, i32, szp]
+    L.conef_loss_forward.argtypes = [i64, i64, i64, i32, vp, i64, vp, i64, vp, vp, vp, vp, vp]
+    L.conef_loss_backward.argtypes = [i64, i64, i64, i32, vp, i64, vp, i64, vp, vp, vp, f32, f32, vp, i64, vp, i64, vp, vp]
     L.conef_destroy.argtypes = [vp]
     L.conef_destroy.restype = None
     L.conef_strerror.argtypes = [i32]
@@ -502,6 +516,9 @@ def face():
         # (hipStreamGetDevice: of the runtime that the library is linked to)
         addresses = (ctypes.cast(getattr(lib(), c), ctypes.c_void_p).value for c in (*("conef_" + c for c in calls), "hipStreamGetDevice"))
         module.connect(conef_drop, ConefError, tuple(addresses))
+        calls = ("q8_quantise", "q8_dequantise", "q8_product_workspace", "q8_product", "rms_forward", "rms_workspace", "rms_backward", "loss_workspace",
+                 "loss_forward", "loss_backward")
+        module.connect_8bit(tuple(ctypes.cast(getattr(lib(), "conef_" + c), ctypes.c_void_p).value for c in calls))
         _face = module
     return _face
 
@@ -560,6 +577,73 @@ def conef_mx_product_workspace(m: int, n: int, k: int) -> int:
 def conef_mx_product(a, b, k: int, alpha: float, beta: float, c, workspace, stream=0):
     """c [m, n] <- alpha A B^T + beta c of the packed operands a (m x k) and b (n x k)."""
     (_face or face()).mx_product(a, b, k, alpha, beta, c, workspace, stream)
+
+
+# a language model's step in 8 bits: quantisation and products, root-mean-square norm, the loss of its vocabulary
+def conef_q8_sizes(rows: int, cols: int) -> dict:
+    v = [ctypes.c_size_t() for _ in range(2)]
+    _check(lib().conef_q8_sizes(rows, cols, *[ctypes.byref(x) for x in v]), "conef_q8_sizes")
+    return {"code_bytes": int(v[0].value), "scale_bytes": int(v[1].value)}
+
+
+def q8_alloc(rows: int, cols: int, device="cuda:0"):
+    """(codes, scales): zeroed buffers of a packed rows x cols operand, as the conef_q8_* calls take it."""
+    import torch
+
+    s = conef_q8_sizes(rows, cols)
+    return tuple(torch.zeros(s[k], dtype=torch.uint8, device=device) for k in ("code_bytes", "scale_bytes"))
+
+
+def conef_q8_quantise(x, format: int, packed, packed_t, stream=0):
+    """packed: (codes, scales) of x by rows, packed_t: of its transpose by rows; either may be None."""
+    (_face or face()).q8_quantise(x, format, packed, packed_t, stream)
+
+
+def conef_q8_dequantise(packed, format: int, out, stream=0):
+    (_face or face()).q8_dequantise(packed, format, out, stream)
+
+
+def conef_q8_product_workspace(m: int, n: int, k: int) -> int:
+    v = ctypes.c_size_t()
+    _check(lib().conef_q8_product_workspace(m, n, k, ctypes.byref(v)), "conef_q8_product_workspace")
+    return int(v.value)
+
+
+def conef_q8_product(a, a_format: int, b, k: int, alpha: float, beta: float, c, workspace, stream=0):
+    """c [m, n] <- alpha A B^T + beta c of the packed operands a (m x k, of a_format) and b (n x k, of E4M3)."""
+    (_face or face()).q8_product(a, a_format, b, k, alpha, beta, c, workspace, stream)
+
+
+def conef_rms_forward(eps: float, x, residual, gamma, z_out, y, packed, rstd_out, stream=0):
+    """packed: (codes, scales) of the norm by rows, or None; y: the norm itself, or None."""
+    (_face or face()).rms_forward(eps, x, residual, gamma, z_out, y, packed, rstd_out, stream)
+
+
+def conef_rms_workspace(rows: int, cols: int) -> int:
+    v = ctypes.c_size_t()
+    _check(lib().conef_rms_workspace(rows, cols, ctypes.byref(v)), "conef_rms_workspace")
+    return int(v.value)
+
+
+def conef_rms_backward(dy, z, gamma, rstd, dz_in, dz, dgamma, workspace, stream=0):
+    (_face or face()).rms_backward(dy, z, gamma, rstd, dz_in, dz, dgamma, workspace, stream)
+
+
+def conef_loss_workspace(tokens: int, vocab: int, width: int, dtype) -> int:
+    """dtype: torch.float32 or torch.bfloat16, x's and w's (or F32, BF16)."""
+    kind = dtype if isinstance(dtype, int) else {"torch.float32": F32, "torch.bfloat16": BF16}.get(str(dtype), -1)
+    v = ctypes.c_size_t()
+    _check(lib().conef_loss_workspace(tokens, vocab, width, kind, ctypes.byref(v)), "conef_loss_workspace")
+    return int(v.value)
+
+
+def conef_loss_forward(x, w, targets, loss, lse, workspace, stream=0):
+    (_face or face()).loss_forward(x, w, targets, loss, lse, workspace, stream)
+
+
+def conef_loss_backward(x, w, targets, lse, dloss, alpha: float, beta: float, dx, dw, workspace, stream=0):
+    """dx [tokens, width]; dw [vocab, width] <- alpha times the gradient + beta dw; either may be None."""
+    (_face or face()).loss_backward(x, w, targets, lse, dloss, alpha, beta, dx, dw, workspace, stream)
 
 
 def conef_set_timing(ctx, on: bool):

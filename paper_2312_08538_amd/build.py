@@ -10,7 +10,7 @@ import sys
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libconef.so")
-SOURCES = ["api.cpp", "plan.cpp", "kernels_generic.hip", "kernels_orth.hip", "kernels_octet.hip", "kernels_strip.hip", "kernels_ragged.hip", "kernels_mixed.hip", "kernels_mfma.hip", "kernels_pack.hip", "kernels_sketch.hip", "kernels_small.hip", "kernels_walk.hip", "layers.cpp", "kernels_norm.hip", "kernels_mx.hip", "kernels_mx_product.hip"]
+SOURCES = ["api.cpp", "plan.cpp", "kernels_generic.hip", "kernels_orth.hip", "kernels_octet.hip", "kernels_strip.hip", "kernels_ragged.hip", "kernels_mixed.hip", "kernels_mfma.hip", "kernels_pack.hip", "kernels_sketch.hip", "kernels_small.hip", "kernels_walk.hip", "layers.cpp", "kernels_norm.hip", "kernels_mx.hip", "kernels_mx_product.hip", "kernels_q8.hip", "kernels_q8_product.hip", "kernels_rms.hip", "kernels_loss.hip"]
 FACE = os.path.join(HERE, "_face.so")
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 

@@ -1,4 +1,4 @@
-// Python's way into the operators of a training step (conef_dropout_*, conef_norm_*, conef_mx_*): reads shapes, types, pitches and
+// Python's way into the operators of a training step (conef_dropout_*, conef_norm_*, conef_mx_*, conef_q8_*, conef_rms_*, conef_loss_*): reads shapes, types, pitches and
 // addresses off torch tensors, refuses those that do not fit or are on another device than the stream, and calls the library by the
 // addresses that it was given.  A small operator's time is that of its call: a dropout of one row takes 3.1 us, of which 2.9 are the launch
 // (marshalled in Python and by ctypes 5.0), a layer norm of one row 4.0 with what its caller does around it (7.6).
@@ -25,6 +25,20 @@ struct Library {
     decltype(&conef_mx_product) mx_product;
     int (*stream_device)(void *stream, int *device);            // the runtime's hipStreamGetDevice
 } L;
+
+// the calls of a step in 8 bits
+struct Library8 {
+    decltype(&conef_q8_quantise) q8_quantise;
+    decltype(&conef_q8_dequantise) q8_dequantise;
+    decltype(&conef_q8_product_workspace) q8_product_workspace;
+    decltype(&conef_q8_product) q8_product;
+    decltype(&conef_rms_forward) rms_forward;
+    decltype(&conef_rms_workspace) rms_workspace;
+    decltype(&conef_rms_backward) rms_backward;
+    decltype(&conef_loss_workspace) loss_workspace;
+    decltype(&conef_loss_forward) loss_forward;
+    decltype(&conef_loss_backward) loss_backward;
+} L8;
 
 PyObject *drop_type, *error_type;       // conef_drop and ConefError of the binding
 
@@ -180,6 +194,16 @@ float *vector(const Stream &st, PyObject *o, int64_t n)
     return static_cast<float *>(t.data_ptr());
 }
 
+// n contiguous 64-bit integers
+const int64_t *integers(const Stream &st, PyObject *o, int64_t n)
+{
+    const at::Tensor &t = tensor(o);
+    if (!on_device(t) || t.dim() != 1 || t.size(0) != n || t.scalar_type() != at::kLong || !t.is_contiguous())
+        refuse(std::to_string(n) + " contiguous 64-bit integers on the device are wanted, not " + about(t));
+    check_place(st, t);
+    return static_cast<const int64_t *>(t.data_ptr());
+}
+
 // a buffer of at least so many bytes, or none
 void *room(const Stream &st, PyObject *o, size_t bytes)
 {
@@ -191,11 +215,11 @@ void *room(const Stream &st, PyObject *o, size_t bytes)
     return t.data_ptr();
 }
 
-// codes and scales of a packed operand, or none
+// codes and scales of a packed operand, or none: of 4 bits and 32 elements a scale, or of other `bits` and `block`
 struct Packed {
     uint8_t *codes = nullptr, *scales = nullptr;
 
-    Packed(const Stream &st, PyObject *o, int64_t rows, int64_t cols)
+    Packed(const Stream &st, PyObject *o, int64_t rows, int64_t cols, int bits = 4, int block = 32)
     {
         if (o == Py_None) return;
         PyObject *both[2] = {};
@@ -211,8 +235,8 @@ struct Packed {
         // (in 128 bits: the library refuses sides that 64 bits could not count)
         const unsigned __int128 elements = (unsigned __int128)(((uint64_t)rows + 63) / 64) * (((uint64_t)cols + 127) / 128) * 8192;
         if (rows < 0 || cols < 0 || elements >> 62) refuse("sides out of range");
-        codes = static_cast<uint8_t *>(room(st, both[0], (size_t)(elements / 2)));
-        scales = static_cast<uint8_t *>(room(st, both[1], (size_t)(elements / 32)));
+        codes = static_cast<uint8_t *>(room(st, both[0], (size_t)(elements * bits / 8)));
+        scales = static_cast<uint8_t *>(room(st, both[1], (size_t)(elements / block)));
     }
 };
 
@@ -343,6 +367,134 @@ PyObject *mx_product(PyObject *, PyObject *const *p, Py_ssize_t n)
     });
 }
 
+int8_t format(PyObject *o)
+{
+    const int64_t v = integer(o);
+    if (v != CONEF_E4M3 && v != CONEF_E5M2) refuse("CONEF_E4M3 or CONEF_E5M2 is wanted");
+    return (int8_t)v;
+}
+
+PyObject *q8_quantise(PyObject *, PyObject *const *p, Py_ssize_t n)
+{
+    return call("conef_q8_quantise", n, 5, [&] {
+        const Stream st(p[4]);
+        const Matrix x(st, p[0]);
+        const int f = format(p[1]);
+        const Packed q(st, p[2], x.rows, x.cols, 8, 128), t(st, p[3], x.cols, x.rows, 8, 128);
+        return unlocked([&] { return L8.q8_quantise(x.data, x.pitch, x.rows, x.cols, x.kind, f, q.codes, q.scales, t.codes, t.scales, st.handle); });
+    });
+}
+
+PyObject *q8_dequantise(PyObject *, PyObject *const *p, Py_ssize_t n)
+{
+    return call("conef_q8_dequantise", n, 4, [&] {
+        const Stream st(p[3]);
+        const Matrix out(st, p[2]);
+        const int f = format(p[1]);
+        const Packed q(st, p[0], out.rows, out.cols, 8, 128);
+        return unlocked([&] { return L8.q8_dequantise(q.codes, q.scales, out.rows, out.cols, f, out.data, out.pitch, out.kind, st.handle); });
+    });
+}
+
+PyObject *q8_product(PyObject *, PyObject *const *p, Py_ssize_t n)
+{
+    return call("conef_q8_product", n, 9, [&] {
+        const Stream st(p[8]);
+        const Matrix c(st, p[6]);
+        const int f = format(p[1]);
+        const int64_t k = integer(p[3]);
+        const Packed a(st, p[0], c.rows, k, 8, 128), b(st, p[2], c.cols, k, 8, 128);
+        const float alpha = real(p[4]), beta = real(p[5]);
+        size_t bytes = 0;
+        if (p[7] != Py_None && L8.q8_product_workspace(c.rows, c.cols, k, &bytes) != CONEF_OK) return (int)CONEF_EINVAL;
+        void *ws = room(st, p[7], bytes);
+        return unlocked([&] {
+            return L8.q8_product(a.codes, a.scales, f, b.codes, b.scales, c.rows, c.cols, k, alpha, beta, c.data, c.pitch, c.kind, ws, st.handle);
+        });
+    });
+}
+
+PyObject *rms_forward(PyObject *, PyObject *const *p, Py_ssize_t n)
+{
+    return call("conef_rms_forward", n, 9, [&] {
+        const Stream st(p[8]);
+        const float eps = real(p[0]);
+        const Matrix x(st, p[1]), r(st, p[2], x), z(st, p[4], x), y(st, p[5], x);
+        const float *gamma = vector(st, p[3], x.cols);
+        const Packed q(st, p[6], x.rows, x.cols, 8, 128);
+        float *rstd = vector(st, p[7], x.rows);
+        return unlocked([&] {
+            return L8.rms_forward(eps, x.rows, x.cols, x.kind, x.data, x.pitch, r.data, r.pitch, gamma, z.data, z.pitch, y.data, y.pitch, q.codes,
+                                  q.scales, rstd, st.handle);
+        });
+    });
+}
+
+PyObject *rms_backward(PyObject *, PyObject *const *p, Py_ssize_t n)
+{
+    return call("conef_rms_backward", n, 9, [&] {
+        const Stream st(p[8]);
+        const Matrix dy(st, p[0]), z(st, p[1], dy), in(st, p[4], dy), dz(st, p[5], dy);
+        const float *gamma = vector(st, p[2], dy.cols), *rstd = vector(st, p[3], dy.rows);
+        float *dgamma = vector(st, p[6], dy.cols);
+        size_t bytes = 0;
+        if (p[7] != Py_None && L8.rms_workspace(dy.rows, dy.cols, &bytes) != CONEF_OK) return (int)CONEF_EINVAL;
+        void *ws = room(st, p[7], bytes);
+        return unlocked([&] {
+            return L8.rms_backward(dy.rows, dy.cols, dy.kind, dy.data, dy.pitch, z.data, z.pitch, gamma, rstd, in.data, in.pitch, dz.data, dz.pitch,
+                                   dgamma, ws, st.handle);
+        });
+    });
+}
+
+// x [tokens, width] and w [vocab, width] of one type
+struct Logits {
+    const Matrix x, w;
+
+    Logits(const Stream &st, PyObject *px, PyObject *pw) : x(st, px), w(st, pw)
+    {
+        if (w.cols != x.cols || w.kind != x.kind)
+            refuse("a matrix of " + std::to_string(x.cols) + (x.kind == CONEF_F32 ? " columns of fp32" : " columns of bf16") + " is wanted, not " + about(tensor(pw)));
+    }
+    void *room_of(const Stream &st, PyObject *o) const
+    {
+        size_t bytes = 0;
+        if (o != Py_None && L8.loss_workspace(x.rows, w.rows, x.cols, x.kind, &bytes) != CONEF_OK) refuse("sides out of range");
+        return room(st, o, bytes);
+    }
+};
+
+PyObject *loss_forward(PyObject *, PyObject *const *p, Py_ssize_t n)
+{
+    return call("conef_loss_forward", n, 7, [&] {
+        const Stream st(p[6]);
+        const Logits l(st, p[0], p[1]);
+        const int64_t *targets = integers(st, p[2], l.x.rows);
+        float *loss = vector(st, p[3], l.x.rows), *lse = vector(st, p[4], l.x.rows);
+        void *ws = l.room_of(st, p[5]);
+        return unlocked([&] {
+            return L8.loss_forward(l.x.rows, l.w.rows, l.x.cols, l.x.kind, l.x.data, l.x.pitch, l.w.data, l.w.pitch, targets, loss, lse, ws, st.handle);
+        });
+    });
+}
+
+PyObject *loss_backward(PyObject *, PyObject *const *p, Py_ssize_t n)
+{
+    return call("conef_loss_backward", n, 11, [&] {
+        const Stream st(p[10]);
+        const Logits l(st, p[0], p[1]);
+        const int64_t *targets = integers(st, p[2], l.x.rows);
+        const float *lse = vector(st, p[3], l.x.rows), *dloss = vector(st, p[4], l.x.rows);
+        const float alpha = real(p[5]), beta = real(p[6]);
+        const Matrix dx(st, p[7], l.x), dw(st, p[8], l.w);
+        void *ws = l.room_of(st, p[9]);
+        return unlocked([&] {
+            return L8.loss_backward(l.x.rows, l.w.rows, l.x.cols, l.x.kind, l.x.data, l.x.pitch, l.w.data, l.w.pitch, targets, lse, dloss, alpha, beta,
+                                    dx.data, dx.pitch, dw.data, dw.pitch, ws, st.handle);
+        });
+    });
+}
+
 // connect(conef_drop, ConefError, addresses of the library's calls in Library's order)
 PyObject *connect(PyObject *, PyObject *args)
 {
@@ -371,9 +523,28 @@ PyObject *connect(PyObject *, PyObject *args)
     Py_RETURN_NONE;
 }
 
+// connect_8bit(addresses of the library's calls in Library8's order), behind connect
+PyObject *connect_8bit(PyObject *, PyObject *args)
+{
+    unsigned long long at[10];
+    if (!PyArg_ParseTuple(args, "(KKKKKKKKKK)", at, at + 1, at + 2, at + 3, at + 4, at + 5, at + 6, at + 7, at + 8, at + 9)) return nullptr;
+    L8.q8_quantise = reinterpret_cast<decltype(L8.q8_quantise)>(at[0]);
+    L8.q8_dequantise = reinterpret_cast<decltype(L8.q8_dequantise)>(at[1]);
+    L8.q8_product_workspace = reinterpret_cast<decltype(L8.q8_product_workspace)>(at[2]);
+    L8.q8_product = reinterpret_cast<decltype(L8.q8_product)>(at[3]);
+    L8.rms_forward = reinterpret_cast<decltype(L8.rms_forward)>(at[4]);
+    L8.rms_workspace = reinterpret_cast<decltype(L8.rms_workspace)>(at[5]);
+    L8.rms_backward = reinterpret_cast<decltype(L8.rms_backward)>(at[6]);
+    L8.loss_workspace = reinterpret_cast<decltype(L8.loss_workspace)>(at[7]);
+    L8.loss_forward = reinterpret_cast<decltype(L8.loss_forward)>(at[8]);
+    L8.loss_backward = reinterpret_cast<decltype(L8.loss_backward)>(at[9]);
+    Py_RETURN_NONE;
+}
+
 #define FAST(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(name)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {{"connect", connect, METH_VARARGS, nullptr}, FAST(dropout_forward), FAST(dropout_backward), FAST(norm_forward),
-                         FAST(norm_backward), FAST(mx_quantise), FAST(mx_dequantise), FAST(mx_product), {nullptr, nullptr, 0, nullptr}};
+                         FAST(norm_backward), FAST(mx_quantise), FAST(mx_dequantise), FAST(mx_product), {"connect_8bit", connect_8bit, METH_VARARGS, nullptr}, FAST(q8_quantise), FAST(q8_dequantise), FAST(q8_product),
+                         FAST(rms_forward), FAST(rms_backward), FAST(loss_forward), FAST(loss_backward), {nullptr, nullptr, 0, nullptr}};
 #undef FAST
 
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_face", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};

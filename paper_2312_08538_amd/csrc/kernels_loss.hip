@@ -1,0 +1,643 @@
+// Softmax cross entropy of a vocabulary's logits l = x w^T and its gradient, without the logits ever being in memory.
+//
+// Forward: the product's tiles end in each row's largest logit and the sum of exponentials over it, 8 bytes a row and tile; k_loss_join adds these up.
+// Backward, a piece of the vocabulary at a time: the tiles of the product end in d = dloss / s (exp(l - lse) - [v = target]), rounded to the
+// operands' type and packed twice, by rows for dx = s d w and by columns for dw = s d^T x.  s is the largest magnitude of dloss: then, where all tokens weigh the same, a
+// target's element is next to -1 and rounding does not move it; dloss itself, 1 / 3686 say, is off by 0.3 % in bf16, and so would all targets' shares be.  Both products then read operands whose steps lie as the matrix
+// instructions take them; w and x are turned for that (k_loss_turn), which is a pass over memory where a product is width (tokens) times as much work.
+// A sum over the vocabulary goes from piece to piece in fp32.
+#include <algorithm>
+#include <cstdint>
+
+#include "product_device.h"
+#include "turned_device.h"
+
+namespace conef {
+
+namespace {
+
+constexpr float kLog2e = 1.44269504088896341f;
+constexpr float kLeast = -3.402823466e38f;              // below every logit but -inf
+
+__device__ __forceinline__ float exp_of(float v) { return __builtin_amdgcn_exp2f(v * kLog2e); }
+
+template <int KIND>
+constexpr bool is_bf16() { return KIND == Kind::BF16; }
+
+// ---------------------------------------------------------------- operands
+// Rows of any alignment as a packed operand: an octet a lane, sixteen rows of four octets a wave.
+template <bool BF16>
+__global__ __launch_bounds__(256) void k_loss_pack(Rows x, int64_t rows, int64_t cols, int64_t padded_rows, int steps, uint8_t *out)
+{
+    constexpr int kStep = BF16 ? 64 : 32;               // elements
+    const int64_t fours = ((int64_t)steps * kStep + 31) / 32, id = (int64_t)group_index() * 4 + (threadIdx.x >> 6);
+    const int lane = threadIdx.x & 63;
+    const int64_t row = id / fours * 16 + (lane & 15), col = id % fours * 32 + 8 * (lane >> 4);
+    if (row >= padded_rows) return;
+    const Octet<BF16> o = fetch_octet<BF16>(x.data, row * x.pitch + col, row < rows ? octet_left(cols - col) : 0);
+    uint8_t *to = out + ((row >> 4) * steps + col / kStep) * 2048 + col % kStep / (BF16 ? 8 : 4) * 256 + (row & 15) * 16;
+#pragma unroll
+    for (int h = 0; h < (BF16 ? 1 : 2); ++h) *reinterpret_cast<uint4 *>(to + h * 256) = make_uint4(o.w[h][0], o.w[h][1], o.w[h][2], o.w[h][3]);
+}
+
+// The transpose as a packed operand: its rows are x's columns, its long axis x's rows.  128 rows of 64 columns a workgroup, turned in LDS.
+template <bool BF16>
+__global__ __launch_bounds__(256) void k_loss_turn(Rows x, int64_t rows, int64_t cols, int64_t padded_cols, int steps, uint8_t *out)
+{
+    constexpr int kStep = BF16 ? 64 : 32;
+    __shared__ __attribute__((aligned(16))) Turned<BF16> tile;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int64_t strips = padded_cols / 64, group = group_index(), row0 = group / strips * 128, col0 = group % strips * 64, depth = (int64_t)steps * kStep;
+    if (row0 >= depth) return;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int r = i * 32 + (threadIdx.x >> 3), c = (threadIdx.x & 7) * 8;
+        const int64_t row = row0 + r;
+        tile.put(r, c, fetch_octet<BF16>(x.data, row * x.pitch + col0 + c, row < rows ? octet_left(cols - col0 - c) : 0));
+    }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int r = (i * 4 + (lane >> 4)) * 8;
+        const int64_t row = row0 + r, col = col0 + 16 * wave;
+        const Octet<BF16> o = tile.get(r, 16 * wave, lane);
+        if (row >= depth) continue;
+        uint8_t *to = out + ((col >> 4) * steps + row / kStep) * 2048 + row % kStep / (BF16 ? 8 : 4) * 256 + (lane & 15) * 16;
+#pragma unroll
+        for (int h = 0; h < (BF16 ? 1 : 2); ++h) *reinterpret_cast<uint4 *>(to + h * 256) = make_uint4(o.w[h][0], o.w[h][1], o.w[h][2], o.w[h][3]);
+    }
+}
+
+// ---------------------------------------------------------------- forward
+struct StatArgs {
+    int64_t tokens = 0, vocab = 0;          // vocab: of the piece, which begins at `first`
+    int64_t first = 0;
+    const int64_t *targets = nullptr;
+    float2 *stats = nullptr;                // a tile's largest logit of a row, and the sum of exp(l - that)
+    float *hit = nullptr;                   // the target's logit
+};
+
+template <int KIND, bool BY_ROWS, int WM, int WN, int TM, int TN, int STAGES, int OCC>
+__global__ __launch_bounds__(64 * WM * WN, OCC) void k_loss_logits(StatArgs p, Side a, Side b, Shape z)
+{
+    typedef Tile<KIND, BY_ROWS, WM, WN, TM, TN, STAGES> T;
+    __shared__ __attribute__((aligned(1024))) uint8_t lds[T::kBytes];
+    if (group_index() >= (uint32_t)z.items) return;
+    const Place at = place_of(z, (int)group_index());
+    typename T::Sums acc;
+    T::run(a, b, z, at.m * T::kM, at.n * T::kN, 0, z.steps, lds, acc);
+    const int lane = threadIdx.x & 63;
+    const int64_t col0 = (int64_t)at.n * T::kN + T::wave_n() * TN * 32 + 4 * (lane >> 5);
+    float2 *red = reinterpret_cast<float2 *>(lds);          // [WN][kM]
+    wait_loads<0>();
+    __syncthreads();
+    const bool whole = (int64_t)(at.n + 1) * T::kN <= p.vocab;
+#pragma unroll
+    for (int i = 0; i < TM; ++i) {
+        const int r = (T::wave_m() * TM + i) * 32 + (lane & 31);
+        const int64_t row = (int64_t)at.m * T::kM + r;
+        if (!whole) {
+#pragma unroll
+            for (int j = 0; j < TN; ++j)
+#pragma unroll
+                for (int e = 0; e < 16; ++e)
+                    if (col0 + j * 32 + 8 * (e >> 2) + (e & 3) >= p.vocab) acc[j][i][e] = -__builtin_inff();
+        }
+        const int64_t of = row < p.tokens ? p.targets[row] : -1, target = of < 0 ? -1 : of - p.first - col0;
+        float most = kLeast;
+#pragma unroll
+        for (int j = 0; j < TN; ++j)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+                most = fmaxf(most, acc[j][i][e]);
+                if (target == j * 32 + 8 * (e >> 2) + (e & 3) && (whole || col0 + target < p.vocab)) p.hit[row] = acc[j][i][e];
+            }
+        auto swap = __builtin_amdgcn_permlane32_swap(__float_as_uint(most), __float_as_uint(most), false, false);
+        most = fmaxf(__uint_as_float(swap[0]), __uint_as_float(swap[1]));
+        float sum = 0.0f;
+#pragma unroll
+        for (int j = 0; j < TN; ++j)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) sum += exp_of(acc[j][i][e] - most);
+        swap = __builtin_amdgcn_permlane32_swap(__float_as_uint(sum), __float_as_uint(sum), false, false);
+        sum = __uint_as_float(swap[0]) + __uint_as_float(swap[1]);
+        if (lane < 32) red[T::wave_n() * T::kM + r] = make_float2(most, sum);
+    }
+    __syncthreads();
+    for (int r = threadIdx.x; r < T::kM; r += T::kThreads) {
+        const int64_t row = (int64_t)at.m * T::kM + r;
+        if (row >= p.tokens) continue;
+        float most = kLeast, sum = 0.0f;
+#pragma unroll
+        for (int w = 0; w < WN; ++w) most = fmaxf(most, red[w * T::kM + r].x);
+#pragma unroll
+        for (int w = 0; w < WN; ++w) sum += red[w * T::kM + r].y * exp_of(red[w * T::kM + r].x - most);
+        p.stats[at.n * p.tokens + row] = make_float2(most, sum);
+    }
+}
+
+// lse and loss of sixteen rows a workgroup: 64 threads to a row, a share of its tiles each.
+__global__ __launch_bounds__(1024) void k_loss_join(const float2 *stats, const float *hit, const int64_t *targets, int64_t tokens, int64_t vocab, int tiles,
+                                                    float *loss, float *lse)
+{
+    __shared__ float2 red[64][16];
+    const int r = threadIdx.x & 15, part = threadIdx.x >> 4;
+    const int64_t row = (int64_t)group_index() * 16 + r;
+    float most = kLeast, sum = 0.0f;
+    if (row < tokens)
+        for (int t = part; t < tiles; t += 64 * 8) {
+            float2 v[8];
+#pragma unroll
+            for (int u = 0; u < 8; ++u) v[u] = t + 64 * u < tiles ? stats[(int64_t)(t + 64 * u) * tokens + row] : make_float2(kLeast, 0.0f);
+            float high = most;
+#pragma unroll
+            for (int u = 0; u < 8; ++u) high = fmaxf(high, v[u].x);
+            sum *= exp_of(most - high);
+#pragma unroll
+            for (int u = 0; u < 8; ++u) sum += v[u].y * exp_of(v[u].x - high);
+            most = high;
+        }
+    red[part][r] = make_float2(most, sum);
+    for (int step = 32; step; step /= 2) {
+        __syncthreads();
+        if (part >= step) continue;
+        const float2 u = red[part][r], v = red[part + step][r];
+        const float high = fmaxf(u.x, v.x);
+        red[part][r] = make_float2(high, u.y * exp_of(u.x - high) + v.y * exp_of(v.x - high));
+    }
+    if (part || row >= tokens) return;
+    const double total = (double)red[0][r].x + log((double)red[0][r].y);
+    if (lse) lse[row] = (float)total;
+    if (loss) {
+        const int64_t t = targets[row];
+        loss[row] = t >= 0 && t < vocab ? (float)(total - (double)hit[row]) : 0.0f;
+    }
+}
+
+// ---------------------------------------------------------------- backward
+// The largest finite magnitude of dloss, or 1 if that is 0.
+__global__ __launch_bounds__(1024) void k_loss_scale(const float *dloss, int64_t tokens, float *scale)
+{
+    __shared__ float red[16];
+    float most = 0.0f;
+    for (int64_t i = threadIdx.x; i < tokens; i += 8 * 1024) {
+        float v[8];
+#pragma unroll
+        for (int u = 0; u < 8; ++u) v[u] = i + 1024 * u < tokens ? fabsf(dloss[i + 1024 * u]) : 0.0f;
+#pragma unroll
+        for (int u = 0; u < 8; ++u) most = v[u] < __builtin_inff() ? fmaxf(most, v[u]) : most;
+    }
+#pragma unroll
+    for (int d = 32; d; d /= 2) most = fmaxf(most, __shfl_xor(most, d));
+    if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = most;
+    __syncthreads();
+    if (threadIdx.x) return;
+    for (int w = 1; w < 16; ++w) most = fmaxf(most, red[w]);
+    *scale = most > 0.0f ? most : 1.0f;
+}
+
+struct GradArgs {
+    int64_t tokens = 0, vocab = 0, first = 0, all = 0;          // vocab: of the piece, which begins at `first` of `all`
+    const int64_t *targets = nullptr;
+    const float *lse = nullptr, *dloss = nullptr, *scale = nullptr;         // dloss null: 1 each, and so is the scale
+    uint8_t *by_rows = nullptr, *by_cols = nullptr;             // either may be null
+    int64_t padded_tokens = 0, padded_vocab = 0;                // to 64
+};
+
+// Eight neighbours along a packed operand's long axis, `at` its row and `along` the first of them
+template <bool BF16>
+__device__ __forceinline__ void put_packed(uint8_t *out, int64_t at, int64_t along, int64_t depth, const float v[8])
+{
+    constexpr int kStep = BF16 ? 64 : 32;
+    uint8_t *to = out + ((at >> 4) * (depth / kStep) + along / kStep) * 2048 + along % kStep / (BF16 ? 8 : 4) * 256 + (at & 15) * 16;
+    if constexpr (BF16) {
+        *reinterpret_cast<uint4 *>(to) = make_uint4(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7]));
+    } else {
+        *reinterpret_cast<float4 *>(to) = make_float4(v[0], v[1], v[2], v[3]);
+        *reinterpret_cast<float4 *>(to + 256) = make_float4(v[4], v[5], v[6], v[7]);
+    }
+}
+
+template <int KIND, bool BY_ROWS, int WM, int WN, int TM, int TN, int STAGES, int OCC>
+__global__ __launch_bounds__(64 * WM * WN, OCC) void k_loss_gradient(GradArgs p, Side a, Side b, Shape z)
+{
+    typedef Tile<KIND, BY_ROWS, WM, WN, TM, TN, STAGES> T;
+    constexpr bool BF16 = is_bf16<KIND>();
+    __shared__ __attribute__((aligned(1024))) uint8_t lds[T::kBytes];
+    if (group_index() >= (uint32_t)z.items) return;
+    const Place at = place_of(z, (int)group_index());
+    typename T::Sums acc;
+    T::run(a, b, z, at.m * T::kM, at.n * T::kN, 0, z.steps, lds, acc);
+    const int lane = threadIdx.x & 63;
+    float *mine = reinterpret_cast<float *>(lds) + T::wave() * 32 * T::kPitch;
+    wait_loads<0>();
+    __syncthreads();
+    const int64_t col0 = (int64_t)at.n * T::kN + T::wave_n() * TN * 32;
+#pragma unroll
+    for (int i = 0; i < TM; ++i) {
+        const int64_t row0 = (int64_t)at.m * T::kM + (T::wave_m() * TM + i) * 32;
+#pragma unroll
+        for (int j = 0; j < TN; ++j)
+#pragma unroll
+            for (int q = 0; q < 4; ++q)
+                *reinterpret_cast<f32x4 *>(mine + (lane & 31) * T::kPitch + j * 32 + 8 * q + 4 * (lane >> 5)) =
+                    f32x4{acc[j][i][4 * q], acc[j][i][4 * q + 1], acc[j][i][4 * q + 2], acc[j][i][4 * q + 3]};
+        __builtin_amdgcn_wave_barrier();
+        constexpr int kAcross = TN * 4, kHigh = 64 / kAcross;
+#pragma unroll
+        for (int t = 0; t < 32 / kHigh; ++t) {
+            const int r = t * kHigh + lane / kAcross, c = lane % kAcross * 8;
+            const int64_t row = row0 + r, col = col0 + c;
+            float *from = mine + r * T::kPitch + c;
+            float v[8], share = 0.0f, lse = 0.0f;
+            int64_t target = -1;
+            if (row < p.tokens) {
+                const int64_t of = p.targets[row];
+                if (of >= 0 && of < p.all) {
+                    share = p.dloss ? p.dloss[row] / *p.scale : 1.0f;
+                    lse = p.lse[row];
+                    target = of - p.first - col;
+                } else {
+                    target = INT64_MIN;             // no target: no gradient
+                }
+            } else {
+                target = INT64_MIN;
+            }
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const float d = exp_of(from[e] - lse) - (target == e ? 1.0f : 0.0f);
+                v[e] = target != INT64_MIN && col + e < p.vocab ? share * d : 0.0f;
+            }
+            *reinterpret_cast<f32x4 *>(from) = f32x4{v[0], v[1], v[2], v[3]};
+            *reinterpret_cast<f32x4 *>(from + 4) = f32x4{v[4], v[5], v[6], v[7]};
+            if (p.by_rows && row < p.padded_tokens && col < p.padded_vocab) put_packed<BF16>(p.by_rows, row, col, p.padded_vocab, v);
+        }
+        __builtin_amdgcn_wave_barrier();
+        if (p.by_cols) {
+            constexpr int kWide = TN * 32, kTall = 64 / kWide;             // columns that a wave takes at a time, and octets of rows
+#pragma unroll
+            for (int t = 0; t < 4 / kTall; ++t) {
+                const int c = lane % kWide, r = (t * kTall + lane / kWide) * 8;
+                float v[8];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) v[e] = mine[(r + e) * T::kPitch + c];
+                if (row0 + r < p.padded_tokens && col0 + c < p.padded_vocab) put_packed<BF16>(p.by_cols, col0 + c, row0 + r, p.padded_tokens, v);
+            }
+        }
+        __builtin_amdgcn_wave_barrier();
+    }
+}
+
+// out <- alpha (scale sum + base) + beta out
+struct SumArgs {
+    int64_t m = 0, n = 0;
+    float alpha = 1.0f, beta = 0.0f;
+    const float *scale = nullptr;           // null: 1
+    const float *base = nullptr;            // m x n, dense: what earlier pieces came to
+    RowsOut out;
+    float *partials = nullptr;              // of the long axis in parts: m x n each
+};
+
+template <bool BF16>
+__device__ __forceinline__ void put_sum(const SumArgs &p, int64_t row, int64_t col, int left, float v[8])
+{
+    if (p.scale) {
+        const float s = *p.scale;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = s * v[i];
+    }
+    if (p.base) {
+        float b[8];
+        load_octet<false>(p.base, row * p.n + col, left, b);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = b[i] + v[i];
+    }
+    if (p.beta != 0.0f) put_octet<BF16, true, false>(p.out, row, col, left, p.alpha, p.beta, v);
+    else put_octet<BF16, false, false>(p.out, row, col, left, p.alpha, 0.0f, v);
+}
+
+template <int KIND, bool BF16, int WM, int WN, int TM, int TN, int STAGES, int OCC>
+__global__ __launch_bounds__(64 * WM * WN, OCC) void k_loss_product(SumArgs p, Side a, Side b, Shape z)
+{
+    typedef Tile<KIND, false, WM, WN, TM, TN, STAGES> T;
+    __shared__ __attribute__((aligned(1024))) uint8_t lds[T::kBytes];
+    if (group_index() >= (uint32_t)z.items) return;
+    const Place at = place_of(z, (int)group_index());
+    const int first = at.part * z.per_part;
+    typename T::Sums acc;
+    T::run(a, b, z, at.m * T::kM, at.n * T::kN, first, min(z.per_part, z.steps - first), lds, acc);
+    T::octets(acc, lds, [&](int r, int c, float v[8]) {
+        const int64_t row = (int64_t)at.m * T::kM + r, col = (int64_t)at.n * T::kN + c;
+        if (row >= p.m || col >= p.n) return;
+        if (p.partials) store_octet<false>(p.partials + (int64_t)at.part * p.m * p.n, row * p.n + col, octet_left(p.n - col), v);
+        else put_sum<BF16>(p, row, col, octet_left(p.n - col), v);
+    });
+}
+
+// Adds the parts of the long axis in their order, eight columns a thread.
+template <bool BF16>
+__global__ __launch_bounds__(256) void k_loss_parts(SumArgs p, int parts, uint32_t octets_a_row)
+{
+    const uint64_t t = (uint64_t)blockIdx.x * 256 + threadIdx.x;
+    const int64_t row = (int64_t)(t / octets_a_row), col = (int64_t)(t % octets_a_row) * 8;
+    if (row >= p.m) return;
+    const int left = octet_left(p.n - col);
+    float v[8] = {};
+    for (int part = 0; part < parts; ++part) {
+        float x[8];
+        load_octet<false>(p.partials, ((int64_t)part * p.m + row) * p.n + col, left, x);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] += x[i];
+    }
+    put_sum<BF16>(p, row, col, left, v);
+}
+
+// ---------------------------------------------------------------- plans
+inline int64_t up(int64_t v, int64_t to) { return (v + to - 1) / to * to; }
+
+// Columns of the vocabulary that are worked on at a time: d of some 2^25 elements, which with its two forms the card's last cache holds, but 4096 columns at least
+// (a product's long axis, and the bytes of dx that go from piece to piece).
+int64_t piece_of(int64_t tokens, int64_t vocab)
+{
+    const int64_t v = std::max<int64_t>(((int64_t)1 << 25) / std::max<int64_t>(tokens, 1) / 256 * 256, 4096);
+    return vocab <= v + v / 4 ? vocab : v;
+}
+
+enum Tiles { kFew, kTiny, kSmall, kLarge };
+
+Tiles tiles_for(int64_t m, int64_t n)
+{
+    auto tiles = [&](int64_t tm, int64_t tn) { return ((m + tm - 1) / tm) * ((n + tn - 1) / tn); };
+    if (std::min(m, n) > 128 && tiles(256, 256) >= 192) return kLarge;
+    if (m > 64 && tiles(128, 128) >= 200) return kSmall;
+    return kTiny;
+}
+
+struct Cut {
+    Tiles tiles;
+    int parts, per_part;
+};
+
+// of a product of `steps` along its long axis
+Cut cut_of(int64_t m, int64_t n, int64_t steps)
+{
+    const Tiles t = tiles_for(m, n);
+    if (t != kTiny) return {t, 1, (int)steps};
+    const int64_t tiles = std::max<int64_t>(((m + 63) / 64) * ((n + 63) / 64), 1);
+    const int64_t parts = std::max<int64_t>(std::min<int64_t>(2 * kCus / tiles, steps / 8), 1), per = std::max<int64_t>((steps + parts - 1) / parts, 1);
+    return {t, (int)std::max<int64_t>((steps + per - 1) / per, 1), (int)per};
+}
+
+// The workspace: both passes' packed x and a piece's packed w (where these do not lie as the kernels take them); forward: a row's statistics by tiles; backward: d by rows and by
+// columns, a piece of w turned, x turned, dx as it grows, parts of a long axis.
+struct Layout {
+    int64_t piece, esz, depth_w;                            // depth_w: bytes of a row of x or w, up to 128
+    size_t x, w, stats, hit, scale, rows, cols, w_t, x_t, grown, parts, end;
+};
+
+Layout layout_of(int64_t tokens, int64_t vocab, int64_t width, bool bf16)
+{
+    Layout l;
+    l.esz = bf16 ? 2 : 4;
+    l.piece = piece_of(tokens, vocab);
+    l.depth_w = up(width * l.esz, 128);
+    size_t at = 0;
+    auto take = [&](size_t bytes) {
+        const size_t here = at;
+        at += (bytes + 255) / 256 * 256;
+        return here;
+    };
+    const int64_t t64 = up(tokens, 64), v64 = up(l.piece, 64), d64 = up(width, 64);
+    l.x = take((size_t)t64 * l.depth_w);
+    l.w = take((size_t)v64 * l.depth_w);
+    const size_t shared = at;
+    l.stats = take((size_t)tokens * ((vocab + 63) / 64 + vocab / l.piece + 1) * sizeof(float2));
+    l.hit = take((size_t)tokens * sizeof(float));
+    const size_t forward = at;
+    at = shared;
+    l.scale = take(sizeof(float));
+    l.rows = take((size_t)t64 * v64 * l.esz);
+    l.cols = take((size_t)t64 * v64 * l.esz);
+    l.w_t = take((size_t)d64 * v64 * l.esz);
+    l.x_t = take((size_t)d64 * t64 * l.esz);
+    l.grown = take(l.piece < vocab ? (size_t)tokens * width * sizeof(float) : 0);
+    size_t most = 0;
+    for (const int64_t n : {std::min(l.piece, vocab), vocab % l.piece}) {
+        const Cut x = cut_of(tokens, width, up(n, 64) * l.esz / 128), w = cut_of(n, width, t64 * l.esz / 128);
+        most = std::max(most, x.parts > 1 ? (size_t)x.parts * tokens * width : 0);
+        most = std::max(most, w.parts > 1 ? (size_t)w.parts * n * width : 0);
+    }
+    l.parts = take(most * sizeof(float));
+    l.end = std::max(at, forward);
+    return l;
+}
+
+// x and w lie as the kernels take them
+bool in_place(const LossArgs &a, int64_t esz)
+{
+    auto fits = [&](const Rows &r) {
+        return reinterpret_cast<uintptr_t>(r.data) % 16 == 0 && r.pitch * esz % 16 == 0 && r.pitch * esz < (int64_t)1 << 29;
+    };
+    return a.width * esz % 16 == 0 && fits(a.x) && fits(a.w);
+}
+
+Rows rows_from(const Rows &r, int64_t first, int64_t esz) { return {static_cast<const uint8_t *>(r.data) + first * r.pitch * esz, r.pitch}; }
+
+template <bool BF16>
+void pack(const Rows &x, int64_t rows, int64_t cols, int64_t depth, uint8_t *out, hipStream_t st)
+{
+    const int64_t padded = up(rows, 64), steps = depth / 128, fours = (steps * (BF16 ? 64 : 32) + 31) / 32;
+    hipLaunchKernelGGL((k_loss_pack<BF16>), grid_of((padded / 16 * fours + 3) / 4), dim3(256), 0, st, x, rows, cols, padded, (int)steps, out);
+}
+
+template <bool BF16>
+void turn(const Rows &x, int64_t rows, int64_t cols, uint8_t *out, hipStream_t st)
+{
+    constexpr int kStep = BF16 ? 64 : 32;
+    const int64_t padded = up(cols, 64), depth = up(rows, 64);
+    hipLaunchKernelGGL((k_loss_turn<BF16>), grid_of((depth + 127) / 128 * (padded / 64)), dim3(256), 0, st, x, rows, cols, padded, (int)(depth / kStep), out);
+}
+
+Side packed_side(const uint8_t *data, int64_t rows)
+{
+    Side s;
+    s.data = data;
+    s.rows = (int)up(rows, 64);
+    return s;
+}
+
+template <int KIND, typename F>
+void with_operands(const LossArgs &a, const Layout &l, bool direct, int64_t first, int64_t n, hipStream_t st, F &&go)
+{
+    constexpr bool BF16 = is_bf16<KIND>();
+    const Rows w = rows_from(a.w, first, l.esz);
+    Side x_side, w_side;
+    if (direct) {
+        x_side.data = static_cast<const uint8_t *>(a.x.data), x_side.pitch = a.x.pitch * l.esz, x_side.rows = (int)a.tokens;
+        w_side.data = static_cast<const uint8_t *>(w.data), w_side.pitch = a.w.pitch * l.esz, w_side.rows = (int)n;
+        go(std::true_type{}, x_side, w_side);
+    } else {
+        pack<BF16>(w, n, a.width, l.depth_w, a.workspace + l.w, st);
+        go(std::false_type{}, packed_side(a.workspace + l.x, a.tokens), packed_side(a.workspace + l.w, n));
+    }
+}
+
+template <int KIND>
+void forward(const LossArgs &a, hipStream_t st)
+{
+    constexpr bool BF16 = is_bf16<KIND>();
+    const Layout l = layout_of(a.tokens, a.vocab, a.width, BF16);
+    const bool direct = in_place(a, l.esz);
+    if (!direct) pack<BF16>(a.x, a.tokens, a.width, l.depth_w, a.workspace + l.x, st);
+    float2 *stats = reinterpret_cast<float2 *>(a.workspace + l.stats);
+    int tiles = 0;
+    const int64_t piece = direct ? a.vocab : l.piece;
+    for (int64_t first = 0; first < a.vocab; first += piece) {
+        const int64_t n = std::min(piece, a.vocab - first);
+        with_operands<KIND>(a, l, direct, first, n, st, [&](auto by_rows, const Side &x, const Side &w) {
+            auto go = [&](auto wm, auto wn, auto tm, auto tn, auto stages, auto occ) {
+                constexpr int WM = decltype(wm)::value, WN = decltype(wn)::value, TM = decltype(tm)::value, TN = decltype(tn)::value;
+                Shape z;
+                z.steps = z.per_part = (int)(l.depth_w / 128);
+                z.last = (int)((a.width * l.esz - 1) % 128 + 1);
+                z.tiles_m = (int)((a.tokens + WM * TM * 32 - 1) / (WM * TM * 32));
+                z.tiles_n = (int)((n + WN * TN * 32 - 1) / (WN * TN * 32));
+                z.items = z.tiles_m * z.tiles_n;
+                StatArgs p;
+                p.tokens = a.tokens, p.vocab = n, p.first = first, p.targets = a.targets;
+                p.stats = stats + (int64_t)tiles * a.tokens;
+                p.hit = reinterpret_cast<float *>(a.workspace + l.hit);
+                hipLaunchKernelGGL((k_loss_logits<KIND, decltype(by_rows)::value, WM, WN, TM, TN, decltype(stages)::value, decltype(occ)::value>),
+                                   grid_of(z.items), dim3(64 * WM * WN), 0, st, p, x, w, z);
+                tiles += z.tiles_n;
+            };
+            using std::integral_constant;
+            const integral_constant<int, 1> one;
+            const integral_constant<int, 2> two;
+            const integral_constant<int, 4> four;
+            const Tiles t = tiles_for(a.tokens, n);
+            if (a.tokens <= 32) go(one, two, one, one, four, two);
+            else if (t == kTiny) go(two, two, one, one, four, two);
+            else if (t == kSmall) go(two, two, two, two, two, two);
+            else go(two, four, four, two, two, two);
+        });
+    }
+    hipLaunchKernelGGL(k_loss_join, grid_of((a.tokens + 15) / 16), dim3(1024), 0, st, stats, reinterpret_cast<float *>(a.workspace + l.hit), a.targets,
+                       a.tokens, a.vocab, tiles, a.loss, a.lse_out);
+}
+
+// out <- alpha (A B^T + base) + beta out of packed operands of `depth` elements
+template <int KIND, bool OUT>
+void product(SumArgs p, const uint8_t *a, const uint8_t *b, int64_t depth, float *partials, hipStream_t st)
+{
+    constexpr int kStep = is_bf16<KIND>() ? 64 : 32;
+    const Cut c = cut_of(p.m, p.n, depth / kStep);
+    p.partials = c.parts > 1 ? partials : nullptr;
+    auto go = [&](auto wm, auto wn, auto tm, auto tn, auto stages, auto occ) {
+        constexpr int WM = decltype(wm)::value, WN = decltype(wn)::value, TM = decltype(tm)::value, TN = decltype(tn)::value;
+        Shape z;
+        z.steps = (int)(depth / kStep);
+        z.per_part = c.per_part;
+        z.tiles_m = (int)((p.m + WM * TM * 32 - 1) / (WM * TM * 32));
+        z.tiles_n = (int)((p.n + WN * TN * 32 - 1) / (WN * TN * 32));
+        z.items = z.tiles_m * z.tiles_n * c.parts;
+        hipLaunchKernelGGL((k_loss_product<KIND, OUT, WM, WN, TM, TN, decltype(stages)::value, decltype(occ)::value>), grid_of(z.items), dim3(64 * WM * WN), 0, st, p, packed_side(a, p.m), packed_side(b, p.n), z);
+    };
+    using std::integral_constant;
+    const integral_constant<int, 1> one;
+    const integral_constant<int, 2> two;
+    const integral_constant<int, 4> four;
+    if (c.tiles == kTiny) go(two, two, one, one, four, two);
+    else if (c.tiles == kSmall) go(two, two, two, two, two, two);
+    else go(two, four, four, two, two, two);
+    if (c.parts > 1) {
+        const uint32_t octets = (uint32_t)((p.n + 7) / 8);
+        hipLaunchKernelGGL((k_loss_parts<OUT>), dim3((unsigned)(((uint64_t)p.m * octets + 255) / 256)), dim3(256), 0, st, p, c.parts, octets);
+    }
+}
+
+template <int KIND>
+void backward(const LossArgs &a, hipStream_t st)
+{
+    constexpr bool BF16 = is_bf16<KIND>();
+    const Layout l = layout_of(a.tokens, a.vocab, a.width, BF16);
+    if (a.tokens == 0) {                        // a sum of nothing
+        SumArgs p;
+        p.m = a.vocab, p.n = a.width, p.alpha = 0.0f, p.beta = a.beta, p.out = a.dw;
+        const uint32_t octets = (uint32_t)((p.n + 7) / 8);
+        if (a.dw.data) hipLaunchKernelGGL((k_loss_parts<BF16>), dim3((unsigned)(((uint64_t)p.m * octets + 255) / 256)), dim3(256), 0, st, p, 0, octets);
+        return;
+    }
+    const bool direct = in_place(a, l.esz);
+    if (!direct) pack<BF16>(a.x, a.tokens, a.width, l.depth_w, a.workspace + l.x, st);
+    float *scale = a.dloss ? reinterpret_cast<float *>(a.workspace + l.scale) : nullptr;
+    if (scale) hipLaunchKernelGGL(k_loss_scale, dim3(1), dim3(1024), 0, st, a.dloss, a.tokens, scale);
+    if (a.dw.data) turn<BF16>(a.x, a.tokens, a.width, a.workspace + l.x_t, st);
+    float *partials = reinterpret_cast<float *>(a.workspace + l.parts), *grown = reinterpret_cast<float *>(a.workspace + l.grown);
+    for (int64_t first = 0; first < a.vocab; first += l.piece) {
+        const int64_t n = std::min(l.piece, a.vocab - first);
+        with_operands<KIND>(a, l, direct, first, n, st, [&](auto by_rows, const Side &x, const Side &w) {
+            auto go = [&](auto wm, auto wn, auto tm, auto tn, auto stages, auto occ) {
+                constexpr int WM = decltype(wm)::value, WN = decltype(wn)::value, TM = decltype(tm)::value, TN = decltype(tn)::value;
+                static_assert(WM * TM * 32 % 64 == 0 && WN * TN * 32 % 64 == 0, "the packed forms are whole to 64 both ways");
+                Shape z;
+                z.steps = z.per_part = (int)(l.depth_w / 128);
+                z.last = (int)((a.width * l.esz - 1) % 128 + 1);
+                z.tiles_m = (int)((a.tokens + WM * TM * 32 - 1) / (WM * TM * 32));
+                z.tiles_n = (int)((n + WN * TN * 32 - 1) / (WN * TN * 32));
+                z.items = z.tiles_m * z.tiles_n;
+                GradArgs p;
+                p.tokens = a.tokens, p.vocab = n, p.first = first, p.all = a.vocab;
+                p.targets = a.targets, p.lse = a.lse, p.dloss = a.dloss, p.scale = scale;
+                p.by_rows = a.dx.data ? a.workspace + l.rows : nullptr;
+                p.by_cols = a.dw.data ? a.workspace + l.cols : nullptr;
+                p.padded_tokens = up(a.tokens, 64), p.padded_vocab = up(n, 64);
+                hipLaunchKernelGGL((k_loss_gradient<KIND, decltype(by_rows)::value, WM, WN, TM, TN, decltype(stages)::value, decltype(occ)::value>),
+                                   grid_of(z.items), dim3(64 * WM * WN), 0, st, p, x, w, z);
+            };
+            using std::integral_constant;
+            const integral_constant<int, 1> one;
+            const integral_constant<int, 2> two;
+            const integral_constant<int, 4> four;
+            const Tiles t = tiles_for(a.tokens, n);
+            if (t == kTiny) go(two, two, one, one, four, two);
+            else if (t == kSmall) go(two, two, two, two, two, two);
+            else go(two, four, four, two, two, two);
+        });
+        if (a.dx.data) {
+            turn<BF16>(rows_from(a.w, first, l.esz), n, a.width, a.workspace + l.w_t, st);
+            SumArgs p;
+            p.m = a.tokens, p.n = a.width, p.scale = scale;
+            p.base = first ? grown : nullptr;
+            const bool done = first + n == a.vocab;
+            p.out = done ? a.dx : RowsOut{grown, a.width};
+            if (done) product<KIND, BF16>(p, a.workspace + l.rows, a.workspace + l.w_t, up(n, 64), partials, st);
+            else product<KIND, false>(p, a.workspace + l.rows, a.workspace + l.w_t, up(n, 64), partials, st);
+        }
+        if (a.dw.data) {
+            SumArgs p;
+            p.m = n, p.n = a.width, p.scale = scale;
+            p.alpha = a.alpha, p.beta = a.beta;
+            p.out = {static_cast<uint8_t *>(a.dw.data) + first * a.dw.pitch * l.esz, a.dw.pitch};
+            product<KIND, BF16>(p, a.workspace + l.cols, a.workspace + l.x_t, up(a.tokens, 64), partials, st);
+        }
+    }
+}
+
+}  // namespace
+
+size_t loss_workspace(int64_t tokens, int64_t vocab, int64_t width, bool bf16) { return layout_of(tokens, vocab, width, bf16).end; }
+
+void launch_loss_forward(const LossArgs &a, bool bf16, hipStream_t st)
+{
+    if (bf16) forward<Kind::BF16>(a, st);
+    else forward<Kind::F32>(a, st);
+}
+
+void launch_loss_backward(const LossArgs &a, bool bf16, hipStream_t st)
+{
+    if (bf16) backward<Kind::BF16>(a, st);
+    else backward<Kind::F32>(a, st);
+}
+
+}  // namespace conef

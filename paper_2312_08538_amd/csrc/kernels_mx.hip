@@ -8,7 +8,7 @@
 // A block with an infinity or a NaN has the scale byte 255, which stands for NaN in all of it.
 #include <type_traits>
 
-#include "layers_device.h"
+#include "turned_device.h"
 
 namespace conef {
 
@@ -111,49 +111,6 @@ __device__ __forceinline__ uint32_t rows_largest(uint32_t m)
     return max((uint32_t)r[0], (uint32_t)r[1]);
 }
 
-// 128 rows of 64 columns in LDS, for reading eight rows of a column.  bf16: by transposing reads, sixteen lanes 4 rows x 16 columns at a
-// time; a row has half the banks, and where in it a piece of 16 columns lies goes by the row, so that the eight rows that half a
-// wave reads from lie in banks of their own.  fp32: element by element.
-template <bool BF16>
-struct Turned {
-    static constexpr int kPitch = BF16 ? 64 : 66;
-    typedef std::conditional_t<BF16, uint16_t, float> Elem;
-    Elem e[128 * kPitch];
-
-    static __device__ __forceinline__ int piece(int row, int col) { return ((col >> 4) ^ (row >> 1 & 1) ^ (row >> 2 & 2)) << 4; }
-
-    __device__ __forceinline__ void put(int row, int col, const Octet<BF16> &o)
-    {
-        if constexpr (BF16) {
-            *reinterpret_cast<uint4 *>(e + row * kPitch + piece(row, col) + (col & 8)) = make_uint4(o.w[0][0], o.w[0][1], o.w[0][2], o.w[0][3]);
-        } else {
-            uint2 *p = reinterpret_cast<uint2 *>(e + row * kPitch + col);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) p[i] = make_uint2(o.w[i >> 1][2 * (i & 1)], o.w[i >> 1][2 * (i & 1) + 1]);
-        }
-    }
-
-    // rows row .. row + 7 (row: a multiple of 8, the same for 16 lanes) of column col + lane % 16
-    __device__ __forceinline__ void get(int row, int col, int lane, Values &v) const
-    {
-        if constexpr (BF16) {
-            typedef short s16x4 __attribute__((ext_vector_type(4)));
-            typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
-            const int from = row + (lane >> 2 & 3);
-            const Elem *p = e + from * kPitch + piece(from, col) + 4 * (lane & 3);          // (the row four on has the same place)
-            union { s16x4 v; uint2 u; } lo, hi;
-            lo.v = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(p));
-            hi.v = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(p + 4 * kPitch));
-            Octet<BF16> o;
-            o.w[0] = u32x4_any{lo.u.x, lo.u.y, hi.u.x, hi.u.y};
-            widen<BF16>(o, v);
-        } else {
-#pragma unroll
-            for (int i = 0; i < 8; ++i) v.v[i].x = e[(row + i) * kPitch + col + (lane & 15)];
-        }
-    }
-};
-
 // A workgroup takes 64 rows of 128 columns, or 128 rows of 64 columns if it quantises by columns too.  By rows: a wave takes 16 rows, of which
 // its lanes read 32 columns at a time, four lanes a block, and writes the 256 bytes of that piece together.  By columns: the same on
 // the tile in LDS, turned, the four octets of a block 16 lanes apart.
@@ -225,7 +182,7 @@ __global__ __launch_bounds__(64 * WAVES) void k_mx_quantise(MxQuantArgs a, int64
             for (int i = 0; i < 16 / WAVES; ++i) {
                 const int b = (wave >> 2) * (16 / WAVES) + i;
                 Values v;
-                tile.get(32 * b + 8 * q16, 16 * strip, lane, v);
+                widen<BF16>(tile.get(32 * b + 8 * q16, 16 * strip, lane), v);
                 uint32_t byte;
                 const uint32_t octet = (uint32_t)col * per_col + (uint32_t)((row0 + 32 * b + 8 * q16) >> 3);
                 const uint32_t c = quantise_octet<STOCHASTIC>(v, rows_largest(largest(v)), d, octet, byte);
