@@ -87,41 +87,46 @@ __global__ __launch_bounds__(64 * WM * WN, OCC) void k_loss_logits(StatArgs p, S
     typename T::Sums acc;
     T::run(a, b, z, at.m * T::kM, at.n * T::kN, 0, z.steps, lds, acc);
     const int lane = threadIdx.x & 63;
-    const int64_t col0 = (int64_t)at.n * T::kN + T::wave_n() * TN * 32 + 4 * (lane >> 5);
+    const int64_t col0 = (int64_t)at.n * T::kN + T::wave_n() * TN * 16 + 4 * (lane >> 4);
     float2 *red = reinterpret_cast<float2 *>(lds);          // [WN][kM]
     wait_loads<0>();
     __syncthreads();
     const bool whole = (int64_t)(at.n + 1) * T::kN <= p.vocab;
 #pragma unroll
     for (int i = 0; i < TM; ++i) {
-        const int r = (T::wave_m() * TM + i) * 32 + (lane & 31);
+        const int r = (T::wave_m() * TM + i) * 16 + (lane & 15);
         const int64_t row = (int64_t)at.m * T::kM + r;
         if (!whole) {
 #pragma unroll
             for (int j = 0; j < TN; ++j)
 #pragma unroll
-                for (int e = 0; e < 16; ++e)
-                    if (col0 + j * 32 + 8 * (e >> 2) + (e & 3) >= p.vocab) acc[j][i][e] = -__builtin_inff();
+                for (int e = 0; e < 4; ++e)
+                    if (col0 + j * 16 + e >= p.vocab) acc[j][i][e] = -__builtin_inff();
         }
         const int64_t of = row < p.tokens ? p.targets[row] : -1, target = of < 0 ? -1 : of - p.first - col0;
         float most = kLeast;
 #pragma unroll
         for (int j = 0; j < TN; ++j)
 #pragma unroll
-            for (int e = 0; e < 16; ++e) {
+            for (int e = 0; e < 4; ++e) {
                 most = fmaxf(most, acc[j][i][e]);
-                if (target == j * 32 + 8 * (e >> 2) + (e & 3) && (whole || col0 + target < p.vocab)) p.hit[row] = acc[j][i][e];
+                if (target == j * 16 + e && (whole || col0 + target < p.vocab)) p.hit[row] = acc[j][i][e];
             }
-        auto swap = __builtin_amdgcn_permlane32_swap(__float_as_uint(most), __float_as_uint(most), false, false);
-        most = fmaxf(__uint_as_float(swap[0]), __uint_as_float(swap[1]));
+        // (the four lanes that share a row are sixteen apart)
+        auto across = [](float v, auto f) {
+            auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+            v = f(__uint_as_float(r[0]), __uint_as_float(r[1]));
+            r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+            return f(__uint_as_float(r[0]), __uint_as_float(r[1]));
+        };
+        most = across(most, [](float x, float y) { return fmaxf(x, y); });
         float sum = 0.0f;
 #pragma unroll
         for (int j = 0; j < TN; ++j)
 #pragma unroll
-            for (int e = 0; e < 16; ++e) sum += exp_of(acc[j][i][e] - most);
-        swap = __builtin_amdgcn_permlane32_swap(__float_as_uint(sum), __float_as_uint(sum), false, false);
-        sum = __uint_as_float(swap[0]) + __uint_as_float(swap[1]);
-        if (lane < 32) red[T::wave_n() * T::kM + r] = make_float2(most, sum);
+            for (int e = 0; e < 4; ++e) sum += exp_of(acc[j][i][e] - most);
+        sum = across(sum, [](float x, float y) { return x + y; });
+        if (lane < 16) red[T::wave_n() * T::kM + r] = make_float2(most, sum);
     }
     __syncthreads();
     for (int r = threadIdx.x; r < T::kM; r += T::kThreads) {
@@ -232,18 +237,12 @@ __global__ __launch_bounds__(64 * WM * WN, OCC) void k_loss_gradient(GradArgs p,
     float *mine = reinterpret_cast<float *>(lds) + T::wave() * 32 * T::kPitch;
     wait_loads<0>();
     __syncthreads();
-    const int64_t col0 = (int64_t)at.n * T::kN + T::wave_n() * TN * 32;
+    const int64_t col0 = (int64_t)at.n * T::kN + T::wave_n() * TN * 16;
 #pragma unroll
-    for (int i = 0; i < TM; ++i) {
-        const int64_t row0 = (int64_t)at.m * T::kM + (T::wave_m() * TM + i) * 32;
-#pragma unroll
-        for (int j = 0; j < TN; ++j)
-#pragma unroll
-            for (int q = 0; q < 4; ++q)
-                *reinterpret_cast<f32x4 *>(mine + (lane & 31) * T::kPitch + j * 32 + 8 * q + 4 * (lane >> 5)) =
-                    f32x4{acc[j][i][4 * q], acc[j][i][4 * q + 1], acc[j][i][4 * q + 2], acc[j][i][4 * q + 3]};
-        __builtin_amdgcn_wave_barrier();
-        constexpr int kAcross = TN * 4, kHigh = 64 / kAcross;
+    for (int i = 0; i < TM; i += 2) {
+        const int64_t row0 = (int64_t)at.m * T::kM + (T::wave_m() * TM + i) * 16;
+        T::turn(acc, i, mine);
+        constexpr int kAcross = TN * 2, kHigh = 64 / kAcross;
 #pragma unroll
         for (int t = 0; t < 32 / kHigh; ++t) {
             const int r = t * kHigh + lane / kAcross, c = lane % kAcross * 8;
@@ -274,7 +273,7 @@ __global__ __launch_bounds__(64 * WM * WN, OCC) void k_loss_gradient(GradArgs p,
         }
         __builtin_amdgcn_wave_barrier();
         if (p.by_cols) {
-            constexpr int kWide = TN * 32, kTall = 64 / kWide;             // columns that a wave takes at a time, and octets of rows
+            constexpr int kWide = TN * 16, kTall = 64 / kWide;             // columns that a wave takes at a time, and octets of rows
 #pragma unroll
             for (int t = 0; t < 4 / kTall; ++t) {
                 const int c = lane % kWide, r = (t * kTall + lane / kWide) * 8;
@@ -363,12 +362,19 @@ int64_t piece_of(int64_t tokens, int64_t vocab)
     return vocab <= v + v / 4 ? vocab : v;
 }
 
-enum Tiles { kFew, kTiny, kSmall, kLarge };
+constexpr std::integral_constant<int, 1> one;
+constexpr std::integral_constant<int, 2> two;
+constexpr std::integral_constant<int, 3> three;
+constexpr std::integral_constant<int, 4> four;
+constexpr std::integral_constant<int, 8> eight;
+
+enum Tiles { kTiny, kSmall, kWide, kLarge };
 
 Tiles tiles_for(int64_t m, int64_t n)
 {
     auto tiles = [&](int64_t tm, int64_t tn) { return ((m + tm - 1) / tm) * ((n + tn - 1) / tn); };
     if (std::min(m, n) > 128 && tiles(256, 256) >= 192) return kLarge;
+    if (std::min(m, n) > 128 && tiles(256, 128) >= 192) return kWide;
     if (m > 64 && tiles(128, 128) >= 200) return kSmall;
     return kTiny;
 }
@@ -500,8 +506,8 @@ void forward(const LossArgs &a, hipStream_t st)
                 Shape z;
                 z.steps = z.per_part = (int)(l.depth_w / 128);
                 z.last = (int)((a.width * l.esz - 1) % 128 + 1);
-                z.tiles_m = (int)((a.tokens + WM * TM * 32 - 1) / (WM * TM * 32));
-                z.tiles_n = (int)((n + WN * TN * 32 - 1) / (WN * TN * 32));
+                z.tiles_m = (int)((a.tokens + WM * TM * 16 - 1) / (WM * TM * 16));
+                z.tiles_n = (int)((n + WN * TN * 16 - 1) / (WN * TN * 16));
                 z.items = z.tiles_m * z.tiles_n;
                 StatArgs p;
                 p.tokens = a.tokens, p.vocab = n, p.first = first, p.targets = a.targets;
@@ -511,15 +517,12 @@ void forward(const LossArgs &a, hipStream_t st)
                                    grid_of(z.items), dim3(64 * WM * WN), 0, st, p, x, w, z);
                 tiles += z.tiles_n;
             };
-            using std::integral_constant;
-            const integral_constant<int, 1> one;
-            const integral_constant<int, 2> two;
-            const integral_constant<int, 4> four;
             const Tiles t = tiles_for(a.tokens, n);
-            if (a.tokens <= 32) go(one, two, one, one, four, two);
-            else if (t == kTiny) go(two, two, one, one, four, two);
-            else if (t == kSmall) go(two, two, two, two, two, two);
-            else go(two, four, four, two, two, two);
+            if (a.tokens <= 32) go(one, two, two, two, four, two);
+            else if (t == kTiny) go(two, two, two, two, four, two);
+            else if (t == kSmall) go(two, two, four, four, two, two);
+            else if (t == kWide) go(four, two, four, four, three, two);
+            else go(two, four, eight, four, two, two);
         });
     }
     hipLaunchKernelGGL(k_loss_join, grid_of((a.tokens + 15) / 16), dim3(1024), 0, st, stats, reinterpret_cast<float *>(a.workspace + l.hit), a.targets,
@@ -538,18 +541,15 @@ void product(SumArgs p, const uint8_t *a, const uint8_t *b, int64_t depth, float
         Shape z;
         z.steps = (int)(depth / kStep);
         z.per_part = c.per_part;
-        z.tiles_m = (int)((p.m + WM * TM * 32 - 1) / (WM * TM * 32));
-        z.tiles_n = (int)((p.n + WN * TN * 32 - 1) / (WN * TN * 32));
+        z.tiles_m = (int)((p.m + WM * TM * 16 - 1) / (WM * TM * 16));
+        z.tiles_n = (int)((p.n + WN * TN * 16 - 1) / (WN * TN * 16));
         z.items = z.tiles_m * z.tiles_n * c.parts;
         hipLaunchKernelGGL((k_loss_product<KIND, OUT, WM, WN, TM, TN, decltype(stages)::value, decltype(occ)::value>), grid_of(z.items), dim3(64 * WM * WN), 0, st, p, packed_side(a, p.m), packed_side(b, p.n), z);
     };
-    using std::integral_constant;
-    const integral_constant<int, 1> one;
-    const integral_constant<int, 2> two;
-    const integral_constant<int, 4> four;
-    if (c.tiles == kTiny) go(two, two, one, one, four, two);
-    else if (c.tiles == kSmall) go(two, two, two, two, two, two);
-    else go(two, four, four, two, two, two);
+    if (c.tiles == kTiny) go(two, two, two, two, four, two);
+    else if (c.tiles == kSmall) go(two, two, four, four, two, two);
+    else if (c.tiles == kWide) go(four, two, four, four, three, two);
+    else go(two, four, eight, four, two, two);
     if (c.parts > 1) {
         const uint32_t octets = (uint32_t)((p.n + 7) / 8);
         hipLaunchKernelGGL((k_loss_parts<OUT>), dim3((unsigned)(((uint64_t)p.m * octets + 255) / 256)), dim3(256), 0, st, p, c.parts, octets);
@@ -579,12 +579,12 @@ void backward(const LossArgs &a, hipStream_t st)
         with_operands<KIND>(a, l, direct, first, n, st, [&](auto by_rows, const Side &x, const Side &w) {
             auto go = [&](auto wm, auto wn, auto tm, auto tn, auto stages, auto occ) {
                 constexpr int WM = decltype(wm)::value, WN = decltype(wn)::value, TM = decltype(tm)::value, TN = decltype(tn)::value;
-                static_assert(WM * TM * 32 % 64 == 0 && WN * TN * 32 % 64 == 0, "the packed forms are whole to 64 both ways");
+                static_assert(WM * TM * 16 % 64 == 0 && WN * TN * 16 % 64 == 0, "the packed forms are whole to 64 both ways");
                 Shape z;
                 z.steps = z.per_part = (int)(l.depth_w / 128);
                 z.last = (int)((a.width * l.esz - 1) % 128 + 1);
-                z.tiles_m = (int)((a.tokens + WM * TM * 32 - 1) / (WM * TM * 32));
-                z.tiles_n = (int)((n + WN * TN * 32 - 1) / (WN * TN * 32));
+                z.tiles_m = (int)((a.tokens + WM * TM * 16 - 1) / (WM * TM * 16));
+                z.tiles_n = (int)((n + WN * TN * 16 - 1) / (WN * TN * 16));
                 z.items = z.tiles_m * z.tiles_n;
                 GradArgs p;
                 p.tokens = a.tokens, p.vocab = n, p.first = first, p.all = a.vocab;
@@ -595,14 +595,11 @@ void backward(const LossArgs &a, hipStream_t st)
                 hipLaunchKernelGGL((k_loss_gradient<KIND, decltype(by_rows)::value, WM, WN, TM, TN, decltype(stages)::value, decltype(occ)::value>),
                                    grid_of(z.items), dim3(64 * WM * WN), 0, st, p, x, w, z);
             };
-            using std::integral_constant;
-            const integral_constant<int, 1> one;
-            const integral_constant<int, 2> two;
-            const integral_constant<int, 4> four;
             const Tiles t = tiles_for(a.tokens, n);
-            if (t == kTiny) go(two, two, one, one, four, two);
-            else if (t == kSmall) go(two, two, two, two, two, two);
-            else go(two, four, four, two, two, two);
+            if (t == kTiny) go(two, two, two, two, four, two);
+            else if (t == kSmall) go(two, two, four, four, two, two);
+            else if (t == kWide) go(four, two, four, four, three, two);
+            else go(two, four, eight, four, two, two);
         });
         if (a.dx.data) {
             turn<BF16>(rows_from(a.w, first, l.esz), n, a.width, a.workspace + l.w_t, st);

@@ -109,7 +109,7 @@ __global__ __launch_bounds__(256) void k_q8_join(Q8ProductArgs p, int parts, uin
     put_octet<BF16, ADD, false>(p.c, row, col, left, p.alpha, p.beta, v);
 }
 
-enum Tiles { kRows, kTiny, kSmall, kLarge };
+enum Tiles { kRows, kTiny, kSmall, kWide, kLarge };
 
 struct Choice {
     Tiles tiles;
@@ -122,6 +122,7 @@ Choice choose(int64_t m, int64_t n, int64_t k)
     auto tiles = [&](int64_t tm, int64_t tn) { return ((m + tm - 1) / tm) * ((n + tn - 1) / tn); };
     if (m <= 64) return {kRows, 1, (int)steps};
     if (std::min(m, n) > 128 && tiles(256, 256) >= 192) return {kLarge, 1, (int)steps};
+    if (std::min(m, n) > 128 && tiles(256, 128) >= 192) return {kWide, 1, (int)steps};
     if (tiles(128, 128) >= 200) return {kSmall, 1, (int)steps};
     const int64_t parts = steps < 32 ? 1 : std::max<int64_t>(std::min<int64_t>(2 * kCus / tiles(64, 64), steps / 8), 1);
     const int64_t per = (steps + parts - 1) / parts;
@@ -131,7 +132,7 @@ Choice choose(int64_t m, int64_t n, int64_t k)
 template <int KIND, bool BF16, bool ADD, bool PAST, int WM, int WN, int TM, int TN, int STAGES, int OCC>
 void launch_tiles(const Q8ProductArgs &p, const Choice &c, hipStream_t st)
 {
-    constexpr int kM = WM * TM * 32, kN = WN * TN * 32;
+    constexpr int kM = WM * TM * 16, kN = WN * TN * 16;
     Shape z;
     z.steps = (int)((p.k + 127) / 128);
     z.tiles_m = (int)((p.m + kM - 1) / kM);
@@ -182,7 +183,7 @@ void launch_q8_product(const Q8ProductArgs &a, bool bf16, hipStream_t st)
             if (c.parts > 1) {
                 Q8ProductArgs p = a;
                 p.alpha = 1.0f;                 // (alpha and beta are for the launch that adds the parts)
-                launch_tiles<K, false, false, false, 2, 2, 1, 1, 4, 2>(p, c, st);
+                launch_tiles<K, false, false, false, 2, 2, 2, 2, 4, 2>(p, c, st);
             }
             by_bool(a.beta != 0.0f, [&](auto add) {
                 constexpr bool ADD = decltype(add)::value;
@@ -192,11 +193,13 @@ void launch_q8_product(const Q8ProductArgs &a, bool bf16, hipStream_t st)
                     const uint32_t octets = (uint32_t)((a.n + 7) / 8);
                     hipLaunchKernelGGL((k_q8_join<B, ADD>), dim3((unsigned)(((uint64_t)a.m * octets + 255) / 256)), dim3(256), 0, st, a, c.parts, octets);
                 } else if (c.tiles == kTiny) {
-                    launch_tiles<K, B, ADD, false, 2, 2, 1, 1, 4, 2>(a, c, st);
+                    launch_tiles<K, B, ADD, false, 2, 2, 2, 2, 4, 2>(a, c, st);
                 } else if (c.tiles == kSmall) {
-                    launch_tiles<K, B, ADD, false, 2, 2, 2, 2, 2, 2>(a, c, st);
+                    launch_tiles<K, B, ADD, false, 2, 2, 4, 4, 2, 2>(a, c, st);
+                } else if (c.tiles == kWide) {
+                    launch_tiles<K, B, ADD, false, 4, 2, 4, 4, 3, 2>(a, c, st);
                 } else {
-                    launch_tiles<K, B, ADD, false, 2, 4, 4, 2, 2, 2>(a, c, st);
+                    launch_tiles<K, B, ADD, false, 2, 4, 8, 4, 2, 2>(a, c, st);
                 }
             });
         });

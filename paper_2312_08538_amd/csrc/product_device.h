@@ -1,5 +1,5 @@
 // Products A B^T whose operands lie in steps of 128 bytes along the long axis, whatever their elements are: 128 of 8 bits, 64 of 16, 32
-// of 32.  A step of 32 rows is the same fragment in every case, 64 bytes a lane in two halves; only the instructions that
+// of 32.  A step of sixteen rows is the same fragment in every case, 32 bytes a lane; only the instructions that
 // multiply it differ.  Also what such kernels share with others: loads to LDS, waits, loops that are unrolled with constants.
 #pragma once
 #include <type_traits>
@@ -33,6 +33,18 @@ __device__ __forceinline__ void to_lds(const uint8_t *src, uint8_t *dst)
     auto *to = (__attribute__((address_space(3))) void *)dst;
     if constexpr (BYTES == 16) __builtin_amdgcn_global_load_lds(from, to, 16, 0, 0);
     else __builtin_amdgcn_global_load_lds(from, to, 4, 0, 0);
+}
+
+// 1024 bytes (256) from `src`, which is the wave's, likewise.  As a load from a buffer, whose base is in scalar registers: a lane's own address would take two
+// vector registers for each place that a kernel loads from.
+template <int BYTES>
+__device__ __forceinline__ void wave_to_lds(const uint8_t *src, uint8_t *dst)
+{
+    auto *to = (__attribute__((address_space(3))) void *)dst;
+    const auto from = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t *>(src), 0, 64 * BYTES, 0x00020000);
+    const int lane = threadIdx.x & 63;
+    if constexpr (BYTES == 16) __builtin_amdgcn_raw_ptr_buffer_load_lds(from, to, 16, lane * 16, 0, 0, 0);
+    else __builtin_amdgcn_raw_ptr_buffer_load_lds(from, to, 4, lane * 4, 0, 0, 0);
 }
 
 // all but the last N loads of this wave have arrived, and all its reads from LDS
@@ -107,51 +119,69 @@ __device__ __forceinline__ Place place_of(const Shape &z, int block)
     return {8 * band + in_band % high, in_band / high, item / tiles};
 }
 
-// WM x WN waves of TM x TN tiles of 32 x 32, STAGES steps in LDS.  A step is two halves of 64 bytes: while one is multiplied the next is read
-// from LDS, and behind the first half's products, when a wave has all of a step in registers, the step STAGES on is fetched into its
-// place.  So there is one barrier a step, and what it waits for was asked for a step before.
+// WM x WN waves of TM x TN tiles of 16 x 16, STAGES steps in LDS.  A fragment is sixteen rows of a step, 32 bytes a lane.  A wave holds B's fragments and four of A's:
+// as soon as one of these is multiplied, the one four on is read into its place; B's next ones go to a set of their own, or follow where the step's
+// last products have been.  When the last of a step is on its way, what is left of it in LDS is nobody's: the step STAGES on is fetched there, and the next
+// one, which was fetched a step before, is read from then on.  So there is one barrier a step, and what it waits for was asked for a step before.
 template <int KIND, bool BY_ROWS, int WM, int WN, int TM, int TN, int STAGES>
 struct Tile {
     static constexpr bool kWide = KIND == Kind::WIDE_E4M3 || KIND == Kind::WIDE_E5M2, kScaled = KIND == Kind::E4M3 || KIND == Kind::E5M2 || kWide;
-    static constexpr int kM = WM * TM * 32, kN = WN * TN * 32, kWaves = WM * WN, kThreads = 64 * kWaves;
+    static constexpr int kM = WM * TM * 16, kN = WN * TN * 16, kWaves = WM * WN, kThreads = 64 * kWaves;
     static constexpr int kCodes = (kM + kN) * 128, kStage = kCodes + (kScaled ? 512 : 0), kBytes = STAGES * kStage;
     static constexpr int kUnits = (kM + kN) / 8 / kWaves, kLoads = kUnits + (kScaled ? 1 : 0);
-    static_assert((kM + kN) / 8 % kWaves == 0 && kM <= 256 && kN <= 256 && STAGES >= 2, "");
+    static constexpr int kRing = TM < 4 ? TM : 4;                   // fragments of A that a wave holds
+    static constexpr bool kTwice = TM <= 4;                         // two sets of B's, this step's and the next one's: larger tiles have no registers for them
+    static_assert((kM + kN) / 8 % kWaves == 0 && kM <= 256 && kN <= 256 && STAGES >= 2 && TM % 2 == 0 && TM % kRing == 0, "");
     static_assert(!kScaled || (!BY_ROWS && kWaves % 2 == 0), "");
     static_assert((STAGES - 1) * kLoads < 64, "the counter of loads");
     // a wave's 32 rows of an output on their way through LDS
-    static constexpr int kPitch = TN * 32 + 4;
+    static constexpr int kPitch = TN * 16 + 4;
     static_assert(kWaves * 32 * kPitch * 4 <= kBytes, "");
 
-    struct Half {
-        v8i a[TM], b[TN];
-        int ea[kScaled ? TM : 1], eb[kScaled ? TN : 1];
+    struct Fragment {
+        v8i v;
+        int scale;
     };
 
-    typedef f32x16 Sums[TN][TM];
+    typedef f32x4 Sums[TN][TM];
 
     static __device__ __forceinline__ int wave() { return __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); }
     static __device__ __forceinline__ int wave_m() { return wave() % WM; }
     static __device__ __forceinline__ int wave_n() { return wave() / WM; }
 
-    // The first operand of the instructions is B's rows: then a lane holds, of one row of the product (lane % 32), columns 8 q + 4 (lane / 32) + e
-    // of 32 in registers 4 q + e.
-    static __device__ __forceinline__ void multiply(const v8i &b, const v8i &a, f32x16 &c, int eb, int ea)
+    // A row of tiles, or columns FROM to TO of it: acc[j][i] += b[j] a.  The instructions' first operand is B's rows: then a lane holds, of one row of the product (lane % 16), columns
+    // 4 (lane / 16) .. + 3 of 16.
+    static constexpr int kEach = kWide ? 4 : kScaled ? 1 : KIND == Kind::BF16 ? 2 : 8;
+    template <int FROM = 0, int TO = TN>
+    static __device__ __forceinline__ void multiply(const Fragment (&b)[TN], const Fragment &a, Sums &acc, int i)
     {
-        if constexpr (kScaled) {
-            c = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(b, a, c, 0, KIND == Kind::E5M2 ? 1 : 0, 0, eb, 0, ea);
+        if constexpr (kWide) {
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const bf16x8 y = widen_octet<KIND == Kind::WIDE_E5M2>(a.v[2 * q], a.v[2 * q + 1], a.scale);
+#pragma unroll
+                for (int j = FROM; j < TO; ++j)
+                    acc[j][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(widen_octet<false>(b[j].v[2 * q], b[j].v[2 * q + 1], b[j].scale), y, acc[j][i], 0, 0, 0);
+            }
+        } else if constexpr (kScaled) {
+#pragma unroll
+            for (int j = FROM; j < TO; ++j)
+                acc[j][i] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(b[j].v, a.v, acc[j][i], 0, KIND == Kind::E5M2 ? 1 : 0, 0, b[j].scale, 0, a.scale);
         } else if constexpr (KIND == Kind::BF16) {
 #pragma unroll
             for (int q = 0; q < 2; ++q) {
-                const v4i x = {b[4 * q], b[4 * q + 1], b[4 * q + 2], b[4 * q + 3]}, y = {a[4 * q], a[4 * q + 1], a[4 * q + 2], a[4 * q + 3]};
-                c = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, x), __builtin_bit_cast(bf16x8, y), c, 0, 0, 0);
+                auto half = [&](const Fragment &f) { return __builtin_bit_cast(bf16x8, q ? __builtin_shufflevector(f.v, f.v, 4, 5, 6, 7) : __builtin_shufflevector(f.v, f.v, 0, 1, 2, 3)); };
+#pragma unroll
+                for (int j = FROM; j < TO; ++j) acc[j][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(half(b[j]), half(a), acc[j][i], 0, 0, 0);
             }
         } else {
 #pragma unroll
-            for (int q = 0; q < 8; ++q) c = __builtin_amdgcn_mfma_f32_32x32x2f32(__int_as_float(b[q]), __int_as_float(a[q]), c, 0, 0, 0);
+            for (int q = 0; q < 8; ++q)
+#pragma unroll
+                for (int j = FROM; j < TO; ++j)
+                    acc[j][i] = __builtin_amdgcn_mfma_f32_16x16x4f32(__int_as_float(b[j].v[q]), __int_as_float(a.v[q]), acc[j][i], 0, 0, 0);
         }
     }
-    static constexpr int kEach = kWide ? 4 : kScaled ? 1 : KIND == Kind::BF16 ? 2 : 8;          // instructions of a multiply
 
     // acc <- rows m0 .. of A times rows n0 .. of B, over `steps` steps from `first` on.  Rows beyond an operand's last are some other of its
     // rows (what comes of them is not used).
@@ -189,121 +219,117 @@ struct Tile {
                 scale_src = of.scales + (int64_t)first * of.rows + min((w & 1 ? n0 : m0) + lane * 4, of.rows - 4);
             }
         }
-        auto fetch = [&](int s, int slot) {
+        // turn T of TURNS: a share of a step's loads
+        auto fetch = [&](int s, int slot, auto turn, auto turns) {
+            constexpr int kFrom = decltype(turn)::value * kUnits / decltype(turns)::value, kTo = (decltype(turn)::value + 1) * kUnits / decltype(turns)::value;
             uint8_t *to = lds + slot * kStage;
             if constexpr (BY_ROWS) {
-                if (first + s + 1 == z.steps && z.last < 128) {         // what is behind a row's end is zeros
-                    const bool there = ((lane & 7) ^ (lane >> 3)) * 16 < z.last;
+                // what is behind a row's end is zeros
+                const bool beyond = ((lane & 7) ^ (lane >> 3)) * 16 >= (first + s + 1 == z.steps ? z.last : 128);
 #pragma unroll
-                    for (int i = 0; i < kUnits; ++i)
-                        to_lds<16>(there ? src[i] + (int64_t)s * 128 + off[i] : reinterpret_cast<const uint8_t *>(kZeros), to + (w + i * kWaves) * 1024);
-                    return;
-                }
-#pragma unroll
-                for (int i = 0; i < kUnits; ++i) to_lds<16>(src[i] + (int64_t)s * 128 + off[i], to + (w + i * kWaves) * 1024);
+                for (int i = kFrom; i < kTo; ++i)
+                    to_lds<16>(beyond ? reinterpret_cast<const uint8_t *>(kZeros) : src[i] + (int64_t)s * 128 + off[i], to + (w + i * kWaves) * 1024);
             } else {
 #pragma unroll
-                for (int i = 0; i < kUnits; ++i) to_lds<16>(src[i] + (int64_t)s * 2048 + lane * 16, to + (w + i * kWaves) * 1024);
-                if constexpr (kScaled) to_lds<4>(scale_src + (int64_t)s * scale_step, to + kCodes + (w & 1) * 256);
+                for (int i = kFrom; i < kTo; ++i) wave_to_lds<16>(src[i] + (int64_t)s * 2048, to + (w + i * kWaves) * 1024);
+                if constexpr (kScaled && decltype(turn)::value == 0) to_lds<4>(scale_src + (int64_t)s * scale_step, to + kCodes + (w & 1) * 256);
             }
         };
-        // Where this lane's fragments begin: row lane % 32; of a half's four pieces of 16 bytes two, by lane / 32.  By rows a row's pieces lie exchanged, by the
-        // row, so that neither way of reading has a bank conflict.
-        const int r = lane & 31, g = lane >> 5;
-        int at[2][2];
-#pragma unroll
-        for (int h = 0; h < 2; ++h)
-#pragma unroll
-            for (int q = 0; q < 2; ++q) {
-                const int chunk = 4 * h + 2 * g + q;
-                at[h][q] = BY_ROWS ? (r >> 3) * 1024 + (r & 7) * 128 + (chunk ^ (r & 7)) * 16 : (r >> 4) * 2048 + chunk * 256 + (r & 15) * 16;
-            }
-        const int la = wave_m() * TM * 4096, lb = kM * 128 + wave_n() * TN * 4096;
-        auto read = [&](int slot, auto half, Half &f) {
-            constexpr int H = decltype(half)::value;
+        // Where this lane's part of a fragment is: of row lane % 16 two pieces of 16 bytes.  Packed, the first half of the row's pieces are before the second, lane by lane; by
+        // rows a row's pieces lie exchanged, by the row.  Neither way of reading has a bank conflict.  (8 bits: an instruction takes 32 bytes
+        // of a lane, whichever they are, if they are the same of both operands.)
+        const int r = lane & 15, g = lane >> 4;
+        const int at0 = BY_ROWS ? (r >> 3) * 1024 + (r & 7) * 128 + (g ^ (r & 7)) * 16 : lane * 16;
+        const int at1 = BY_ROWS ? (r >> 3) * 1024 + (r & 7) * 128 + ((g + 4) ^ (r & 7)) * 16 : lane * 16 + 1024;
+        const int la = wave_m() * TM * 2048, lb = kM * 128 + wave_n() * TN * 2048;
+        auto read = [&](int slot, int of, int scale, Fragment &f) {
             const uint8_t *from = lds + slot * kStage;
-            auto one = [&](const uint8_t *p) {
-                const v4i lo = *reinterpret_cast<const v4i *>(p + at[H][0]), hi = *reinterpret_cast<const v4i *>(p + at[H][1]);
-                return v8i{lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
-            };
-            if constexpr (kScaled) {
-#pragma unroll
-                for (int i = 0; i < TM; ++i) f.ea[i] = from[kCodes + (wave_m() * TM + i) * 32 + r];
-#pragma unroll
-                for (int j = 0; j < TN; ++j) f.eb[j] = from[kCodes + 256 + (wave_n() * TN + j) * 32 + r];
-            }
-#pragma unroll
-            for (int j = 0; j < TN; ++j) f.b[j] = one(from + lb + j * 4096);
-#pragma unroll
-            for (int i = 0; i < TM; ++i) f.a[i] = one(from + la + i * 4096);
+            const v4i lo = *reinterpret_cast<const v4i *>(from + of + at0), hi = *reinterpret_cast<const v4i *>(from + of + at1);
+            f.v = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+            if constexpr (kScaled) f.scale = from[kCodes + scale + r];
         };
-        constexpr int kReads = (TM + TN) * (kScaled ? 3 : 2), kProducts = TM * TN * kEach;
-        auto products = [&](const Half &f) {
-            if constexpr (kWide) {
-                unroll<4>([&](auto q) {
-                    constexpr int Q = decltype(q)::value;
-                    bf16x8 x[TN], y[TM];
-#pragma unroll
-                    for (int j = 0; j < TN; ++j) x[j] = widen_octet<false>(f.b[j][2 * Q], f.b[j][2 * Q + 1], f.eb[j]);
-#pragma unroll
-                    for (int i = 0; i < TM; ++i) y[i] = widen_octet<KIND == Kind::WIDE_E5M2>(f.a[i][2 * Q], f.a[i][2 * Q + 1], f.ea[i]);
-#pragma unroll
-                    for (int i = 0; i < TM; ++i)
-#pragma unroll
-                        for (int j = 0; j < TN; ++j) acc[j][i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x[j], y[i], acc[j][i], 0, 0, 0);
-                });
-            } else {
-                unroll<TM>([&](auto i) {
-                    unroll<TN>([&](auto j) {
-                        constexpr int I = decltype(i)::value, J = decltype(j)::value;
-                        multiply(f.b[J], f.a[I], acc[J][I], f.eb[kScaled ? J : 0], f.ea[kScaled ? I : 0]);
-                    });
-                });
-            }
-            // a few reads behind every few products: reads wait for LDS in the order of their issue, and products behind them would wait with them
-            constexpr int kTurns = kProducts < 8 ? kProducts : 8;
-            unroll<kTurns>([&](auto t) {
-                constexpr int T = decltype(t)::value;
-                __builtin_amdgcn_sched_group_barrier(0x008, (T + 1) * kProducts / kTurns - T * kProducts / kTurns, 0);
-                __builtin_amdgcn_sched_group_barrier(0x100, (T + 1) * kReads / kTurns - T * kReads / kTurns, 0);
-            });
-            __builtin_amdgcn_sched_barrier(0);
-        };
+        auto read_a = [&](int slot, int i, Fragment &f) { read(slot, la + i * 2048, (wave_m() * TM + i) * 16, f); };
+        auto read_b = [&](int slot, int j, Fragment &f) { read(slot, lb + j * 2048, 256 + (wave_n() * TN + j) * 16, f); };
 #pragma unroll
         for (int j = 0; j < TN; ++j)
 #pragma unroll
-            for (int i = 0; i < TM; ++i) acc[j][i] = f32x16{};
-        const std::integral_constant<int, 0> low;
-        const std::integral_constant<int, 1> high;
+            for (int i = 0; i < TM; ++i) acc[j][i] = f32x4{};
         int slot = 0;
-        Half even, odd;
-        for (int s = 0; s < min(steps, STAGES); ++s) fetch(s, s);
+        if (steps <= 0) return;
+        for (int s = 0; s < min(steps, STAGES); ++s) fetch(s, s, std::integral_constant<int, 0>{}, std::integral_constant<int, 1>{});
         if (steps >= STAGES) wait_loads<(STAGES - 1) * kLoads>();
         else wait_loads<0>();
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
-        read(0, low, even);
+        Fragment ring[kRing], even[TN], odd[kTwice ? TN : 1];
+#pragma unroll
+        for (int j = 0; j < TN; ++j) read_b(0, j, even[j]);
+#pragma unroll
+        for (int i = 0; i < kRing; ++i) read_a(0, i, ring[i]);
         __builtin_amdgcn_sched_barrier(0);
-        auto step = [&](int s, auto steady) {
+        // (a step is a block without branches: over one the compiler would move products, away from the reads that they are to hide, and hold both)
+        auto step = [&](int s, auto more, Fragment (&now)[TN], auto &next) {
+            constexpr bool kMore = decltype(more)::value;                               // there is a step to fetch
             const int after = slot + 1 == STAGES ? 0 : slot + 1;
-            read(slot, high, odd);
-            products(even);
-            wait_loads<decltype(steady)::value ? (STAGES - 2) * kLoads : 0>();
-            __builtin_amdgcn_s_barrier();
-            asm volatile("" ::: "memory");
-            if (decltype(steady)::value || s + STAGES < steps) fetch(s + STAGES, slot);
-            __builtin_amdgcn_sched_barrier(0);
-            read(after, low, even);             // (behind the last step: what is left there, for nothing)
-            products(odd);
+            unroll<TM>([&](auto index) {
+                constexpr int I = decltype(index)::value, kTurn = TM - kRing;           // from here on the next step's fragments are read
+                if constexpr (!kTwice && I == TM - 1) {
+                    constexpr int kHalf = TN / 2;
+                    unroll<2>([&](auto half) {
+                        constexpr int J = decltype(half)::value * kHalf;
+                        multiply<J, J + kHalf>(now, ring[I % kRing], acc, I);
+                        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                        for (int j = J; j < J + kHalf; ++j) read_b(after, j, now[j]);
+                    });
+                } else {
+                    multiply(now, ring[I % kRing], acc, I);
+                }
+                __builtin_amdgcn_sched_barrier(0);
+                if constexpr (I < kTurn) {
+                    read_a(slot, I + kRing, ring[I % kRing]);
+                } else {
+                    if constexpr (I == kTurn) {
+                        wait_loads<kMore ? (STAGES - 2) * kLoads : 0>();
+                        __builtin_amdgcn_s_barrier();
+                        asm volatile("" ::: "memory");
+                    }
+                    // (behind the last step: what is left there, for nothing)
+                    if constexpr (kTwice && I < kTurn + 2) {
+#pragma unroll
+                        for (int j = 0; j < TN / 2; ++j) read_b(after, (I - kTurn) * (TN / 2) + j, next[(I - kTurn) * (TN / 2) + j]);
+                    }
+                    read_a(after, I - kTurn, ring[I % kRing]);
+                    // a few loads at a time: as many as there are, one behind the other, would keep the waves from their products
+                    if constexpr (kMore) fetch(s + STAGES, slot, std::integral_constant<int, I - kTurn>{}, std::integral_constant<int, kRing>{});
+                }
+                __builtin_amdgcn_sched_barrier(0);
+            });
             slot = after;
         };
         int s = 0;
-        for (; s + STAGES < steps; ++s) step(s, std::true_type{});
-        for (; s < steps; ++s) step(s, std::false_type{});
+        if constexpr (kTwice) {
+            // (steps in twos, so that fragments need not be moved)
+            for (; s + 1 + STAGES < steps; s += 2) {
+                step(s, std::true_type{}, even, odd);
+                step(s + 1, std::true_type{}, odd, even);
+            }
+            auto alone = [&](auto more) {
+                step(s, more, even, odd);
+#pragma unroll
+                for (int j = 0; j < TN; ++j) even[j] = odd[j];
+                ++s;
+            };
+            if (s + STAGES < steps) alone(std::true_type{});
+            while (s < steps) alone(std::false_type{});
+        } else {
+            for (; s + STAGES < steps; ++s) step(s, std::true_type{}, even, odd);
+            for (; s < steps; ++s) step(s, std::false_type{}, even, odd);
+        }
     }
 
     // The product by eight neighbours of a row at a time, by way of LDS, where each wave turns 32 rows of its own: f(row, col, v) of the tile's row and
-    // column and eight sums; a wave's lanes hold eight rows of TN * 32 columns (TN = 2; else sixteen of 32).
+    // column and eight sums; a wave's lanes hold eight rows of TN * 16 columns (TN = 4; else sixteen of 32).
     template <typename F>
     static __device__ __forceinline__ void octets(const Sums &acc, uint8_t *lds, F &&f)
     {
@@ -312,24 +338,29 @@ struct Tile {
         wait_loads<0>();
         __syncthreads();
 #pragma unroll
-        for (int i = 0; i < TM; ++i) {
-#pragma unroll
-            for (int j = 0; j < TN; ++j)
-#pragma unroll
-                for (int q = 0; q < 4; ++q)
-                    *reinterpret_cast<f32x4 *>(mine + (lane & 31) * kPitch + j * 32 + 8 * q + 4 * (lane >> 5)) =
-                        f32x4{acc[j][i][4 * q], acc[j][i][4 * q + 1], acc[j][i][4 * q + 2], acc[j][i][4 * q + 3]};
-            __builtin_amdgcn_wave_barrier();
-            constexpr int kAcross = TN * 4, kHigh = 64 / kAcross;
+        for (int i = 0; i < TM; i += 2) {
+            turn(acc, i, mine);
+            constexpr int kAcross = TN * 2, kHigh = 64 / kAcross;
 #pragma unroll
             for (int t = 0; t < 32 / kHigh; ++t) {
                 const int r = t * kHigh + lane / kAcross, c = lane % kAcross * 8;
                 const f32x4 x = *reinterpret_cast<const f32x4 *>(mine + r * kPitch + c), y = *reinterpret_cast<const f32x4 *>(mine + r * kPitch + c + 4);
                 float v[8] = {x[0], x[1], x[2], x[3], y[0], y[1], y[2], y[3]};
-                f((wave_m() * TM + i) * 32 + r, wave_n() * TN * 32 + c, v);
+                f((wave_m() * TM + i) * 16 + r, wave_n() * TN * 16 + c, v);
             }
             __builtin_amdgcn_wave_barrier();
         }
+    }
+
+    // 32 rows (tiles i and i + 1) of a wave to its part of LDS
+    static __device__ __forceinline__ void turn(const Sums &acc, int i, float *mine)
+    {
+        const int lane = threadIdx.x & 63;
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int j = 0; j < TN; ++j) *reinterpret_cast<f32x4 *>(mine + (h * 16 + (lane & 15)) * kPitch + j * 16 + 4 * (lane >> 4)) = acc[j][i + h];
+        __builtin_amdgcn_wave_barrier();
     }
 };
 
