@@ -370,8 +370,10 @@ constexpr std::integral_constant<int, 8> eight;
 
 enum Tiles { kTiny, kSmall, kWide, kLarge };
 
-Tiles tiles_for(int64_t m, int64_t n)
+// fp32: the matrix instructions take sixteen times as long as those of 16 bits, so that the smallest tiles' reads hide behind them, too; and there are many, for even turns
+Tiles tiles_for(int64_t m, int64_t n, bool bf16)
 {
+    if (!bf16) return kTiny;
     auto tiles = [&](int64_t tm, int64_t tn) { return ((m + tm - 1) / tm) * ((n + tn - 1) / tn); };
     if (std::min(m, n) > 128 && tiles(256, 256) >= 192) return kLarge;
     if (std::min(m, n) > 128 && tiles(256, 128) >= 192) return kWide;
@@ -385,12 +387,12 @@ struct Cut {
 };
 
 // of a product of `steps` along its long axis
-Cut cut_of(int64_t m, int64_t n, int64_t steps)
+Cut cut_of(int64_t m, int64_t n, int64_t steps, bool bf16)
 {
-    const Tiles t = tiles_for(m, n);
+    const Tiles t = tiles_for(m, n, bf16);
     if (t != kTiny) return {t, 1, (int)steps};
     const int64_t tiles = std::max<int64_t>(((m + 63) / 64) * ((n + 63) / 64), 1);
-    const int64_t parts = std::max<int64_t>(std::min<int64_t>(2 * kCus / tiles, steps / 8), 1), per = std::max<int64_t>((steps + parts - 1) / parts, 1);
+    const int64_t parts = std::max<int64_t>(std::min<int64_t>((bf16 ? 2 : 4) * kCus / tiles, steps / 8), 1), per = std::max<int64_t>((steps + parts - 1) / parts, 1);
     return {t, (int)std::max<int64_t>((steps + per - 1) / per, 1), (int)per};
 }
 
@@ -429,7 +431,7 @@ Layout layout_of(int64_t tokens, int64_t vocab, int64_t width, bool bf16)
     l.grown = take(l.piece < vocab ? (size_t)tokens * width * sizeof(float) : 0);
     size_t most = 0;
     for (const int64_t n : {std::min(l.piece, vocab), vocab % l.piece}) {
-        const Cut x = cut_of(tokens, width, up(n, 64) * l.esz / 128), w = cut_of(n, width, t64 * l.esz / 128);
+        const Cut x = cut_of(tokens, width, up(n, 64) * l.esz / 128, bf16), w = cut_of(n, width, t64 * l.esz / 128, bf16);
         most = std::max(most, x.parts > 1 ? (size_t)x.parts * tokens * width : 0);
         most = std::max(most, w.parts > 1 ? (size_t)w.parts * n * width : 0);
     }
@@ -517,8 +519,9 @@ void forward(const LossArgs &a, hipStream_t st)
                                    grid_of(z.items), dim3(64 * WM * WN), 0, st, p, x, w, z);
                 tiles += z.tiles_n;
             };
-            const Tiles t = tiles_for(a.tokens, n);
-            if (a.tokens <= 32) go(one, two, two, two, four, two);
+            const Tiles t = tiles_for(a.tokens, n, BF16);
+            if constexpr (!BF16) go(two, two, two, two, two, four);
+            else if (a.tokens <= 32) go(one, two, two, two, four, two);
             else if (t == kTiny) go(two, two, two, two, four, two);
             else if (t == kSmall) go(two, two, four, four, two, two);
             else if (t == kWide) go(four, two, four, four, three, two);
@@ -534,7 +537,7 @@ template <int KIND, bool OUT>
 void product(SumArgs p, const uint8_t *a, const uint8_t *b, int64_t depth, float *partials, hipStream_t st)
 {
     constexpr int kStep = is_bf16<KIND>() ? 64 : 32;
-    const Cut c = cut_of(p.m, p.n, depth / kStep);
+    const Cut c = cut_of(p.m, p.n, depth / kStep, is_bf16<KIND>());
     p.partials = c.parts > 1 ? partials : nullptr;
     auto go = [&](auto wm, auto wn, auto tm, auto tn, auto stages, auto occ) {
         constexpr int WM = decltype(wm)::value, WN = decltype(wn)::value, TM = decltype(tm)::value, TN = decltype(tn)::value;
@@ -546,7 +549,8 @@ void product(SumArgs p, const uint8_t *a, const uint8_t *b, int64_t depth, float
         z.items = z.tiles_m * z.tiles_n * c.parts;
         hipLaunchKernelGGL((k_loss_product<KIND, OUT, WM, WN, TM, TN, decltype(stages)::value, decltype(occ)::value>), grid_of(z.items), dim3(64 * WM * WN), 0, st, p, packed_side(a, p.m), packed_side(b, p.n), z);
     };
-    if (c.tiles == kTiny) go(two, two, two, two, four, two);
+    if constexpr (KIND == Kind::F32) go(two, two, two, two, two, four);
+    else if (c.tiles == kTiny) go(two, two, two, two, four, two);
     else if (c.tiles == kSmall) go(two, two, four, four, two, two);
     else if (c.tiles == kWide) go(four, two, four, four, three, two);
     else go(two, four, eight, four, two, two);
@@ -595,8 +599,9 @@ void backward(const LossArgs &a, hipStream_t st)
                 hipLaunchKernelGGL((k_loss_gradient<KIND, decltype(by_rows)::value, WM, WN, TM, TN, decltype(stages)::value, decltype(occ)::value>),
                                    grid_of(z.items), dim3(64 * WM * WN), 0, st, p, x, w, z);
             };
-            const Tiles t = tiles_for(a.tokens, n);
-            if (t == kTiny) go(two, two, two, two, four, two);
+            const Tiles t = tiles_for(a.tokens, n, BF16);
+            if constexpr (!BF16) go(two, two, two, two, two, four);
+            else if (t == kTiny) go(two, two, two, two, four, two);
             else if (t == kSmall) go(two, two, four, four, two, two);
             else if (t == kWide) go(four, two, four, four, three, two);
             else go(two, four, eight, four, two, two);
