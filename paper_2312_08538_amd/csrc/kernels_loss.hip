@@ -370,15 +370,32 @@ constexpr std::integral_constant<int, 8> eight;
 
 enum Tiles { kTiny, kSmall, kWide, kLarge };
 
-// fp32: the matrix instructions take sixteen times as long as those of 16 bits, so that the smallest tiles' reads hide behind them, too; and there are many, for even turns
 Tiles tiles_for(int64_t m, int64_t n, bool bf16)
 {
-    if (!bf16) return kTiny;
     auto tiles = [&](int64_t tm, int64_t tn) { return ((m + tm - 1) / tm) * ((n + tn - 1) / tn); };
+    // fp32: the matrix instructions take sixteen times as long as those of 16 bits, so that the smallest tiles' reads hide behind them, too, and many tiles make even turns:
+    // us of 1024 x 5056 x 512 alone 48 (three steps in LDS, three workgroups a CU; two and four 55), of 128 x 128 69; 4096 x 4096 x 2048, 1024 of these, 511 and 466 (147 TFLOP/s;
+    // the instructions alone 141 to 157, by the clock)
+    if (!bf16) return tiles(128, 128) >= 4 * kCus ? kSmall : kTiny;
     if (std::min(m, n) > 128 && tiles(256, 256) >= 192) return kLarge;
     if (std::min(m, n) > 128 && tiles(256, 128) >= 192) return kWide;
     if (m > 64 && tiles(128, 128) >= 200) return kSmall;
     return kTiny;
+}
+
+// waves, tiles of a wave, steps in LDS, waves a SIMD
+template <bool BF16, typename F>
+void by_tiles(Tiles t, F &&go)
+{
+    if (t == kSmall) {
+        go(two, two, four, four, two, two);
+    } else if constexpr (!BF16) {
+        go(two, two, two, two, three, three);
+    } else {
+        if (t == kTiny) go(two, two, two, two, four, two);
+        else if (t == kWide) go(four, two, four, four, three, two);
+        else go(two, four, eight, four, two, two);
+    }
 }
 
 struct Cut {
@@ -392,7 +409,7 @@ Cut cut_of(int64_t m, int64_t n, int64_t steps, bool bf16)
     const Tiles t = tiles_for(m, n, bf16);
     if (t != kTiny) return {t, 1, (int)steps};
     const int64_t tiles = std::max<int64_t>(((m + 63) / 64) * ((n + 63) / 64), 1);
-    const int64_t parts = std::max<int64_t>(std::min<int64_t>((bf16 ? 2 : 4) * kCus / tiles, steps / 8), 1), per = std::max<int64_t>((steps + parts - 1) / parts, 1);
+    const int64_t parts = std::max<int64_t>(std::min<int64_t>((bf16 ? 2 : 3) * kCus / tiles, steps / 8), 1), per = std::max<int64_t>((steps + parts - 1) / parts, 1);
     return {t, (int)std::max<int64_t>((steps + per - 1) / per, 1), (int)per};
 }
 
@@ -520,12 +537,8 @@ void forward(const LossArgs &a, hipStream_t st)
                 tiles += z.tiles_n;
             };
             const Tiles t = tiles_for(a.tokens, n, BF16);
-            if constexpr (!BF16) go(two, two, two, two, two, four);
-            else if (a.tokens <= 32) go(one, two, two, two, four, two);
-            else if (t == kTiny) go(two, two, two, two, four, two);
-            else if (t == kSmall) go(two, two, four, four, two, two);
-            else if (t == kWide) go(four, two, four, four, three, two);
-            else go(two, four, eight, four, two, two);
+            if (a.tokens <= 32) go(one, two, two, two, four, two);
+            else by_tiles<BF16>(t, go);
         });
     }
     hipLaunchKernelGGL(k_loss_join, grid_of((a.tokens + 15) / 16), dim3(1024), 0, st, stats, reinterpret_cast<float *>(a.workspace + l.hit), a.targets,
@@ -549,11 +562,7 @@ void product(SumArgs p, const uint8_t *a, const uint8_t *b, int64_t depth, float
         z.items = z.tiles_m * z.tiles_n * c.parts;
         hipLaunchKernelGGL((k_loss_product<KIND, OUT, WM, WN, TM, TN, decltype(stages)::value, decltype(occ)::value>), grid_of(z.items), dim3(64 * WM * WN), 0, st, p, packed_side(a, p.m), packed_side(b, p.n), z);
     };
-    if constexpr (KIND == Kind::F32) go(two, two, two, two, two, four);
-    else if (c.tiles == kTiny) go(two, two, two, two, four, two);
-    else if (c.tiles == kSmall) go(two, two, four, four, two, two);
-    else if (c.tiles == kWide) go(four, two, four, four, three, two);
-    else go(two, four, eight, four, two, two);
+    by_tiles<is_bf16<KIND>()>(c.tiles, go);
     if (c.parts > 1) {
         const uint32_t octets = (uint32_t)((p.n + 7) / 8);
         hipLaunchKernelGGL((k_loss_parts<OUT>), dim3((unsigned)(((uint64_t)p.m * octets + 255) / 256)), dim3(256), 0, st, p, c.parts, octets);
@@ -600,11 +609,7 @@ void backward(const LossArgs &a, hipStream_t st)
                                    grid_of(z.items), dim3(64 * WM * WN), 0, st, p, x, w, z);
             };
             const Tiles t = tiles_for(a.tokens, n, BF16);
-            if constexpr (!BF16) go(two, two, two, two, two, four);
-            else if (t == kTiny) go(two, two, two, two, four, two);
-            else if (t == kSmall) go(two, two, four, four, two, two);
-            else if (t == kWide) go(four, two, four, four, three, two);
-            else go(two, four, eight, four, two, two);
+            by_tiles<BF16>(t, go);
         });
         if (a.dx.data) {
             turn<BF16>(rows_from(a.w, first, l.esz), n, a.width, a.workspace + l.w_t, st);
