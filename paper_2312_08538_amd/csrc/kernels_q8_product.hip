@@ -23,6 +23,10 @@ __global__ __launch_bounds__(64 * WM * WN, OCC) void k_q8_product(Q8ProductArgs 
         p.c.data = p.partials + (int64_t)at.part * p.m * p.n;
         p.c.pitch = p.n;
     }
+    if constexpr (BF16 && !ADD) {
+        T::template store_bf16<PAST>(acc, lds, p.c, p.m, p.n, (int64_t)at.m * T::kM, (int64_t)at.n * T::kN, p.alpha);
+        return;
+    }
     T::octets(acc, lds, [&](int r, int c, float v[8]) {
         const int64_t row = (int64_t)at.m * T::kM + r, col = (int64_t)at.n * T::kN + c;
         if (row < p.m && col < p.n) put_octet<BF16, ADD, PAST>(p.c, row, col, octet_left(p.n - col), p.alpha, p.beta, v);
@@ -175,6 +179,10 @@ size_t q8_product_workspace(int64_t m, int64_t n, int64_t k)
 void launch_q8_product(const Q8ProductArgs &a, bool bf16, hipStream_t st)
 {
     const Choice c = choose(a.m, a.n, a.k);
+    // What the dies' caches do not hold goes past them, so that operands stay there: 8192 x 8192 x 2048 bf16 122 / 134 us; but not rows that end within 64 bytes, of which
+    // halves would be written twice, and not what is read first (beta).
+    const int64_t size = bf16 ? 2 : 4, ends = (a.c.pitch * size) | (int64_t)reinterpret_cast<uintptr_t>(a.c.data);
+    const bool past = a.m * a.n * size > (int64_t)32 << 20 && ends % 64 == 0;
     by_bool(a.a_e5m2 != 0, [&](auto e5m2) {
         by_bool(bf16, [&](auto b) {
             // C in fp32 is summed in fp32 throughout; what the instructions of 8 bits cut off is an eighth of C's rounding to bf16 and less.
@@ -194,12 +202,13 @@ void launch_q8_product(const Q8ProductArgs &a, bool bf16, hipStream_t st)
                     hipLaunchKernelGGL((k_q8_join<B, ADD>), dim3((unsigned)(((uint64_t)a.m * octets + 255) / 256)), dim3(256), 0, st, a, c.parts, octets);
                 } else if (c.tiles == kTiny) {
                     launch_tiles<K, B, ADD, false, 2, 2, 2, 2, 4, 2>(a, c, st);
-                } else if (c.tiles == kSmall) {
-                    launch_tiles<K, B, ADD, false, 2, 2, 4, 4, 2, 2>(a, c, st);
-                } else if (c.tiles == kWide) {
-                    launch_tiles<K, B, ADD, false, 4, 2, 4, 4, 3, 2>(a, c, st);
                 } else {
-                    launch_tiles<K, B, ADD, false, 2, 4, 8, 4, 2, 2>(a, c, st);
+                    by_bool(past && !ADD, [&](auto p) {
+                        constexpr bool PAST = decltype(p)::value;
+                        if (c.tiles == kSmall) launch_tiles<K, B, ADD, PAST && !ADD, 2, 2, 4, 4, 2, 2>(a, c, st);
+                        else if (c.tiles == kWide) launch_tiles<K, B, ADD, PAST && !ADD, 4, 2, 4, 4, 3, 2>(a, c, st);
+                        else launch_tiles<K, B, ADD, PAST && !ADD, 2, 4, 8, 4, 2, 2>(a, c, st);
+                    });
                 }
             });
         });

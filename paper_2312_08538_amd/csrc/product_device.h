@@ -352,6 +352,46 @@ struct Tile {
         }
     }
 
+    // alpha times the product to C in bf16, rounded on its way through LDS, where a row of 64 columns takes 128 bytes and sixteen more
+    template <bool PAST>
+    static __device__ __forceinline__ void store_bf16(const Sums &acc, uint8_t *lds, const RowsOut &c, int64_t m, int64_t n, int64_t m0, int64_t n0, float alpha)
+    {
+        constexpr int kRow = TN * 32 + 16, kAcross = TN * 2, kHigh = 64 / kAcross;
+        const int lane = threadIdx.x & 63;
+        uint8_t *mine = lds + wave() * 32 * kRow;
+        wait_loads<0>();
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < TM; i += 2) {
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int j = 0; j < TN; ++j) {
+                    const f32x4 v = acc[j][i + h];
+                    *reinterpret_cast<uint2 *>(mine + (h * 16 + (lane & 15)) * kRow + j * 32 + 8 * (lane >> 4)) =
+                        make_uint2(pack_bf16(alpha * v[0], alpha * v[1]), pack_bf16(alpha * v[2], alpha * v[3]));
+                }
+            __builtin_amdgcn_wave_barrier();
+#pragma unroll
+            for (int t = 0; t < 32 / kHigh; ++t) {
+                const int r = t * kHigh + lane / kAcross, q = lane % kAcross;
+                const int64_t row = m0 + (wave_m() * TM + i) * 16 + r, col = n0 + wave_n() * TN * 16 + q * 8;
+                const uint4 w = *reinterpret_cast<const uint4 *>(mine + r * kRow + q * 16);
+                if (row >= m || col >= n) continue;
+                uint16_t *to = static_cast<uint16_t *>(c.data) + row * c.pitch + col;
+                if (col + 8 <= n) {
+                    store_16<PAST>(to, u32x4_any{w.x, w.y, w.z, w.w});
+                } else {
+                    const uint32_t e[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+                    for (int k = 0; k < 7; ++k)
+                        if (col + k < n) to[k] = (uint16_t)(e[k >> 1] >> (16 * (k & 1)));
+                }
+            }
+            __builtin_amdgcn_wave_barrier();
+        }
+    }
+
     // 32 rows (tiles i and i + 1) of a wave to its part of LDS
     static __device__ __forceinline__ void turn(const Sums &acc, int i, float *mine)
     {
