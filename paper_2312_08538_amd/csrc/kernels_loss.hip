@@ -7,7 +7,6 @@
 // instructions take them; w and x are turned for that (k_loss_turn), which is a pass over memory where a product is width (tokens) times as much work.
 // A sum over the vocabulary goes from piece to piece in fp32.
 #include <algorithm>
-#include <cstdint>
 
 #include "product_device.h"
 #include "turned_device.h"
@@ -81,13 +80,17 @@ template <int KIND, bool BY_ROWS, int WM, int WN, int TM, int TN, int STAGES, in
 __global__ __launch_bounds__(64 * WM * WN, OCC) void k_loss_logits(StatArgs p, Side a, Side b, Shape z)
 {
     typedef Tile<KIND, BY_ROWS, WM, WN, TM, TN, STAGES> T;
-    __shared__ __attribute__((aligned(1024))) uint8_t lds[T::kBytes];
+    __shared__ __attribute__((aligned(1024))) uint8_t lds[T::kBytes + T::kM * 4];
     if (group_index() >= (uint32_t)z.items) return;
     const Place at = place_of(z, (int)group_index());
+    int *targets = reinterpret_cast<int *>(lds + T::kBytes);         // in the piece, or -1; asked for before the product, read behind it
+    for (int r = threadIdx.x; r < T::kM; r += T::kThreads) {
+        const int64_t row = (int64_t)at.m * T::kM + r, of = row < p.tokens ? p.targets[row] : -1;
+        targets[r] = of >= p.first && of < p.first + p.vocab ? (int)(of - p.first) : -1;
+    }
     typename T::Sums acc;
     T::run(a, b, z, at.m * T::kM, at.n * T::kN, 0, z.steps, lds, acc);
-    const int lane = threadIdx.x & 63;
-    const int64_t col0 = (int64_t)at.n * T::kN + T::wave_n() * TN * 16 + 4 * (lane >> 4);
+    const int lane = threadIdx.x & 63, col0 = at.n * T::kN + T::wave_n() * TN * 16 + 4 * (lane >> 4);
     float2 *red = reinterpret_cast<float2 *>(lds);          // [WN][kM]
     wait_loads<0>();
     __syncthreads();
@@ -103,14 +106,14 @@ __global__ __launch_bounds__(64 * WM * WN, OCC) void k_loss_logits(StatArgs p, S
                 for (int e = 0; e < 4; ++e)
                     if (col0 + j * 16 + e >= p.vocab) acc[j][i][e] = -__builtin_inff();
         }
-        const int64_t of = row < p.tokens ? p.targets[row] : -1, target = of < 0 ? -1 : of - p.first - col0;
+        const int target = targets[r] - col0;              // (none: below 0)
         float most = kLeast;
 #pragma unroll
         for (int j = 0; j < TN; ++j)
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
                 most = fmaxf(most, acc[j][i][e]);
-                if (target == j * 16 + e && (whole || col0 + target < p.vocab)) p.hit[row] = acc[j][i][e];
+                if (target == j * 16 + e) p.hit[row] = acc[j][i][e];
             }
         // (the four lanes that share a row are sixteen apart)
         auto across = [](float v, auto f) {
@@ -228,9 +231,17 @@ __global__ __launch_bounds__(64 * WM * WN, OCC) void k_loss_gradient(GradArgs p,
 {
     typedef Tile<KIND, BY_ROWS, WM, WN, TM, TN, STAGES> T;
     constexpr bool BF16 = is_bf16<KIND>();
-    __shared__ __attribute__((aligned(1024))) uint8_t lds[T::kBytes];
+    __shared__ __attribute__((aligned(1024))) uint8_t lds[T::kBytes + T::kM * sizeof(float4)];
     if (group_index() >= (uint32_t)z.items) return;
     const Place at = place_of(z, (int)group_index());
+    // Of each row its share of the gradient (0: no target), lse, and the target's place in the piece: asked for before the product, read behind it.
+    float4 *about = reinterpret_cast<float4 *>(lds + T::kBytes);
+    for (int r = threadIdx.x; r < T::kM; r += T::kThreads) {
+        const int64_t row = (int64_t)at.m * T::kM + r, of = row < p.tokens ? p.targets[row] : -1;
+        const bool there = of >= 0 && of < p.all, here = of >= p.first && of < p.first + p.vocab;
+        about[r] = make_float4(there ? (p.dloss ? p.dloss[row] / *p.scale : 1.0f) : 0.0f, there ? p.lse[row] : 0.0f, __int_as_float(here ? (int)(of - p.first) : -1),
+                               __int_as_float(there));
+    }
     typename T::Sums acc;
     T::run(a, b, z, at.m * T::kM, at.n * T::kN, 0, z.steps, lds, acc);
     const int lane = threadIdx.x & 63;
@@ -248,24 +259,13 @@ __global__ __launch_bounds__(64 * WM * WN, OCC) void k_loss_gradient(GradArgs p,
             const int r = t * kHigh + lane / kAcross, c = lane % kAcross * 8;
             const int64_t row = row0 + r, col = col0 + c;
             float *from = mine + r * T::kPitch + c;
-            float v[8], share = 0.0f, lse = 0.0f;
-            int64_t target = -1;
-            if (row < p.tokens) {
-                const int64_t of = p.targets[row];
-                if (of >= 0 && of < p.all) {
-                    share = p.dloss ? p.dloss[row] / *p.scale : 1.0f;
-                    lse = p.lse[row];
-                    target = of - p.first - col;
-                } else {
-                    target = INT64_MIN;             // no target: no gradient
-                }
-            } else {
-                target = INT64_MIN;
-            }
+            const float4 of = about[(T::wave_m() * TM + i) * 16 + r];
+            const int target = __float_as_int(of.z) - (int)col;
+            float v[8];
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-                const float d = exp_of(from[e] - lse) - (target == e ? 1.0f : 0.0f);
-                v[e] = target != INT64_MIN && col + e < p.vocab ? share * d : 0.0f;
+                const float d = exp_of(from[e] - of.y) - (target == e ? 1.0f : 0.0f);
+                v[e] = __float_as_int(of.w) && col + e < p.vocab ? of.x * d : 0.0f;         // (no target: whatever the logits are)
             }
             *reinterpret_cast<f32x4 *>(from) = f32x4{v[0], v[1], v[2], v[3]};
             *reinterpret_cast<f32x4 *>(from + 4) = f32x4{v[4], v[5], v[6], v[7]};
