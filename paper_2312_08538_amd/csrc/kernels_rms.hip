@@ -101,6 +101,13 @@ __device__ __forceinline__ void load_columns(const float *p, int cols, int t, fl
     for (int v = 0; v < V; ++v) finish<false, G>(o[v], cols - 8 * (t + G * v), cols, out[v]);
 }
 
+// 1 / sqrt(v), from the instruction's 2^-23 by a step whose error is that to the third power; 0 and infinity as they are
+__device__ __forceinline__ double inverse_root(double v)
+{
+    const double y = __builtin_amdgcn_rsq(v), e = __builtin_fma(-v * y, y, 1.0), z = __builtin_fma(y * e, __builtin_fma(0.375, e, 0.5), y);
+    return y > 0.0 && y < __builtin_inf() ? z : y;
+}
+
 // A value of 64 bits in 32, rounded to odd (the last bit set if anything is lost): what is rounded from there to fewer bits is as if rounded from the value itself.
 __device__ __forceinline__ float to_odd(double v)
 {
@@ -137,6 +144,7 @@ __global__ __launch_bounds__(threads_of(G)) void k_rms_forward(RmsArgs a, int64_
     int turn = 0;
     const int t = threadIdx.x % G, mine = threadIdx.x / G;
     const int64_t rows = H ? padded_rows : a.rows;
+    const double inv = 1.0 / (double)a.cols;
     Octet<BF16> x[V] = {}, r[FUSED ? V : 1] = {};
     auto fetch = [&](int64_t from) {
 #pragma unroll
@@ -152,6 +160,7 @@ __global__ __launch_bounds__(threads_of(G)) void k_rms_forward(RmsArgs a, int64_
     for (int64_t group = blockIdx.x; group * kGroup < rows; group += gridDim.x) {
 #pragma unroll 1
         for (int i = 0; i < kPer; ++i) {
+            if (H && group * kGroup + i * kRows >= a.rows) break;               // (of what fills the operand up there is nothing to compute)
             const int64_t row = group * kGroup + i * kRows + mine;
             const bool there = row < a.rows;
             float z[V][8];
@@ -174,7 +183,7 @@ __global__ __launch_bounds__(threads_of(G)) void k_rms_forward(RmsArgs a, int64_
 #pragma unroll
                 for (int e = 0; e < 8; ++e) sum = __builtin_fma((double)z[v][e], (double)z[v][e], sum);
             sum = group_sum<G>(sum, red, turn);
-            const double rstd = 1.0 / sqrt(sum / (double)a.cols + (double)a.eps);
+            const double rstd = inverse_root(__builtin_fma(sum, inv, (double)a.eps));
             if (there && t == 0 && a.rstd_out) a.rstd_out[row] = (float)rstd;
 #pragma unroll
             for (int v = 0; v < V; ++v) {
@@ -185,7 +194,7 @@ __global__ __launch_bounds__(threads_of(G)) void k_rms_forward(RmsArgs a, int64_
                     const uint32_t byte = q8_scale<false>(neighbours_largest<16>(largest(y)));
                     const int square = octet >> 1, at = i * kRows + mine;
                     *reinterpret_cast<uint2 *>(codes + square * (16 * H) + ((at + square) % H) * 16 + (octet & 1) * 8) = q8_codes<false>(y, byte);
-                    if ((octet & 15) == 0 && octet < 16 * pieces) a.packed.scales[(octet >> 4) * padded_rows + row] = (uint8_t)byte;
+                    if (there && (octet & 15) == 0 && octet < 16 * pieces) a.packed.scales[(octet >> 4) * padded_rows + row] = (uint8_t)byte;
                 }
             }
         }
@@ -195,7 +204,10 @@ __global__ __launch_bounds__(threads_of(G)) void k_rms_forward(RmsArgs a, int64_
             uint8_t *to = a.packed.codes + row0 / 16 * pieces * 2048 + row0 % 16 * 16;
             for (int u = threadIdx.x; u < (int)pieces * 8 * H; u += threads_of(G)) {
                 const int square = u / H, at = u % H;
-                *reinterpret_cast<uint4 *>(to + (int64_t)square * 256 + at * 16) = *reinterpret_cast<const uint4 *>(codes + square * (16 * H) + ((at + square) % H) * 16);
+                const bool there = row0 + at < a.rows;
+                const uint4 c = *reinterpret_cast<const uint4 *>(codes + square * (16 * H) + ((at + square) % H) * 16);
+                *reinterpret_cast<uint4 *>(to + (int64_t)square * 256 + at * 16) = there ? c : make_uint4(0, 0, 0, 0);
+                if (!there && (square & 7) == 0) a.packed.scales[(square >> 3) * padded_rows + row0 + at] = 0;
             }
             __syncthreads();
         }
@@ -209,6 +221,7 @@ __global__ __launch_bounds__(kThreads) void k_rms_forward_long(RmsArgs a, int64_
     __shared__ double red[8];
     int turn = 0;
     const bool packed = a.packed.codes != nullptr;
+    const double inv = 1.0 / (double)a.cols;
     for (int64_t row = blockIdx.x; row < (packed ? padded_rows : a.rows); row += gridDim.x) {
         const bool there = row < a.rows;
         const void *src = FUSED ? a.z.data : a.x.data;
@@ -229,7 +242,7 @@ __global__ __launch_bounds__(kThreads) void k_rms_forward_long(RmsArgs a, int64_
             for (int i = 0; i < 8; ++i) sum = __builtin_fma((double)z[i], (double)z[i], sum);
         }
         sum = group_sum<kThreads>(sum, red, turn);
-        const double rstd = 1.0 / sqrt(sum / (double)a.cols + (double)a.eps);
+        const double rstd = inverse_root(__builtin_fma(sum, inv, (double)a.eps));
         if (there && threadIdx.x == 0 && a.rstd_out) a.rstd_out[row] = (float)rstd;
         // (whole blocks: the sixteen lanes that share one go round together)
         for (int64_t col = 8 * threadIdx.x; col < end; col += 8 * kThreads) {

@@ -183,6 +183,27 @@ struct Tile {
         }
     }
 
+    // The same of widened fragments: B's, which all of a step's rows of tiles take, beforehand, where there are registers for them.
+    struct Widened {
+        bf16x8 v[kWide ? TN : 1][4];
+    };
+    static __device__ __forceinline__ void widen(const Fragment (&b)[TN], Widened &out)
+    {
+#pragma unroll
+        for (int j = 0; j < TN; ++j)
+#pragma unroll
+            for (int q = 0; q < 4; ++q) out.v[j][q] = widen_octet<false>(b[j].v[2 * q], b[j].v[2 * q + 1], b[j].scale);
+    }
+    static __device__ __forceinline__ void multiply(const Widened &b, const Fragment &a, Sums &acc, int i)
+    {
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            const bf16x8 y = widen_octet<KIND == Kind::WIDE_E5M2>(a.v[2 * q], a.v[2 * q + 1], a.scale);
+#pragma unroll
+            for (int j = 0; j < TN; ++j) acc[j][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(b.v[j][q], y, acc[j][i], 0, 0, 0);
+        }
+    }
+
     // acc <- rows m0 .. of A times rows n0 .. of B, over `steps` steps from `first` on.  Rows beyond an operand's last are some other of its
     // rows (what comes of them is not used).
     static __device__ __forceinline__ void run(const Side &a, const Side &b, const Shape &z, int m0, int n0, int first, int steps, uint8_t *lds, Sums &acc)
@@ -271,6 +292,8 @@ struct Tile {
         auto step = [&](int s, auto more, Fragment (&now)[TN], auto &next) {
             constexpr bool kMore = decltype(more)::value;                               // there is a step to fetch
             const int after = slot + 1 == STAGES ? 0 : slot + 1;
+            Widened wide;
+            if constexpr (kWide && kTwice) widen(now, wide);
             unroll<TM>([&](auto index) {
                 constexpr int I = decltype(index)::value, kTurn = TM - kRing;           // from here on the next step's fragments are read
                 if constexpr (!kTwice && I == TM - 1) {
@@ -282,6 +305,8 @@ struct Tile {
 #pragma unroll
                         for (int j = J; j < J + kHalf; ++j) read_b(after, j, now[j]);
                     });
+                } else if constexpr (kWide && kTwice) {
+                    multiply(wide, ring[I % kRing], acc, I);
                 } else {
                     multiply(now, ring[I % kRing], acc, I);
                 }
