@@ -568,7 +568,8 @@ int conef_rms_backward(int64_t rows, int64_t cols, int dtype, const void *dy, in
  * A target outside 0 .. vocab - 1 is none: its loss is 0 and it adds nothing to the gradients.
  * x                device, in, tokens x width of dtype                 w         device, in, vocab x width of dtype
  * targets          device, in, tokens 64-bit integers
- * loss, lse        device, out, tokens floats each; lse is what the backward pass takes (either may be null, not both)
+ * loss, lse        device, out, tokens floats each; lse is what the backward pass takes (either may be null, not both, and they
+ *                  must not be the same buffer)
  * dloss            device, in, tokens floats, the loss's gradient, may be null: 1 each
  * dx               device, out, tokens x width of dtype      dw   device, out (beta = 0: not read), vocab x width of dtype.  Either may be null, not both.
  *                  They must not overlap an input.

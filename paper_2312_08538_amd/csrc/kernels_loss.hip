@@ -183,17 +183,22 @@ __global__ __launch_bounds__(1024) void k_loss_join(const float2 *stats, const f
 }
 
 // ---------------------------------------------------------------- backward
-// The largest finite magnitude of dloss, or 1 if that is 0.
-__global__ __launch_bounds__(1024) void k_loss_scale(const float *dloss, int64_t tokens, float *scale)
+// The largest finite magnitude of dloss among tokens that have a target, or 1 if that is 0.
+__global__ __launch_bounds__(1024) void k_loss_scale(const float *dloss, const int64_t *targets, int64_t tokens, int64_t vocab, float *scale)
 {
     __shared__ float red[16];
     float most = 0.0f;
     for (int64_t i = threadIdx.x; i < tokens; i += 8 * 1024) {
         float v[8];
+        int64_t of[8];
 #pragma unroll
-        for (int u = 0; u < 8; ++u) v[u] = i + 1024 * u < tokens ? fabsf(dloss[i + 1024 * u]) : 0.0f;
+        for (int u = 0; u < 8; ++u) {
+            const int64_t t = min(i + 1024 * u, tokens - 1);
+            v[u] = fabsf(dloss[t]);
+            of[u] = targets[t];
+        }
 #pragma unroll
-        for (int u = 0; u < 8; ++u) most = v[u] < __builtin_inff() ? fmaxf(most, v[u]) : most;
+        for (int u = 0; u < 8; ++u) most = v[u] < __builtin_inff() && of[u] >= 0 && of[u] < vocab ? fmaxf(most, v[u]) : most;
     }
 #pragma unroll
     for (int d = 32; d; d /= 2) most = fmaxf(most, __shfl_xor(most, d));
@@ -337,7 +342,7 @@ __global__ __launch_bounds__(64 * WM * WN, OCC) void k_loss_product(SumArgs p, S
 template <bool BF16>
 __global__ __launch_bounds__(256) void k_loss_parts(SumArgs p, int parts, uint32_t octets_a_row)
 {
-    const uint64_t t = (uint64_t)blockIdx.x * 256 + threadIdx.x;
+    const uint64_t t = (uint64_t)group_index() * 256 + threadIdx.x;
     const int64_t row = (int64_t)(t / octets_a_row), col = (int64_t)(t % octets_a_row) * 8;
     if (row >= p.m) return;
     const int left = octet_left(p.n - col);
@@ -565,7 +570,7 @@ void product(SumArgs p, const uint8_t *a, const uint8_t *b, int64_t depth, float
     by_tiles<is_bf16<KIND>()>(c.tiles, go);
     if (c.parts > 1) {
         const uint32_t octets = (uint32_t)((p.n + 7) / 8);
-        hipLaunchKernelGGL((k_loss_parts<OUT>), dim3((unsigned)(((uint64_t)p.m * octets + 255) / 256)), dim3(256), 0, st, p, c.parts, octets);
+        hipLaunchKernelGGL((k_loss_parts<OUT>), grid_of((p.m * octets + 255) / 256), dim3(256), 0, st, p, c.parts, octets);
     }
 }
 
@@ -578,13 +583,13 @@ void backward(const LossArgs &a, hipStream_t st)
         SumArgs p;
         p.m = a.vocab, p.n = a.width, p.alpha = 0.0f, p.beta = a.beta, p.out = a.dw;
         const uint32_t octets = (uint32_t)((p.n + 7) / 8);
-        if (a.dw.data) hipLaunchKernelGGL((k_loss_parts<BF16>), dim3((unsigned)(((uint64_t)p.m * octets + 255) / 256)), dim3(256), 0, st, p, 0, octets);
+        if (a.dw.data) hipLaunchKernelGGL((k_loss_parts<BF16>), grid_of((p.m * octets + 255) / 256), dim3(256), 0, st, p, 0, octets);
         return;
     }
     const bool direct = in_place(a, l.esz);
     if (!direct) pack<BF16>(a.x, a.tokens, a.width, l.depth_w, a.workspace + l.x, st);
     float *scale = a.dloss ? reinterpret_cast<float *>(a.workspace + l.scale) : nullptr;
-    if (scale) hipLaunchKernelGGL(k_loss_scale, dim3(1), dim3(1024), 0, st, a.dloss, a.tokens, scale);
+    if (scale) hipLaunchKernelGGL(k_loss_scale, dim3(1), dim3(1024), 0, st, a.dloss, a.targets, a.tokens, a.vocab, scale);
     if (a.dw.data) turn<BF16>(a.x, a.tokens, a.width, a.workspace + l.x_t, st);
     float *partials = reinterpret_cast<float *>(a.workspace + l.parts), *grown = reinterpret_cast<float *>(a.workspace + l.grown);
     for (int64_t first = 0; first < a.vocab; first += l.piece) {

@@ -411,7 +411,7 @@ int conef_loss_forward(int64_t tokens, int64_t vocab, int64_t width, int dtype, 
     LossArgs a;
     if (bad_loss(tokens, vocab, width, dtype)) return CONEF_EINVAL;
     if (tokens == 0) return CONEF_OK;
-    if (bad_rows(x, x_pitch, width, dtype) || bad_rows(w, w_pitch, width, dtype) || !targets || misaligned(targets, 8) || (!loss && !lse) ||
+    if (bad_rows(x, x_pitch, width, dtype) || bad_rows(w, w_pitch, width, dtype) || !targets || misaligned(targets, 8) || (!loss && !lse) || (loss && loss == lse) ||
         misaligned(loss, 4) || misaligned(lse, 4) || !workspace || misaligned(workspace, 256))
         return CONEF_EINVAL;
     a.tokens = tokens;

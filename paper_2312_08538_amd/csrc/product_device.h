@@ -89,7 +89,7 @@ __device__ __forceinline__ bf16x8 widen_octet(int lo, int hi, int byte)
 
 constexpr int kCus = 256;
 
-static __device__ const uint32_t kZeros[4] = {};
+static __device__ const uint4 kZeros = {};
 
 // An operand.  By rows: `rows` of them, `pitch` bytes apart, pitch (below 2^29) and address multiples of 16.  Packed: squares of 16 rows and 16 bytes,
 // 256 bytes each, eight of them a step (2048 bytes), the steps of 16 rows one after the other; `rows` a multiple of 16.
@@ -249,7 +249,7 @@ struct Tile {
                 const bool beyond = ((lane & 7) ^ (lane >> 3)) * 16 >= (first + s + 1 == z.steps ? z.last : 128);
 #pragma unroll
                 for (int i = kFrom; i < kTo; ++i)
-                    to_lds<16>(beyond ? reinterpret_cast<const uint8_t *>(kZeros) : src[i] + (int64_t)s * 128 + off[i], to + (w + i * kWaves) * 1024);
+                    to_lds<16>(beyond ? reinterpret_cast<const uint8_t *>(&kZeros) : src[i] + (int64_t)s * 128 + off[i], to + (w + i * kWaves) * 1024);
             } else {
 #pragma unroll
                 for (int i = kFrom; i < kTo; ++i) wave_to_lds<16>(src[i] + (int64_t)s * 2048, to + (w + i * kWaves) * 1024);

@@ -574,6 +574,57 @@ def test_large_loss(env, tokens, vocab, width, bf16):  # noqa: F811
     assert not bool(dx[~there].any())
 
 
+def test_weights_of_tokens_without_a_target_do_not_count(env):  # noqa: F811
+    torch, B = env
+    g, x, w, t = loss_inputs(70, 300, 64, True)
+    X, W, targets = column_vector(torch, x).bfloat16(), column_vector(torch, w).bfloat16(), torch.from_numpy(t).cuda()
+    there = (targets >= 0) & (targets < 300)
+    st, ws = B.Model.stream_handle(), room_of(torch, B.conef_loss_workspace(70, 300, 64, torch.bfloat16))
+    lse, outs = torch.empty(70, device="cuda:0"), []
+    B.conef_loss_forward(X, W, targets, None, lse, ws, st)
+    for elsewhere in (0.0, 1e30, float("inf"), float("nan")):
+        dloss = torch.where(there, torch.full((70,), 3e-4, device="cuda:0"), elsewhere)
+        dx, dw = torch.empty_like(X), torch.empty_like(W)
+        B.conef_loss_backward(X, W, targets, lse, dloss, 1.0, 0.0, dx, dw, ws, st)
+        outs.append((dx, dw))
+    for dx, dw in outs[1:]:
+        assert torch.equal(dx, outs[0][0]) and torch.equal(dw, outs[0][1])
+
+
+@pytest.mark.parametrize("tokens,vocab,width,bf16", [(70001, 40009, 16, True), (66001, 9, 33336, True), (9, 66001, 33337, True), (66001, 5, 17000, False)])
+def test_loss_beyond_31_bits(env, tokens, vocab, width, bf16):  # noqa: F811
+    """More than 2^31 logits, or elements of x or of w (the last two at least 4 GB): the first and last tokens' losses and gradients, the last words' gradient."""
+    torch, B = env
+    dt, st = torch.bfloat16 if bf16 else torch.float32, B.Model.stream_handle()
+    g = torch.Generator(device="cuda:0").manual_seed(9)
+    x, w = torch.zeros(tokens, width, dtype=dt, device="cuda:0"), torch.zeros(vocab, width, dtype=dt, device="cuda:0")
+    rows, words = [0, 1, tokens - 2, tokens - 1], [0, 1, vocab - 2, vocab - 1]
+    for r in rows:
+        x[r] = torch.randn(width, device="cuda:0", generator=g).to(dt)
+    for r in words:
+        w[r] = (torch.randn(width, device="cuda:0", generator=g) / width ** 0.5).to(dt)
+    t = torch.full((tokens,), -1, device="cuda:0")
+    t[rows] = torch.tensor([words[3], words[0], words[2], words[3]], device="cuda:0")
+    loss, lse = torch.full((tokens,), 7.0, device="cuda:0"), torch.full((tokens,), 7.0, device="cuda:0")
+    ws = torch.empty(B.conef_loss_workspace(tokens, vocab, width, dt), dtype=torch.uint8, device="cuda:0")
+    B.conef_loss_forward(x, w, t, loss, lse, ws, st)
+    X, W = x[rows].double(), w[words].double()
+    logits = torch.mm(X, W.t())                                   # of these four words; all others' are 0
+    total = torch.logsumexp(torch.cat((logits, torch.zeros(4, vocab - 4, dtype=torch.float64, device="cuda:0")), 1), 1)
+    at = torch.tensor([3, 0, 2, 3], device="cuda:0")
+    e = 4 * 2.0 ** -23 * width ** 0.5 * 2 + 80 * U + 3 * U * total
+    assert bool(((lse[rows].double() - total).abs() <= e).all())
+    assert bool(((loss[rows].double() - (total - logits.gather(1, at[:, None])[:, 0])).abs() <= 2 * e).all())
+    assert not bool(loss[2:-2].any())
+    dx, dw = torch.full_like(x, 7.0), torch.full_like(w, 7.0)
+    B.conef_loss_backward(x, w, t, lse, None, 1.0, 0.0, dx, dw, ws, st)
+    d = torch.exp(logits - total[:, None])
+    d[torch.arange(4), at] -= 1
+    for got, want in ((dx[rows], torch.mm(d, W)), (dw[words], torch.mm(d.t(), X))):
+        assert float((got.double() - want).norm() / want.norm()) <= (1.5 * U16 if bf16 else 1e-4)
+    assert not bool(dx[2:-2].any())
+
+
 def test_loss_of_no_tokens(env):  # noqa: F811
     torch, B = env
     st = B.Model.stream_handle()

@@ -75,12 +75,12 @@ def test_norm_refuses_bad_arguments():
 def test_loss_refuses_bad_arguments():
     L = B.lib()
 
-    def fwd(t=4, v=9, d=8, dtype=0, x=P, xp=8, w=P, wp=8, targets=P, loss=P, lse=P, ws=P):
+    def fwd(t=4, v=9, d=8, dtype=0, x=P, xp=8, w=P, wp=8, targets=P, loss=P, lse=2 * P, ws=P):
         return L.conef_loss_forward(t, v, d, dtype, x, xp, w, wp, targets, loss, lse, ws, 0)
 
     sizes = [dict(t=-1), dict(v=0), dict(d=0), dict(v=-3), dict(t=1 << 30), dict(v=1 << 30), dict(d=1 << 30, xp=1 << 30, wp=1 << 30), dict(t=1 << 20, v=1 << 15),
              dict(v=1 << 18, d=1 << 17, xp=1 << 17, wp=1 << 17), dict(dtype=2), dict(dtype=-1)]
-    for bad in sizes + [dict(x=0), dict(w=0), dict(x=P + 2), dict(w=P + 2), dict(xp=7), dict(wp=7), dict(targets=0), dict(targets=P + 4), dict(loss=0, lse=0),
+    for bad in sizes + [dict(x=0), dict(w=0), dict(x=P + 2), dict(w=P + 2), dict(xp=7), dict(wp=7), dict(targets=0), dict(targets=P + 4), dict(loss=0, lse=0), dict(loss=2 * P),
                         dict(loss=P + 2), dict(lse=P + 2), dict(ws=0), dict(ws=P + 128)]:
         assert fwd(**bad) == B.EINVAL, bad
     assert fwd(t=0, x=0, w=0, targets=0, loss=0, lse=0, ws=0) == B.OK

@@ -45,7 +45,7 @@ LOSSES = [(1, 1, 1), (1, (1 << 30) - 1, 24), ((1 << 30) - 1, 1, 8), (1 << 18, (1
 @pytest.mark.parametrize("dtype", [0, 1])
 @pytest.mark.parametrize("skew", [0, 4])                 # what lies as the kernels take it, and what is packed first
 def test_losses_of_every_size(record, tokens, vocab, width, dtype, skew):  # noqa: F811
-    calls = [("conef_loss_forward", [tokens, vocab, width, dtype, P, width, P + skew, width, P, P, P, P, 0]),
+    calls = [("conef_loss_forward", [tokens, vocab, width, dtype, P, width, P + skew, width, P, P, 2 * P, P, 0]),
              ("conef_loss_backward", [tokens, vocab, width, dtype, P, width, P + skew, width, P, P, P, 1.0, 0.0, 2 * P, width, 3 * P, width, P, 0])]
     for code, seen in record(calls):
         assert code == 0 and seen
@@ -77,7 +77,7 @@ def test_every_kernel_is_reached(record):  # noqa: F811
                         calls.append(("conef_q8_product", [P, P, form, P, P, m, n, k, 1.0, beta, c, n, dtype, P, 0]))
         for tokens, vocab, width in ((16, 50304, 768), (64, 300, 64), (200, 3000, 300), (1000, 5000, 500), (2048, 2048, 2048), (4096, 50304, 2048), (16, 50304, 2048), (4096, 4096, 512), (9000, 9000, 24), (16384, 10000, 4096)):
             for skew in (0, 4):
-                calls += [("conef_loss_forward", [tokens, vocab, width, dtype, P, width, P + skew, width, P, P, P, P, 0]),
+                calls += [("conef_loss_forward", [tokens, vocab, width, dtype, P, width, P + skew, width, P, P, 2 * P, P, 0]),
                           ("conef_loss_backward", [tokens, vocab, width, dtype, P, width, P + skew, width, P, P, P, 1.0, 0.5, 2 * P, width, 3 * P, width, P, 0])]
     reached = set()
     for code, seen in record(calls):
