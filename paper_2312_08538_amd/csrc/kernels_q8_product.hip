@@ -203,11 +203,11 @@ void launch_q8_product(const Q8ProductArgs &a, bool bf16, hipStream_t st)
                 } else if (c.tiles == kTiny) {
                     launch_tiles<K, B, ADD, false, 2, 2, 2, 2, 4, 2>(a, c, st);
                 } else {
-                    by_bool(past && !ADD, [&](auto p) {
-                        constexpr bool PAST = decltype(p)::value;
-                        if (c.tiles == kSmall) launch_tiles<K, B, ADD, PAST && !ADD, 2, 2, 4, 4, 2, 2>(a, c, st);
-                        else if (c.tiles == kWide) launch_tiles<K, B, ADD, PAST && !ADD, 4, 2, 4, 4, 3, 2>(a, c, st);
-                        else launch_tiles<K, B, ADD, PAST && !ADD, 2, 4, 8, 4, 2, 2>(a, c, st);
+                    by_bool(past, [&](auto p) {
+                        constexpr bool PAST = decltype(p)::value && !ADD;
+                        if (c.tiles == kSmall) launch_tiles<K, B, ADD, PAST, 2, 2, 4, 4, 2, 2>(a, c, st);
+                        else if (c.tiles == kWide) launch_tiles<K, B, ADD, PAST && !B, 4, 2, 4, 4, 3, 2>(a, c, st);          // (fewer than 192 large tiles are no 32 MB in bf16)
+                        else launch_tiles<K, B, ADD, PAST, 2, 4, 8, 4, 2, 2>(a, c, st);
                     });
                 }
             });
