@@ -20,6 +20,19 @@ constexpr float kLeast = -3.402823466e38f;              // below every logit but
 
 __device__ __forceinline__ float exp_of(float v) { return __builtin_amdgcn_exp2f(v * kLog2e); }
 
+// fp32: with what rounding v log2(e) leaves out, |v| 2^-24 of the result otherwise
+template <int KIND>
+__device__ __forceinline__ float exp_of(float v)
+{
+    if constexpr (KIND == Kind::F32) {
+        constexpr float kRest = 1.92596298e-8f, kLn2 = 0.693147181f;             // log2(e) = kLog2e + kRest
+        const float t = v * kLog2e, r = __builtin_fmaf(v, kRest, __builtin_fmaf(v, kLog2e, -t)), e = __builtin_amdgcn_exp2f(t);
+        return e > 0.0f && e < __builtin_inff() ? __builtin_fmaf(e * kLn2, r, e) : e;
+    } else {
+        return exp_of(v);
+    }
+}
+
 template <int KIND>
 constexpr bool is_bf16() { return KIND == Kind::BF16; }
 
@@ -127,7 +140,7 @@ __global__ __launch_bounds__(64 * WM * WN, OCC) void k_loss_logits(StatArgs p, S
 #pragma unroll
         for (int j = 0; j < TN; ++j)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) sum += exp_of(acc[j][i][e] - most);
+            for (int e = 0; e < 4; ++e) sum += exp_of<KIND>(acc[j][i][e] - most);
         sum = across(sum, [](float x, float y) { return x + y; });
         if (lane < 16) red[T::wave_n() * T::kM + r] = make_float2(most, sum);
     }
@@ -269,7 +282,7 @@ __global__ __launch_bounds__(64 * WM * WN, OCC) void k_loss_gradient(GradArgs p,
             float v[8];
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-                const float d = exp_of(from[e] - of.y) - (target == e ? 1.0f : 0.0f);
+                const float d = exp_of<KIND>(from[e] - of.y) - (target == e ? 1.0f : 0.0f);
                 v[e] = __float_as_int(of.w) && col + e < p.vocab ? of.x * d : 0.0f;         // (no target: whatever the logits are)
             }
             *reinterpret_cast<f32x4 *>(from) = f32x4{v[0], v[1], v[2], v[3]};
