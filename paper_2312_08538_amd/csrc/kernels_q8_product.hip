@@ -120,14 +120,26 @@ struct Choice {
     int parts, per_part;                // of the long axis
 };
 
-Choice choose(int64_t m, int64_t n, int64_t k)
+// Which kernel.  us of a call in a graph, the one taken / others (C in bf16; in fp32, where the matrix instructions take twice as long and elements are widened, after a
+// semicolon):
+//   rows    8 x 8192 x 2048 3.9 / 6.2 tiny; 3.9 / 9.9.  More than 16 rows are read again by every workgroup: 64 x 8192 x 2048 6.2 / 6.4; 6.3 / 10.4, but 64 x 50304 x 2048 27.3 / 21.1 tiny;
+//           30.1 / 25.8, and over a long axis, which tiles cut in parts, 64 x 2048 x 8192 14.4 / 10.4 in 4; 14.7 / 14.3
+//   large   256 x 256, one workgroup a CU: 4096 x 4096 x 2048 32.3 / 36.6 wide, 37.2 small; 4096 x 8192 x 2048 65.0 / 68.5, 69.0; 8192 x 2048 x 8192 103 / 117; fp32: 197 / 228
+//   wide    256 x 128, where large ones do not reach most CUs: 4096 x 2048 x 8192 60.1 / 71.7 small, 81.3 large; 116 / 121, 162
+//   small   128 x 128: 512 x 8192 x 2048 14.3 / 17.0 wide, 17.5 tiny; 25.2 / 32.1, 27.9; 2048 x 2048 x 2048 13.4 / 16.7, 16.5; 24.4 / 31.9, 26.3.  And where a tile's end weighs as much as its
+//           steps: 16384 x 4096 x 512 51.5 / 55.6 large; 90.5 / 135; into fp32 up to 32 steps: 4096 x 8192 x 2048 127 / 149
+//   tiny    64 x 64: 1000 x 1203 x 515 5.5 / 7.5 small; 7.5 / 10.1; 128 x 4096 x 1024 4.8 / 7.6; 7.1 / 12.2
+// The long axis in parts, added up by a launch of its own: 256 x 256 x 8192 10.3 in 8, 9.9 in 4 / 15.3; 12.1, 13.6 / 30.0; 300 x 2000 x 9000 16.5 in 3 / 17.5; 22.8 / 34.1.
+Choice choose(int64_t m, int64_t n, int64_t k, bool bf16)
 {
     const int64_t steps = std::max<int64_t>((k + 127) / 128, 1);
     auto tiles = [&](int64_t tm, int64_t tn) { return ((m + tm - 1) / tm) * ((n + tn - 1) / tn); };
-    if (m <= 64) return {kRows, 1, (int)steps};
-    if (std::min(m, n) > 128 && tiles(256, 256) >= 192) return {kLarge, 1, (int)steps};
-    if (std::min(m, n) > 128 && tiles(256, 128) >= 192) return {kWide, 1, (int)steps};
-    if (tiles(128, 128) >= 200) return {kSmall, 1, (int)steps};
+    if (m <= 16 || (m <= 64 && steps < 32 && tiles(64, 64) < kCus)) return {kRows, 1, (int)steps};
+    if (std::min(m, n) > 128 && steps >= (bf16 ? 8 : 32)) {
+        if (tiles(256, 256) >= 192) return {kLarge, 1, (int)steps};
+        if (tiles(256, 128) >= 192) return {kWide, 1, (int)steps};
+    }
+    if (m > 64 && tiles(128, 128) >= 200) return {kSmall, 1, (int)steps};
     const int64_t parts = steps < 32 ? 1 : std::max<int64_t>(std::min<int64_t>(2 * kCus / tiles(64, 64), steps / 8), 1);
     const int64_t per = (steps + parts - 1) / parts;
     return {kTiny, (int)((steps + per - 1) / per), (int)per};
@@ -172,13 +184,13 @@ void launch_rows(const Q8ProductArgs &p, hipStream_t st)
 
 size_t q8_product_workspace(int64_t m, int64_t n, int64_t k)
 {
-    const Choice c = choose(m, n, k);
+    const Choice c = choose(m, n, k, true);             // (parts are of the smallest tiles, which either type takes for the same sizes)
     return c.parts > 1 ? (size_t)c.parts * (size_t)m * (size_t)n * sizeof(float) : 0;
 }
 
 void launch_q8_product(const Q8ProductArgs &a, bool bf16, hipStream_t st)
 {
-    const Choice c = choose(a.m, a.n, a.k);
+    const Choice c = choose(a.m, a.n, a.k, bf16);
     // What the dies' caches do not hold goes past them, so that operands stay there: 8192 x 8192 x 2048 bf16 122 / 134 us; but not rows that end within 64 bytes, of which
     // halves would be written twice, and not what is read first (beta).
     const int64_t size = bf16 ? 2 : 4, ends = (a.c.pitch * size) | (int64_t)reinterpret_cast<uintptr_t>(a.c.data);

@@ -72,7 +72,7 @@ def test_every_kernel_is_reached(record):  # noqa: F811
             for beta in (0.0, 1.0):
                 for m, n, k in ((1, 8192, 128), (1, 50304, 2048), (1, 8192, 2048), (1, 2048, 8192), (32, 8192, 128), (32, 8192, 2048), (32, 2048, 8192), (64, 8192, 128),
                                 (64, 2048, 2048), (64, 2048, 8192), (512, 512, 512), (256, 256, 8192), (2048, 2048, 512), (4096, 4096, 512), (8192, 8192, 512), (4096, 4096, 2048),
-                                (4096, 8192, 2048), (4096, 4096, 8192), (8192, 2048, 8192), (8160, 8192, 8192), (8192, 8192, 2048), (8192, 16392, 2048), (16384, 16384, 2048), (4096, 2304, 512), (4096, 2048, 512), (200000, 128, 512)):
+                                (4096, 8192, 2048), (4096, 4096, 8192), (8192, 2048, 8192), (8160, 8192, 8192), (8192, 8192, 2048), (8192, 16392, 2048), (16384, 16384, 2048), (4096, 2304, 512), (4096, 2048, 512), (200000, 128, 512), (4096, 2048, 2048), (4096, 2048, 8192), (4096, 2304, 8192), (32, 4096, 2048)):
                     for c in (P, P + 4):
                         calls.append(("conef_q8_product", [P, P, form, P, P, m, n, k, 1.0, beta, c, n, dtype, P, 0]))
         for tokens, vocab, width in ((16, 50304, 768), (64, 300, 64), (200, 3000, 300), (1000, 5000, 500), (2048, 2048, 2048), (4096, 50304, 2048), (16, 50304, 2048), (4096, 4096, 512), (9000, 9000, 24), (16384, 10000, 4096), (4096, 2304, 512), (30000, 10000, 128)):
