@@ -134,6 +134,8 @@ __device__ __forceinline__ void norm_octet(const RmsArgs &a, const float z[8], c
 // G lanes hold a row, V octets each: octet v of lane t starts at column 8 (t + G v), so that sixteen lanes hold a block.  The next row's octets are on their way while
 // a row is worked on.  H > 0: a packed output.  A workgroup then takes H neighbouring rows, since a line of packed codes holds four of them (a square of 256 bytes
 // sixteen): the codes wait in LDS, a square's rows turned by its index, so that the lanes of a wave write to different banks.
+// Bound by memory: 16384 x 2048 bf16 with residual and codes, 235 MB, 42 us (5.6 TB/s); 777 x 5003 fp32 13.0 us (a copy's rate: 9.9); 64 x 2048 3.5 us, of
+// which a launch is 2.6.
 template <bool BF16, int G, int V, bool FUSED, int H>
 __global__ __launch_bounds__(threads_of(G)) void k_rms_forward(RmsArgs a, int64_t padded_rows, int64_t pieces)
 {
@@ -272,6 +274,7 @@ __device__ __forceinline__ void finish_dz(const RmsArgs &a, int64_t row, int64_t
     store_octet<BF16>(a.dz.data, row * a.dz.pitch + col, left, v);
 }
 
+// Bound by memory: 16384 x 2048 bf16 with dz_in, 268 MB, 47 us with the sums behind it (5.7 TB/s); 777 x 5003 fp32 18 (three rows a CU, one after the other).
 // Each workgroup takes every gridDim-th row (or 256 / G of them) and keeps its share of dgamma in registers, since a lane sees the same columns
 // in every row; k_rms_columns adds the shares.  The next row's octets are on their way while a row is worked on.
 template <bool BF16, int G, int V>
@@ -429,7 +432,7 @@ __global__ __launch_bounds__(1024) void k_rms_columns(const float *partials, int
     const int lane = threadIdx.x & 63, part = threadIdx.x >> 6;
     const int64_t c = (int64_t)group_index() * 64 + lane, n = cols;
     double s = 0.0;
-    if (c < n) {
+    if (c < n && parts > 0) {
         int p = part;
         for (; p + 112 < parts; p += 128) {                 // eight loads on their way at a time
             float v[8];
@@ -438,11 +441,12 @@ __global__ __launch_bounds__(1024) void k_rms_columns(const float *partials, int
 #pragma unroll
             for (int u = 0; u < 8; ++u) s += (double)v[u];
         }
-        float v[8];
+        float v[8];                                         // (loaded without a branch: eight that wait for one another cost 500 x 8192 fp32 1.3 us)
 #pragma unroll
-        for (int u = 0; u < 8; ++u) v[u] = p + 16 * u < parts ? partials[(p + 16 * u) * n + c] : 0.0f;
+        for (int u = 0; u < 8; ++u) v[u] = partials[min(p + 16 * u, parts - 1) * n + c];
 #pragma unroll
-        for (int u = 0; u < 8; ++u) s += (double)v[u];
+        for (int u = 0; u < 8; ++u)
+            if (p + 16 * u < parts) s += (double)v[u];
     }
     red[part][lane] = s;
     __syncthreads();
@@ -452,7 +456,9 @@ __global__ __launch_bounds__(1024) void k_rms_columns(const float *partials, int
     dgamma[c] = (float)s;
 }
 
-// Lanes to a row and octets a lane.
+// Lanes to a row and octets a lane: the fewest that hold a row in 8 or 16 columns each up to 1024 columns, so that a row ends without a barrier and a
+// workgroup has several (16384 x 1024 bf16 on 64 lanes 21.3 us, the three quarters as many elements of 8192 x 1536 on 256 lanes 21.8); beyond that an octet a lane, since a
+// row's values of 64 bits are many registers.
 template <typename F>
 void by_width(int64_t cols, F &&go)
 {
@@ -469,8 +475,9 @@ void by_width(int64_t cols, F &&go)
     else go(integral_constant<int, 1024>{}, One{});
 }
 
-// Workgroups of the backward pass: about as many as the card holds at a time, but four rows each where that leaves one a CU: their shares of dgamma are
-// written and read again.
+// Workgroups of the backward pass: about as many as the card holds at a time, but four rows each (two of the widest) where that leaves one a CU: their shares of dgamma are
+// written and read again.  us / with as many as there are rows: 512 x 2048 bf16 7.9 / 9.3, 1024 x 2048 9.9 / 10.6, 300 x 8192 11.8 / 13.2; in between / with the whole number
+// that the card holds: 1500 x 2048 11.6 / 11.9, 500 x 8192 fp32 18.7 / 19.4.
 int64_t parts_of(int64_t rows, int64_t cols)
 {
     int64_t most = 512, few = 256, least = 4;
@@ -506,7 +513,10 @@ void launch_rms_forward(const RmsArgs &a, bool bf16, hipStream_t st)
             }
             by_width(a.cols, [&](auto g, auto v) {
                 constexpr int G = decltype(g)::value, V = decltype(v)::value, kRows = threads_of(G) / G;
-                constexpr int kHigh = G * V <= 512 ? 16 : 8, kLow = kRows > 4 ? kRows : 4;
+                constexpr int kFew = kRows, kLow = kRows > 4 ? kRows : 4, kHigh = G <= 64 || G == 512 ? 16 : G == 256 ? 4 : 8;
+                // Rows a workgroup, us: one row, so that all CUs work, 64 x 2048 bf16 3.5, 256 x 8192 7.4 / four rows 6.6, 12.6; four 2048 x 2048 9.7, 1024 x 8192 15 / one row 10.9, 24.  Whole
+                // squares of codes where 512 workgroups have them: 8192 x 4096 43.3, 16384 x 1024 21.3, 4096 x 8192 (half ones) 45.6 / four rows 44.8, eight rows 23.1, four 51.0;
+                // but not on 256 threads, whose rows follow one another: 16384 x 2048 sixteen rows 43.3 / four 41.0, 8192 x 2048 27.3 / 23.5.
                 auto go = [&](auto h) {
                     constexpr int H = decltype(h)::value, kGroup = H ? H : kRows;
                     const int64_t groups = (rows + kGroup - 1) / kGroup;
@@ -514,8 +524,9 @@ void launch_rms_forward(const RmsArgs &a, bool bf16, hipStream_t st)
                                        pieces);
                 };
                 if (!packed) go(std::integral_constant<int, 0>{});
-                else if (kLow == kHigh || rows >= 512 * kHigh) go(std::integral_constant<int, kHigh>{});
-                else go(std::integral_constant<int, kLow>{});
+                else if (rows <= 512) go(std::integral_constant<int, kFew>{});
+                else if (rows < 512 * kHigh) go(std::integral_constant<int, kLow>{});
+                else go(std::integral_constant<int, kHigh>{});
             });
         });
     });
