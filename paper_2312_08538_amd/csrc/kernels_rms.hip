@@ -513,10 +513,10 @@ void launch_rms_forward(const RmsArgs &a, bool bf16, hipStream_t st)
             }
             by_width(a.cols, [&](auto g, auto v) {
                 constexpr int G = decltype(g)::value, V = decltype(v)::value, kRows = threads_of(G) / G;
-                constexpr int kFew = kRows, kLow = kRows > 4 ? kRows : 4, kHigh = G <= 64 || G == 512 ? 16 : G == 256 ? 4 : 8;
+                constexpr int kFew = kRows, kLow = kRows > 4 ? kRows : 4, kHigh = G <= 512 ? 16 : 8, kFull = G == 256 ? 1024 : 512;
                 // Rows a workgroup, us: one row, so that all CUs work, 64 x 2048 bf16 3.5, 256 x 8192 7.4 / four rows 6.6, 12.6; four 2048 x 2048 9.7, 1024 x 8192 15 / one row 10.9, 24.  Whole
                 // squares of codes where 512 workgroups have them: 8192 x 4096 43.3, 16384 x 1024 21.3, 4096 x 8192 (half ones) 45.6 / four rows 44.8, eight rows 23.1, four 51.0;
-                // but not on 256 threads, whose rows follow one another: 16384 x 2048 sixteen rows 43.3 / four 41.0, 8192 x 2048 27.3 / 23.5.
+                // 1024 workgroups of one row at a time in 256 threads: with the values' launch behind it 16384 x 2048 113 us a step / four rows 118, but 8192 x 2048 27.3 alone / 23.6.
                 auto go = [&](auto h) {
                     constexpr int H = decltype(h)::value, kGroup = H ? H : kRows;
                     const int64_t groups = (rows + kGroup - 1) / kGroup;
@@ -525,7 +525,7 @@ void launch_rms_forward(const RmsArgs &a, bool bf16, hipStream_t st)
                 };
                 if (!packed) go(std::integral_constant<int, 0>{});
                 else if (rows <= 512) go(std::integral_constant<int, kFew>{});
-                else if (rows < 512 * kHigh) go(std::integral_constant<int, kLow>{});
+                else if (rows < kFull * kHigh) go(std::integral_constant<int, kLow>{});
                 else go(std::integral_constant<int, kHigh>{});
             });
         });
