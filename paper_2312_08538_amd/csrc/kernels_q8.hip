@@ -18,6 +18,7 @@ constexpr int kThreads = 256;
 // A workgroup takes 64 rows of 128 columns, or 128 rows of 128 columns if it quantises by columns too.  By rows: a wave takes 16 rows, four lanes each; a lane reads four
 // octets 32 columns apart, so that four lanes read 64 bytes (bf16) together, and half a wave writes a square of 256 bytes at a time.  By columns: the same on the tile in
 // LDS, turned, 16 columns a wave.
+// Bound by memory: 8192 x 8192 bf16 by rows 30.2 us, by columns 30.1 (6.7 TB/s), both ways of one read 42.1 (6.4); fp32 57.6, 58.9 and 73.6 (6.0).
 template <bool BF16, bool E5M2, bool BY_ROWS, bool BY_COLS>
 __global__ __launch_bounds__(BY_COLS ? 512 : 256) void k_q8_quantise(Q8QuantArgs a, int64_t row_pieces, int64_t col_pieces, int64_t padded_rows,
                                                                      int64_t padded_cols)
@@ -77,7 +78,8 @@ __global__ __launch_bounds__(BY_COLS ? 512 : 256) void k_q8_quantise(Q8QuantArgs
     }
 }
 
-// What a packed operand stands for: 16 rows a wave, 128 columns, so that a store writes 128 bytes of each of eight rows.
+// What a packed operand stands for: 16 rows a wave, 128 columns, so that a store writes 128 bytes of each of eight rows.  Bound by memory: 8192 x 8192 into bf16 30.9 us
+// (6.5 TB/s), into fp32 50.3 (6.7).
 template <bool BF16, bool E5M2, bool PAST>
 __global__ __launch_bounds__(kThreads) void k_q8_dequantise(Q8DequantArgs a, int64_t pieces, int64_t groups, int64_t padded_rows)
 {
@@ -142,7 +144,7 @@ void launch_q8_dequantise(const Q8DequantArgs &a, bool bf16, hipStream_t st)
 {
     const int64_t pieces = (a.cols + 127) / 128, groups = (a.rows + 15) / 16, padded_rows = (a.rows + 63) / 64 * 64;
     const dim3 grid = grid_of((pieces * groups + 3) / 4);
-    // (past the caches as the 4-bit values are, and for the same reasons)
+    // Past the caches, where these do not hold what is written anyway and no line is written in halves: 8192 x 8192 into fp32 50 us / 67, into bf16 30.9 / 30.9.
     const int64_t size = bf16 ? 2 : 4;
     const bool whole = a.out.pitch * size % 64 == 0 && reinterpret_cast<uintptr_t>(a.out.data) % 64 == 0;
     const bool past = whole && a.rows * a.cols * size > (int64_t)32 << 20;

@@ -1,6 +1,10 @@
 // C = alpha A B^T + beta C of two packed operands of 8-bit floating point with a scale for each block of 128, on the matrix instructions that take such
-// operands with powers of two as scales (v_mfma_scale_f32_32x32x64_f8f6f4, 16x16x128 for few rows): the scale costs nothing, and a sum stays in
-// its register from the first step of the long axis to the last.
+// operands with powers of two as scales (v_mfma_scale_f32_16x16x128_f8f6f4): the scale costs nothing, and a sum stays in
+// its register from the first step of the long axis to the last.  C in fp32 is summed by the instructions of 16 bits (Kind::WIDE_*).
+//
+// What bounds it: on random operands these instructions alone reach 4.1 to 4.3 PFLOP/s here (the 32 x 32 x 64 ones 3.7 to 3.8), since the card lowers its clock to stay within its power, and
+// what moves operands to them draws on the same power: 8192 x 8192 x 2048 into bf16 121 us, 2.3 PFLOP/s, of which 134 MB of C are 26 us at a copy's rate and overlap little; 8192 x 2048 x 8192 103 us,
+// 2.7 PFLOP/s.  Into fp32 312 and 206 (0.9 and 1.3 PFLOP/s; 16-bit instructions alone: 1.9 to 2.0).
 #include <algorithm>
 
 #include "product_device.h"
@@ -34,7 +38,8 @@ __global__ __launch_bounds__(64 * WM * WN, OCC) void k_q8_product(Q8ProductArgs 
 }
 
 // Few rows of A (16 MT at most): a workgroup takes 16 rows of B, read once, straight to registers; its WAVES waves take steps of the long axis in
-// turn, and their sums are added in order.  Elements are widened for it: the products hide behind the loads.
+// turn, and their sums are added in order.  Elements are widened for it: the products hide behind the loads.  Bound by B's bytes where B is large (1 x 50304 x 2048 17.5 us,
+// 5.9 TB/s), else by the way to memory and back: 8 x 8192 x 2048 3.8 us, a launch 2.6.
 template <bool E5M2, bool BF16, bool ADD, int MT, int WAVES>
 __global__ __launch_bounds__(64 * WAVES) void k_q8_rows(Q8ProductArgs p, int steps, int64_t a_rows, int64_t b_rows)
 {
@@ -171,6 +176,7 @@ void launch_rows(const Q8ProductArgs &p, hipStream_t st)
         hipLaunchKernelGGL((k_q8_rows<E5M2, BF16, ADD, decltype(mt)::value, W>), grid_of(groups), dim3(64 * W), 0, st, p, steps, (p.m + 63) / 64 * 64,
                            (p.n + 63) / 64 * 64);
     };
+    // Eight waves where there are few workgroups, or a long axis keeps each busy: 8 x 2048 x 8192 5.5 us / 6.7 on four, 16 x 1024 x 16384 7.2 / 8.4, 8 x 8192 x 2048 3.8 / 3.8.
     auto by_waves = [&](auto mt) {
         if (steps > 4 && (groups < 2 * kCus || steps >= 64)) go(mt, std::integral_constant<int, 8>{});
         else go(mt, std::integral_constant<int, 4>{});

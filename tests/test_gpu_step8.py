@@ -138,8 +138,8 @@ def wide_error(magnitudes, k):
 
 
 def cut_error(A, W, k, xp=np):
-    """C in bf16, by the instructions of 8 bits: a product loses less than 2^-12 of the largest one of the 64 of its instruction, of which no more is known
-    than that it is at most the product of both operands' largest."""
+    """C in bf16, by the instructions of 8 bits: a product loses less than 2^-12 of the largest one of the 128 of its instruction, of which no more is known
+    than that it is at most the product of both operands' largest.  Held to the largest of its 64, which is no more than that."""
     total = 0
     for f in range(0, k, 64):
         a, w = abs(A[:, f:f + 64]), abs(W[:, f:f + 64])
