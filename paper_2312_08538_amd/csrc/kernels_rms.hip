@@ -134,7 +134,7 @@ __device__ __forceinline__ void norm_octet(const RmsArgs &a, const float z[8], c
 // G lanes hold a row, V octets each: octet v of lane t starts at column 8 (t + G v), so that sixteen lanes hold a block.  The next row's octets are on their way while
 // a row is worked on.  H > 0: a packed output.  A workgroup then takes H neighbouring rows, since a line of packed codes holds four of them (a square of 256 bytes
 // sixteen): the codes wait in LDS, a square's rows turned by its index, so that the lanes of a wave write to different banks.
-// Bound by memory: 16384 x 2048 bf16 with residual and codes, 235 MB, 42 us (5.6 TB/s); 777 x 5003 fp32 13.0 us (a copy's rate: 9.9); 64 x 2048 3.5 us, of
+// Bound by memory: 16384 x 2048 bf16 with residual and codes, 235 MB, 43 us (5.4 TB/s); 777 x 5003 fp32 13.0 us (a copy's rate: 9.9); 64 x 2048 3.5 us, of
 // which a launch is 2.6.
 template <bool BF16, int G, int V, bool FUSED, int H>
 __global__ __launch_bounds__(threads_of(G)) void k_rms_forward(RmsArgs a, int64_t padded_rows, int64_t pieces)
