@@ -364,6 +364,36 @@ def depth(cols):
 
 
 @pytest.mark.parametrize("bf16", [False, True])
+@pytest.mark.parametrize("fused", [False, True])
+@pytest.mark.parametrize("rows,cols", [(600, 1100), (16390, 1100), (513, 2100), (8195, 2100), (700, 4200), (4100, 4200), (600, 6200), (4097, 6200)])
+def test_norm_of_many_rows_is_that_of_few(env, rows, cols, bf16, fused):  # noqa: F811
+    """How many rows a workgroup takes goes by their number; a row's results do not: bit for bit those of calls on 448 rows each."""
+    torch, B = env
+    dtype = torch.bfloat16 if bf16 else torch.float32
+    g = torch.Generator(device="cuda:0").manual_seed(rows + cols)
+    x, r = (torch.randn(rows, cols, device="cuda:0", generator=g).to(dtype) for _ in range(2))
+    gamma = torch.rand(cols, device="cuda:0", generator=g) + 0.5
+
+    def norm(x, r):
+        n = x.shape[0]
+        z, y, rstd, q = torch.empty_like(x), torch.empty_like(x), torch.empty(n, device="cuda:0"), B.q8_alloc(n, cols)
+        for t in q:
+            t.fill_(0xAA)
+        B.conef_rms_forward(1e-5, x, r if fused else None, gamma, z if fused else None, y, q, rstd, B.Model.stream_handle())
+        pieces = -(-cols // 128)
+        return (z if fused else x), y, rstd, q[0].view(-1, pieces * 2048), q[1].view(pieces, -1).t()
+
+    whole = norm(x, r)
+    for at in range(0, rows, 448):
+        n = min(448, rows - at)
+        z, y, rstd, codes, scales = norm(x[at:at + n], r[at:at + n])
+        assert torch.equal(whole[0][at:at + n], z) and torch.equal(whole[1][at:at + n], y) and torch.equal(whole[2][at:at + n], rstd)
+        assert torch.equal(whole[3][at // 16:at // 16 + codes.shape[0]], codes) and torch.equal(whole[4][at:at + scales.shape[0]], scales)
+    assert not bool(whole[3].view(-1, -(-cols // 128), 8, 16, 16).transpose(1, 3).reshape(-1, 8 * -(-cols // 128) * 16)[rows:].any())
+    assert not bool(whole[4][rows:].any())
+
+
+@pytest.mark.parametrize("bf16", [False, True])
 @pytest.mark.parametrize("rows,cols", NORM_SHAPES)
 @pytest.mark.parametrize("skip,gap,residual", [(0, 0, False), (1, 3, True)])
 def test_norm_backward(env, rows, cols, bf16, skip, gap, residual):  # noqa: F811
