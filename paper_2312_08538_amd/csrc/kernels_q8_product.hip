@@ -139,7 +139,8 @@ Choice choose(int64_t m, int64_t n, int64_t k, bool bf16)
 {
     const int64_t steps = std::max<int64_t>((k + 127) / 128, 1);
     auto tiles = [&](int64_t tm, int64_t tn) { return ((m + tm - 1) / tm) * ((n + tn - 1) / tn); };
-    if (m <= 16 || (m <= 64 && steps < 32 && tiles(64, 64) < kCus)) return {kRows, 1, (int)steps};
+    // (no columns: no tiles, whose number divides below, and no launch)
+    if (n == 0 || m <= 16 || (m <= 64 && steps < 32 && tiles(64, 64) < kCus)) return {kRows, 1, (int)steps};
     if (std::min(m, n) > 128 && steps >= (bf16 ? 8 : 32)) {
         if (tiles(256, 256) >= 192) return {kLarge, 1, (int)steps};
         if (tiles(256, 128) >= 192) return {kWide, 1, (int)steps};
