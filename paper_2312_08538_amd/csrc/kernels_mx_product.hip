@@ -603,7 +603,8 @@ Choice choose(int64_t m, int64_t n, int64_t k)
     const int64_t pieces = std::max<int64_t>((k + 127) / 128, 1);
     auto tiles = [&](int64_t tm, int64_t tn) { return ((m + tm - 1) / tm) * ((n + tn - 1) / tn); };
     const bool deep = m > 16 && tiles(64, 64) >= kCus && (m + 15) / 16 * pieces >= 64;
-    if (m <= 64 && !deep) return {kRows, 1, (int)pieces};
+    // (no columns: no tiles, whose number divides below, and no launch)
+    if (n == 0 || (m <= 64 && !deep)) return {kRows, 1, (int)pieces};
     if (std::min(m, n) > 128 && tiles(256, 256) >= 192 && pieces >= 12) return {tiles(256, 256) >= 4 * kCus ? kStream : pieces >= 32 ? kLarge : kWide, 1, (int)pieces};
     if (tiles(128, 128) >= 200) return {kSmall, 1, (int)pieces};
     const int64_t parts = pieces < 64 ? 1 : std::max<int64_t>(std::min<int64_t>(kCus / tiles(64, 64), pieces / 16), 1);

@@ -57,11 +57,11 @@ def run(code, *args):
 
 
 @pytest.mark.parametrize("m,n,k", SHAPES)
-@pytest.mark.parametrize("name", ["q8"])
+@pytest.mark.parametrize("name", ["q8", "mx"])
 def test_a_product_of_nothing_needs_nothing(name, m, n, k):
     run(SIZES, name, m, n, k)
 
 
-@pytest.mark.parametrize("name", ["q8"])
+@pytest.mark.parametrize("name", ["q8", "mx"])
 def test_the_binding_takes_a_product_of_no_columns(name):
     run(BINDING, name, 100, 0, 8192)
