@@ -566,7 +566,7 @@ int conef_rms_backward(int64_t rows, int64_t cols, int dtype, const void *dy, in
  *   lse_i = log(sum over v of exp(l_iv))      loss_i = lse_i - l_(i, target_i)
  * and its gradient: with d_iv = dloss_i (exp(l_iv - lse_i) - [v = target_i])
  *   dx = d w                                  dw <- alpha d^T x + beta dw
- * A target outside 0 .. vocab - 1 is none: its loss is 0 and it adds nothing to the gradients.
+ * A target outside 0 .. vocab - 1 is none: its loss is 0 and it adds nothing to the gradients, whatever its row of x holds.
  * x                device, in, tokens x width of dtype                 w         device, in, vocab x width of dtype
  * targets          device, in, tokens 64-bit integers
  * loss, lse        device, out, tokens floats each; lse is what the backward pass takes (either may be null, not both, and they
