@@ -4,7 +4,7 @@
 // instructions take twice as long as those of 32 here and hide behind the loads: a value that lies next to a border of the 8-bit grid is rounded to the
 // side that it is on, and y, the codes and rstd are each rounded once.  With a = dy gamma and hat = z rstd:
 //   dz = rstd (a - hat mean(a hat)) + dz_in,   dgamma = sum over rows of dy hat,
-// in fp32 (its results are not rounded to 8 bits), sums over rows in fp64 at the last level, in a fixed order.
+// in fp32 (its results are not rounded to 8 bits), sums over rows in fp64 at the last level, in a fixed order; a long row's mean in fp64.
 #include <algorithm>
 #include <type_traits>
 
@@ -372,16 +372,18 @@ __global__ __launch_bounds__(threads_of(G)) void k_rms_backward(RmsArgs a)
     }
 }
 
-// Rows of more than 8192 columns: two sweeps by a workgroup; the sums over rows are k_rms_column_parts's, which reads dy and z once more.
+// Rows of more than 8192 columns: two sweeps by a workgroup; the sums over rows are k_rms_column_parts's, which reads dy and z once more.  The mean is
+// summed in 64 bits: a lane's share of a row has no bound here, and in 32 the mean of 3000001 equal terms was off by 4.8e-6 of itself, 80 times 2^-24.
 template <bool BF16>
 __global__ __launch_bounds__(kThreads) void k_rms_backward_long(RmsArgs a)
 {
-    __shared__ float red[8];
+    __shared__ double red[8];
     int turn = 0;
-    const float inv = 1.0f / (float)a.cols;
+    const double inv = 1.0 / (double)a.cols;
     for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
         const float rstd = a.rstd[row];
-        float sum = 0.0f, z[8], dy[8], gamma[8], w[8];
+        double sum = 0.0;
+        float z[8], dy[8], gamma[8], w[8];
         for (int64_t col = 8 * threadIdx.x; col < a.cols; col += 8 * kThreads) {
             const int left = octet_left(a.cols - col);
             load_octet<BF16>(a.z_in.data, row * a.z_in.pitch + col, left, z);
@@ -389,9 +391,9 @@ __global__ __launch_bounds__(kThreads) void k_rms_backward_long(RmsArgs a)
             load_octet<false>(a.gamma, col, left, gamma);
 #pragma unroll
             for (int i = 0; i < 8; ++i)
-                if (i < left) sum = __builtin_fmaf(dy[i] * gamma[i], z[i] * rstd, sum);
+                if (i < left) sum = __builtin_fma((double)(dy[i] * gamma[i]), (double)(z[i] * rstd), sum);
         }
-        const float mean = group_sum<kThreads>(sum, red, turn) * inv;
+        const float mean = (float)(group_sum<kThreads>(sum, red, turn) * inv);
         for (int64_t col = 8 * threadIdx.x; col < a.cols; col += 8 * kThreads) {
             const int left = octet_left(a.cols - col);
             load_octet<BF16>(a.z_in.data, row * a.z_in.pitch + col, left, z);
