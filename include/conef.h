@@ -576,7 +576,9 @@ int conef_rms_backward(int64_t rows, int64_t cols, int dtype, const void *dy, in
  *                  They must not overlap an input.
  * Logits and all sums are fp32; the backward pass makes the logits again, a piece of the vocabulary at a time, and rounds d to dtype for the products that
  * take it.
- * workspace        device, conef_loss_workspace() bytes (of either pass), 256-byte aligned
+ * workspace        device, conef_loss_workspace() bytes (of either pass), 256-byte aligned.  It holds no logits and no whole w of more than some 2^28 elements, but x twice, and twice the
+ *                  gradient of a piece's logits: tokens times 4096 columns at least, so it grows with the tokens (65536 of 50304 x 2048 bf16: 2.2 GB); batches beyond
+ *                  that may be passed in parts, with beta = 1 for dw, which is rounded to dtype after each
  * tokens, vocab, width < 2^30, width and vocab at least 1; also tokens ceil(vocab / 8), tokens ceil(width / 8), vocab ceil(width / 8) < 2^32 */
 int conef_loss_workspace(int64_t tokens, int64_t vocab, int64_t width, int dtype, size_t *bytes);
 int conef_loss_forward(int64_t tokens, int64_t vocab, int64_t width, int dtype, const void *x, int64_t x_pitch, const void *w, int64_t w_pitch,

@@ -383,10 +383,12 @@ inline int64_t up(int64_t v, int64_t to) { return (v + to - 1) / to * to; }
 
 // Columns of the vocabulary that are worked on at a time: d of some 2^25 elements, which with its two forms the card's last cache holds, but 4096 columns at least
 // (a product's long axis, and the bytes of dx that go from piece to piece).  4096 x 50304 x 2048, both passes: 2^24 elements 3210 us, 2^25 3100, 2^26 3135, 2^27 3080 in four times the
-// workspace.
-int64_t piece_of(int64_t tokens, int64_t vocab)
+// workspace.  Of w, which is turned (and packed, if it has to be) a piece at a time, some 2^28 elements, so that few tokens of a wide w do not need all of it once more: 16 x 256000 x 8192
+// bf16 backward 5.2 ms in 0.55 GB / 4.6 in 4.3 as one piece / 5.4 in 2^27 elements / 5.7 in 2^26; 64 x 100000 x 4096 1055 us / 1020 as one.
+int64_t piece_of(int64_t tokens, int64_t vocab, int64_t width)
 {
-    const int64_t v = std::max<int64_t>(((int64_t)1 << 25) / std::max<int64_t>(tokens, 1) / 256 * 256, 4096);
+    const int64_t most = std::min(((int64_t)1 << 25) / std::max<int64_t>(tokens, 1), ((int64_t)1 << 28) / width);
+    const int64_t v = std::max<int64_t>(most / 256 * 256, 4096);
     return vocab <= v + v / 4 ? vocab : v;
 }
 
@@ -444,7 +446,7 @@ Cut cut_of(int64_t m, int64_t n, int64_t steps, bool bf16)
 }
 
 // The workspace: both passes' packed x and a piece's packed w (where these do not lie as the kernels take them); forward: a row's statistics by tiles; backward: d by rows and by
-// columns, a piece of w turned, x turned, dx as it grows, parts of a long axis.
+// columns, a piece of w turned (in the place of the packed one, which only the launch before it reads), x turned, dx as it grows, parts of a long axis.
 struct Layout {
     int64_t piece, esz, depth_w;                            // depth_w: bytes of a row of x or w, up to 128
     size_t x, w, stats, hit, scale, rows, cols, w_t, x_t, grown, parts, end;
@@ -454,7 +456,7 @@ Layout layout_of(int64_t tokens, int64_t vocab, int64_t width, bool bf16)
 {
     Layout l;
     l.esz = bf16 ? 2 : 4;
-    l.piece = piece_of(tokens, vocab);
+    l.piece = piece_of(tokens, vocab, width);
     l.depth_w = up(width * l.esz, 128);
     size_t at = 0;
     auto take = [&](size_t bytes) {
@@ -464,7 +466,7 @@ Layout layout_of(int64_t tokens, int64_t vocab, int64_t width, bool bf16)
     };
     const int64_t t64 = up(tokens, 64), v64 = up(l.piece, 64), d64 = up(width, 64);
     l.x = take((size_t)t64 * l.depth_w);
-    l.w = take((size_t)v64 * l.depth_w);
+    l.w = l.w_t = take((size_t)v64 * std::max(l.depth_w, d64 * l.esz));
     const size_t shared = at;
     l.stats = take((size_t)tokens * ((vocab + 63) / 64 + vocab / l.piece + 1) * sizeof(float2));
     l.hit = take((size_t)tokens * sizeof(float));
@@ -473,7 +475,6 @@ Layout layout_of(int64_t tokens, int64_t vocab, int64_t width, bool bf16)
     l.scale = take(sizeof(float));
     l.rows = take((size_t)t64 * v64 * l.esz);
     l.cols = take((size_t)t64 * v64 * l.esz);
-    l.w_t = take((size_t)d64 * v64 * l.esz);
     l.x_t = take((size_t)d64 * t64 * l.esz);
     l.grown = take(l.piece < vocab ? (size_t)tokens * width * sizeof(float) : 0);
     size_t most = 0;
