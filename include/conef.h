@@ -545,7 +545,8 @@ int conef_q8_product(const uint8_t *a_codes, const uint8_t *a_scales, int a_form
 /* Root-mean-square norm over each row, with a residual in front of it and its output in 8 bits:
  *   z = residual + x     y = z rstd gamma,  rstd = 1 / sqrt(mean(z^2) + eps)
  * The sum is rounded to dtype; the rest is computed from that in 64 bits and rounded once, to y, to the codes and to rstd_out, so that codes are those of
- * the norm itself.
+ * the norm itself, not of y in dtype (elements below 2^-126, where bf16 and codes are concerned, to a multiple of 2^-149 first).  There is no output by columns: codes of y's transpose, which a
+ * weight's gradient takes, are conef_q8_quantise's of y, which in CONEF_BF16 has been rounded before.
  * residual, z_out  both or neither; without them z is x
  * gamma            device, in, cols floats          rstd_out   device, out, rows floats, may be null
  * y                device, out, may be null          codes, scales   device, out, both or neither: y by rows as a packed operand of CONEF_E4M3

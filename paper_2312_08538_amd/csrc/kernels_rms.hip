@@ -108,7 +108,8 @@ __device__ __forceinline__ double inverse_root(double v)
     return y > 0.0 && y < __builtin_inf() ? z : y;
 }
 
-// A value of 64 bits in 32, rounded to odd (the last bit set if anything is lost): what is rounded from there to fewer bits is as if rounded from the value itself.
+// A value of 64 bits in 32, rounded to odd (the last bit set if anything is lost): what is rounded from there to fewer bits is as if rounded from the value itself.  That holds for
+// magnitudes of 2^-126 and more; below, the cast rounds to nearest, to a multiple of 2^-149, and the second rounding may go the other way for a value within 2^-150 of a tie.
 __device__ __forceinline__ float to_odd(double v)
 {
     const uint64_t b = __builtin_bit_cast(uint64_t, v);
