@@ -482,7 +482,7 @@ void by_width(int64_t cols, F &&go)
 // written and read again.  us / with as many as there are rows: 512 x 2048 bf16 7.9 / 9.3, 1024 x 2048 9.9 / 10.6, 300 x 8192 11.8 / 13.2; in between / with the whole number
 // that the card holds: 1500 x 2048 11.6 / 11.9, 500 x 8192 fp32 18.7 / 19.4.
 // A lane adds its rows' terms in fp32, kMostAdded of them at the most, so that its sum's error has a bound: of more rows there are whole turns of workgroups
-// (in one turn 20000000 rows of five equal terms were off by 1.2e-5 of their sum).  us / in one turn: 131072 x 2048 bf16 321 / 305, 40000 x 4096 193 / 180, 1000000 x 700 876 / 1070.
+// (in one turn the sum of 20000000 equal terms, five columns of them, was off by 1.2e-5).  us / in one turn: 131072 x 2048 bf16 321 / 305, 40000 x 4096 193 / 180, 1000000 x 700 876 / 1070.
 constexpr int64_t kMostAdded = 128;
 int64_t parts_of(int64_t rows, int64_t cols)
 {
@@ -529,6 +529,10 @@ void launch_rms_forward(const RmsArgs &a, bool bf16, hipStream_t st)
                 // Rows a workgroup, us: one row, so that all CUs work, 64 x 2048 bf16 3.5, 256 x 8192 7.4 / four rows 6.6, 12.6; four 2048 x 2048 9.7, 1024 x 8192 15 / one row 10.9, 24.  Whole
                 // squares of codes where 512 workgroups have them: 8192 x 4096 43.3, 16384 x 1024 21.3, 4096 x 8192 (half ones) 45.6 / four rows 44.8, eight rows 23.1, four 51.0;
                 // 1024 workgroups of one row at a time in 256 threads: with the values' launch behind it 16384 x 2048 113 us a step / four rows 118, but 8192 x 2048 27.3 alone / 23.6.
+                // And only where their turns are filled to three quarters (of 256 threads, three fifths): 28000 x 2048 80.9 / four rows 85.8, 32000 x 2048 91.6 / 95.4, 20000 x 1024 29.4 /
+                // 30.7, but 17000 x 2048 57.7 / 53.1, 20000 x 2048 64.4 / 64.1, 9000 x 4096 66.6 / 55.7, 12000 x 4096 72.5 / 69.5, 9000 x 1024 15.7 / 14.6, 9000 x 5120 98.1 / 94.2.
+                const int64_t full = kFull * kHigh, turns = (rows + full - 1) / full;
+                const bool filled = rows >= full && (G == 256 ? rows * 5 >= turns * full * 3 : rows * 4 >= turns * full * 3);
                 auto go = [&](auto h) {
                     constexpr int H = decltype(h)::value, kGroup = H ? H : kRows;
                     const int64_t groups = (rows + kGroup - 1) / kGroup;
@@ -537,7 +541,7 @@ void launch_rms_forward(const RmsArgs &a, bool bf16, hipStream_t st)
                 };
                 if (!packed) go(std::integral_constant<int, 0>{});
                 else if (rows <= 512) go(std::integral_constant<int, kFew>{});
-                else if (rows < kFull * kHigh) go(std::integral_constant<int, kLow>{});
+                else if (!filled) go(std::integral_constant<int, kLow>{});
                 else go(std::integral_constant<int, kHigh>{});
             });
         });
