@@ -68,13 +68,21 @@ __global__ __launch_bounds__(256) void k_loss_turn(Rows x, int64_t rows, int64_t
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int64_t strips = padded_cols / 64, group = group_index(), row0 = group / strips * 128, col0 = group % strips * 64, depth = (int64_t)steps * kStep;
     if (row0 >= depth) return;
+    bool there[4];                                      // (beforehand: a target between two octets' loads would keep them apart)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) there[i] = row0 + i * 32 + (threadIdx.x >> 3) < rows;
+    if (targets) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int64_t of = targets[min(row0 + i * 32 + (threadIdx.x >> 3), rows - 1)];
+            there[i] = there[i] && of >= 0 && of < vocab;
+        }
+    }
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         const int r = i * 32 + (threadIdx.x >> 3), c = (threadIdx.x & 7) * 8;
         const int64_t row = row0 + r;
-        bool there = row < rows;
-        if (there && targets) there = targets[row] >= 0 && targets[row] < vocab;
-        tile.put(r, c, fetch_octet<BF16>(x.data, row * x.pitch + col0 + c, there ? octet_left(cols - col0 - c) : 0));
+        tile.put(r, c, fetch_octet<BF16>(x.data, row * x.pitch + col0 + c, there[i] ? octet_left(cols - col0 - c) : 0));
     }
     __syncthreads();
 #pragma unroll
@@ -446,7 +454,7 @@ Cut cut_of(int64_t m, int64_t n, int64_t steps, bool bf16)
 }
 
 // The workspace: both passes' packed x and a piece's packed w (where these do not lie as the kernels take them); forward: a row's statistics by tiles; backward: d by rows and by
-// columns, a piece of w turned (in the place of the packed one, which only the launch before it reads), x turned, dx as it grows, parts of a long axis.
+// columns, a piece of w turned (a large one in the place of the packed one, which only the launch before it reads), x turned, dx as it grows, parts of a long axis.
 struct Layout {
     int64_t piece, esz, depth_w;                            // depth_w: bytes of a row of x or w, up to 128
     size_t x, w, stats, hit, scale, rows, cols, w_t, x_t, grown, parts, end;
@@ -466,7 +474,12 @@ Layout layout_of(int64_t tokens, int64_t vocab, int64_t width, bool bf16)
     };
     const int64_t t64 = up(tokens, 64), v64 = up(l.piece, 64), d64 = up(width, 64);
     l.x = take((size_t)t64 * l.depth_w);
-    l.w = l.w_t = take((size_t)v64 * std::max(l.depth_w, d64 * l.esz));
+    // One place for both forms of a piece of w, but for pieces that the dies' caches hold: writing over what was read there last costs 1001 x 5003 x 515 fp32 244.2 us / 242.4 in two;
+    // one place of 94 MB, 3 x 24640 x 1796 bf16 174 / 197.
+    const size_t packed = (size_t)v64 * l.depth_w, turned = (size_t)v64 * d64 * l.esz;
+    const bool in_one = std::max(packed, turned) > (size_t)32 << 20;
+    l.w = take(in_one ? std::max(packed, turned) : packed);
+    l.w_t = in_one ? l.w : take(turned);
     const size_t shared = at;
     l.stats = take((size_t)tokens * ((vocab + 63) / 64 + vocab / l.piece + 1) * sizeof(float2));
     l.hit = take((size_t)tokens * sizeof(float));
