@@ -575,7 +575,7 @@ int conef_rms_backward(int64_t rows, int64_t cols, int dtype, const void *dy, in
  * targets          device, in, tokens 64-bit integers
  * loss, lse        device, out, tokens floats each; lse is what the backward pass takes (either may be null, not both, and they
  *                  must not be the same buffer)
- * dloss            device, in, tokens floats, the loss's gradient, may be null: 1 each
+ * dloss            device, in, tokens floats, the loss's gradient, may be null: 1 each.  d is formed over the largest finite magnitude of these: what is below 2^-100 of that keeps fewer bits
  * dx               device, out, tokens x width of dtype      dw   device, out (beta = 0: not read), vocab x width of dtype.  Either may be null, not both.
  *                  They must not overlap an input.
  * Logits and all sums are fp32; the backward pass makes the logits again, a piece of the vocabulary at a time, and rounds d to dtype for the products that

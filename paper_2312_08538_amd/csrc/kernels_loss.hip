@@ -152,7 +152,8 @@ __global__ __launch_bounds__(64 * WM * WN, OCC) void k_loss_logits(StatArgs p, S
             r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
             return f(__uint_as_float(r[0]), __uint_as_float(r[1]));
         };
-        most = across(most, [](float x, float y) { return fmaxf(x, y); });
+        // (an infinite logit less the largest finite one is infinity, less itself it would be NaN)
+        most = fminf(across(most, [](float x, float y) { return fmaxf(x, y); }), -kLeast);
         float sum = 0.0f;
 #pragma unroll
         for (int j = 0; j < TN; ++j)
