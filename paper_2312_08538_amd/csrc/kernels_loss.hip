@@ -7,9 +7,9 @@
 // instructions take them; w and x are turned for that (k_loss_turn), which is a pass over memory where a product is width (tokens) times as much work.
 // A sum over the vocabulary goes from piece to piece in fp32.
 //
-// What bounds it: four products, the logits twice.  4096 x 50304 x 2048 bf16, 844 GFLOP each: forward 0.69 ms (1.2 PFLOP/s; storing the logits would add 412 MB twice), backward 2.34 ms, a piece of 8192
-// columns 131 us of gradient, 109 of dx and 105 of dw (1.05, 1.26 and 1.31 PFLOP/s; a library's product of these sizes 1.1 to 1.25 here), 12 of turning w.  1001 x 5003 x 515 fp32, 5.2 GFLOP
-// each: 52, 57, 56, 57 us, where the instructions alone take 33 to 37.
+// What bounds it: four products, the logits twice.  4096 x 50304 x 2048 bf16, 844 GFLOP each: forward 0.67 to 0.69 ms (1.2 PFLOP/s; storing the logits would add 412 MB twice), backward 2.35 to 2.4 ms, a piece of 8192
+// columns 131 us of gradient, 109 of dx and 105 of dw (1.05, 1.26 and 1.31 PFLOP/s; a library's product of these sizes 1.1 to 1.25 here), 12 of turning w; the matrix units are busy in 51 to 63 % of the cycles, waves wait in 30 to 34 % of
+// theirs.  1001 x 5003 x 515 fp32, 5.2 GFLOP each: 52, 57, 56, 57 us, where the instructions alone take 33 to 37.
 #include <algorithm>
 
 #include "product_device.h"

@@ -2,9 +2,10 @@
 // operands with powers of two as scales (v_mfma_scale_f32_16x16x128_f8f6f4): the scale costs nothing, and a sum stays in
 // its register from the first step of the long axis to the last.  C in fp32 is summed by the instructions of 16 bits (Kind::WIDE_*).
 //
-// What bounds it: on random operands these instructions alone reach 4.1 to 4.3 PFLOP/s here (the 32 x 32 x 64 ones 3.7 to 3.8), since the card lowers its clock to stay within its power, and
-// what moves operands to them draws on the same power: 8192 x 8192 x 2048 into bf16 121 us, 2.3 PFLOP/s, of which 134 MB of C are 26 us at a copy's rate and overlap little; 8192 x 2048 x 8192 103 us,
-// 2.7 PFLOP/s.  Into fp32 312 and 206 (0.9 and 1.3 PFLOP/s; 16-bit instructions alone: 1.9 to 2.0).
+// What bounds it: on random operands these instructions alone reach 4.1 to 4.3 PFLOP/s here (the 32 x 32 x 64 ones 3.7 to 3.8).  8192 x 8192 x 2048 into bf16 takes 121 to 125 us, 2.2 PFLOP/s, and
+// 8192 x 2048 x 8192 103 us, 2.7: the matrix units are busy in 51 and 66 % of the cycles and waves wait in 32 and 26 % of theirs, whatever the clock (which falls under load, besides).  Two steps are all that LDS
+// holds of the large tiles, so that a step's loads are waited for from half a step behind the asking on; and of 134 MB of C, 26 us at a copy's rate, little overlaps.
+// Into fp32 240 to 262 and 196 to 204 (1.1 and 1.4 PFLOP/s; 16-bit instructions alone: 1.9 to 2.0): with eight rows of tiles a wave widens B's fragments again for each of them.
 #include <algorithm>
 
 #include "product_device.h"
